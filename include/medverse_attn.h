@@ -259,6 +259,102 @@ mv_status mv_dag_decode_attn_fp8(const mv_plan* plan, const mv_attn_geom* geom, 
                                  const void* v_pages8, const float* kv_scale, void* out, void* workspace,
                                  size_t workspace_bytes, void* cuda_stream);
 
+/* ---- Decode steps planned on the device, over a block-scaled 8-bit cache -------------------------------------------
+ * Three calls that make a decode step without a host step (no counterpart in the paper: a packaging of its decode step and a
+ * storage format): the batch description lives in DEVICE memory, mv_step_tables_build turns it into positions, slots and
+ * block tables, mv_rope_write_kv_fp8_blk fills a cache of 8-bit floats whose scales belong to (page, KV head) and follow
+ * the data, and mv_dag_decode_attn_fp8_blk attends over it.  Lengths that advance on the device need no new launch
+ * arguments, so a step can be captured into a CUDA graph once and replayed while the requests grow.
+ *
+ * The step's tables: device arrays of the caller.  A row is a new token of the step, rows ordered as everywhere (request,
+ * node, token).  The rows of a request are cut into groups of at most rows_per_group consecutive rows (1 .. 64;
+ * rows_per_group * group_size <= 64 for the attention call); a group never holds rows of two requests.  An ENTRY of a group
+ * is four int32 words {page, tokens, mask low, mask high}: the rows of the group whose bits are set see the first `tokens`
+ * (1 .. 16) tokens of the page, and nothing else of the page through this entry.  Entries of a group are ordered by (node, page of the node, tokens);
+ * a page stands there once unless rows see different counts of it (several new tokens in one node).  A TILE is eight
+ * consecutive entries of one group (the last of a group may have fewer).
+ * What lies beyond the step's counts: slot = -1 and pos_id = 0 for unused rows, empty groups (every offset repeats the
+ * total); entries beyond the total are left as they were.  The arrays may also be filled by the caller's own code. */
+typedef struct {
+  int32_t max_rows, max_groups, max_entries; /* capacities; max_groups = max_entries = 0: positions and slots only  */
+  int32_t rows_per_group;
+  int32_t* pos_id;         /* device [max_rows]       position index of every row (Sec. 4.2)                        */
+  int64_t* slot;           /* device [max_rows]       pool slot = page * 16 + offset, -1 = unused row               */
+  int32_t* group_row_off;  /* device [max_groups + 1] CSR over rows       (NULL when max_groups = 0, as the next three) */
+  int32_t* group_ent_off;  /* device [max_groups + 1] CSR over entries                                              */
+  int32_t* group_tile_off; /* device [max_groups + 1] running count of tiles                                        */
+  int32_t* entries;        /* device [max_entries][4], 16-byte aligned                                              */
+  int32_t* counts;         /* device [8]: rows, groups, entries, tiles, status (an mv_status), three zeros          */
+} mv_step_tables;
+
+/* What the launch has to know about the batch (everything else is read on the device). */
+typedef struct {
+  int32_t n_nodes;       /* length of node_len / node_new                                                       */
+  int32_t n_parents;     /* length of parent_idx                                                                */
+  int32_t n_pages;       /* length of page_idx                                                                  */
+  int32_t max_req_nodes; /* most nodes of one request, 1 .. MV_STEP_MAX_REQ_NODES                               */
+  int64_t num_pages;     /* pages of the pool: ids in [0, num_pages) are accepted                               */
+} mv_step_shape;
+#define MV_STEP_MAX_REQ_NODES 2048
+
+/* Positions, slots and block tables of a step from its batch description, on the device (the canonical tables of
+ * mv_plan_dag, and the block tables the attention call below reads).
+ *   batch  the struct itself is read during the call; n_req, page_size, vis_mode and pos_mode are host values, every
+ *          POINTER in it is a DEVICE pointer (4-byte aligned).  A request may have no nodes (node_off repeats), so a batch of fixed
+ *          n_req serves a varying number of live requests.
+ *   tables in: capacities and device pointers; out: the arrays' contents.
+ *   workspace  device, 256-byte aligned, mv_step_tables_workspace_bytes(n_req) bytes, scratch.  Two calls that may
+ *          overlap on the device must not share it, nor the tables.
+ * Errors found on the host: MV_ERR_INVALID_ARG, MV_ERR_WORKSPACE, MV_ERR_UNSUPPORTED (max_req_nodes, rows_per_group), MV_ERR_CUDA.
+ * Errors in the arrays' contents are found on the device: counts[4] then holds the status (the largest, if several
+ * requests are wrong) and the tables describe an empty step, so that the calls below touch nothing:
+ * MV_ERR_NOT_TOPOLOGICAL, MV_ERR_PAGE_CAPACITY, MV_ERR_INVALID_ARG (offsets, negative lengths, a page id outside the
+ * pool), MV_ERR_WORKSPACE (more rows, groups or entries than the capacities), MV_ERR_UNSUPPORTED (a request with more
+ * than max_req_nodes nodes; with block tables also a node with more than 256 new tokens).  mv_step_tables_read_status reads it.  Pages must
+ * belong to one node each (as for mv_plan_dag; not checked). */
+size_t mv_step_tables_workspace_bytes(int32_t n_req);
+mv_status mv_step_tables_build(const mv_dag_batch* batch, const mv_step_shape* shape, const mv_step_tables* tables,
+                               void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Status word of the tables (counts[4]): what the build found, or what the calls below recorded (MV_ERR_TIMEOUT,
+ * MV_ERR_INVALID_ARG for a slot, page or row offset out of range, which they skip).  Synchronises the stream. */
+mv_status mv_step_tables_read_status(const mv_step_tables* tables, void* cuda_stream, int32_t* status);
+
+/* mv_rope_write_kv_fp8 with one scale per (page, KV head), K and V apart, kept by the call itself.
+ * Pools as there: [num_pages][n_kv_heads][page_size][head_dim] bytes.  kv_scale: device float [num_pages][n_kv_heads][2],
+ * the K scale then the V scale of every block; value = stored byte * scale; read and written in place.
+ * A scale is a power of two, 2^-60 .. 2^40: the smallest s for which the block's new tokens have |k| <= 316 s before the
+ * rotation (a rotated element is at most sqrt 2 times the largest raw one, and 316 sqrt 2 < 448), resp. |v| <= 448 s; where
+ * the largest magnitude is exactly at that bound, s or 2 s (ceil(log2(max / 316)) as CUDA's double-precision log2 gives it).  A block
+ * that already holds tokens of its node keeps the larger of its own scale and that one; if it grows, the stored tokens are
+ * moved to it (dividing by a power of two: exact, but for what falls among the format's subnormals, which is rounded to
+ * nearest even).  Values round to nearest even and saturate.  A block that receives an infinity or a NaN gets the
+ * scale NaN and keeps it: rows that see the block get NaN, rows that do not see it are untouched.
+ * A page whose first slot is written by this call starts afresh: its old scale and bytes count for nothing.
+ * Rows with slot -1 are skipped and their outputs left as they were.  Rows of one page must be consecutive and ascending
+ * (they are, in tables built above), and one page must not be written by two overlapping calls.
+ *   q, k, v  device [max_rows][heads][head_dim] bf16, q may be NULL;  q_rot  out (may alias q), NULL exactly when q is;
+ *   k_rot    out, optional (NULL to skip; may alias k): rotated keys in bf16, what mv_dag_prefill_attn reads
+ * dtype MV_BF16, head_dim 64 or 128; all tensors 16-byte aligned.  Errors: MV_ERR_INVALID_ARG, MV_ERR_UNSUPPORTED, MV_ERR_CUDA. */
+mv_status mv_rope_write_kv_fp8_blk(const mv_step_tables* tables, const mv_attn_geom* geom, const void* q, const void* k, const void* v,
+                                   void* q_rot, void* k_rot, void* k_pages8, void* v_pages8, float* kv_scale, void* cuda_stream);
+
+/* Decode attention over that cache: for every row r of the tables and query head h
+ *   out[r][h] = sum_j softmax_j(sm_scale * <q_rot[r][h], K_j>) V_j
+ * over the tokens the entries of r's group give it (a row that no entry names gets zeros).  The step's new tokens must be
+ * in the cache first (mv_rope_write_kv_fp8_blk before this call in stream order).  A group's pages are read once per KV head, for all
+ * its rows and the whole GQA group.  Rows beyond the tables' count are left as they were.
+ *   q_rot, out  device [max_rows][n_q_heads][head_dim] bf16;  pools, kv_scale as above
+ *   workspace   device, 256-byte aligned, mv_decode_fp8_blk_workspace_bytes(geom) bytes (it does not depend on the step);
+ *               scratch, not to be shared by calls that may overlap on the device
+ * The same inputs give the same bits on every call.  dtype MV_BF16, head_dim 64 or 128, group size at most
+ * 64 and rows_per_group * group size <= 64; all tensors 16-byte aligned.  Errors: MV_ERR_INVALID_ARG, MV_ERR_UNSUPPORTED,
+ * MV_ERR_WORKSPACE, MV_ERR_CUDA. */
+size_t mv_decode_fp8_blk_workspace_bytes(const mv_attn_geom* geom);
+mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* tables, const mv_attn_geom* geom, const void* q_rot, const void* k_pages8,
+                                     const void* v_pages8, const float* kv_scale, void* out, void* workspace,
+                                     size_t workspace_bytes, void* cuda_stream);
+
 /* Decode attention for callers that cannot allocate device memory.  (The paper has no counterpart: this is
  * a packaging variant of mv_dag_decode_attn, same arithmetic, same kernels.)
  *

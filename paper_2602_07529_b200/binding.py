@@ -30,7 +30,9 @@ EXPORTS = ["mv_plan_dag", "mv_plan_bind_geometry", "mv_plan_table", "mv_plan_get
            "mv_dag_prefill_attn", "mv_dag_prefill_attn_bwd", "mv_decode_step_staging_bytes", "mv_decode_step_host", "mv_decode_step_host_batch", "mv_decode_step_pipelined_plan", "mv_decode_step_pipelined_staging_bytes",
            "mv_decode_step_host_pipelined", "mv_status_string",
            "mv_launch_count", "mv_plan_read_status", "mv_dag_decode_attn_static",
-           "mv_static_workspace_bytes", "mv_rope_write_kv_fp8", "mv_dag_decode_attn_fp8", "mv_selftest_bounded_wait", "mv_selftest_tmap_cache",
+           "mv_static_workspace_bytes", "mv_rope_write_kv_fp8", "mv_dag_decode_attn_fp8", "mv_step_tables_workspace_bytes",
+           "mv_step_tables_build", "mv_step_tables_read_status", "mv_rope_write_kv_fp8_blk", "mv_decode_fp8_blk_workspace_bytes",
+           "mv_dag_decode_attn_fp8_blk", "mv_selftest_bounded_wait", "mv_selftest_tmap_cache",
            "mv_sched_create", "mv_sched_destroy", "mv_sched_add_request", "mv_sched_step", "mv_sched_rows",
            "mv_sched_commit", "mv_sched_page_refs", "mv_sched_get_stats"]
 
@@ -70,6 +72,16 @@ class _SchedStats(C.Structure):
         "pages_in_use", "pages_peak")]
 
 
+class _StepTables(C.Structure):
+    _fields_ = [("max_rows", C.c_int32), ("max_groups", C.c_int32), ("max_entries", C.c_int32), ("rows_per_group", C.c_int32)] + [
+        (n, C.c_void_p) for n in ("pos_id", "slot", "group_row_off", "group_ent_off", "group_tile_off", "entries", "counts")]
+
+
+class _StepShape(C.Structure):
+    _fields_ = [("n_nodes", C.c_int32), ("n_parents", C.c_int32), ("n_pages", C.c_int32), ("max_req_nodes", C.c_int32),
+                ("num_pages", C.c_int64)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2602_07529_b200.build` "
@@ -94,6 +106,14 @@ def _load():
     lib.mv_dag_decode_attn_static.argtypes = [vp, C.POINTER(_Geom), vp, vp, vp, vp, vp]
     lib.mv_rope_write_kv_fp8.argtypes = [vp, C.POINTER(_Geom)] + [vp] * 8
     lib.mv_dag_decode_attn_fp8.argtypes = [vp, C.POINTER(_Geom), vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.mv_step_tables_workspace_bytes.argtypes = [i32]
+    lib.mv_step_tables_workspace_bytes.restype = sz
+    lib.mv_step_tables_build.argtypes = [vp, vp, vp, vp, sz, vp]
+    lib.mv_step_tables_read_status.argtypes = [vp, vp, C.POINTER(i32)]
+    lib.mv_rope_write_kv_fp8_blk.argtypes = [vp] * 11
+    lib.mv_decode_fp8_blk_workspace_bytes.argtypes = [C.POINTER(_Geom)]
+    lib.mv_decode_fp8_blk_workspace_bytes.restype = sz
+    lib.mv_dag_decode_attn_fp8_blk.argtypes = [vp] * 8 + [sz, vp]
     lib.mv_static_workspace_bytes.argtypes = []
     lib.mv_static_workspace_bytes.restype = sz
     lib.mv_decode_step_staging_bytes.argtypes = [vp, C.POINTER(_Geom)]
@@ -292,6 +312,126 @@ def mv_dag_decode_attn_fp8(plan: Plan, geom: _Geom, q_rot, k_pages8, v_pages8, k
     _check(lib.mv_dag_decode_attn_fp8(plan.handle, C.byref(geom), _ptr(q_rot), _ptr(k_pages8), _ptr(v_pages8), _ptr(kv_scale), _ptr(out),
                                       _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
            "mv_dag_decode_attn_fp8")
+
+
+# ---- decode steps planned on the device, over the block-scaled 8-bit cache
+
+def _arr(t, name: str, dtype: str, least: int, device):
+    """Device pointer of a contiguous CUDA tensor of the given dtype with at least ``least`` elements on ``device``."""
+    if t is None or not t.is_cuda or t.dtype is not _dtype(dtype) or t.numel() < least or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name}: a contiguous CUDA tensor of {dtype} with at least {least} elements on {device} is needed, got "
+                         + ("None" if t is None else f"{tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}"))
+    return t.data_ptr()
+
+
+_DTYPES: dict = {}
+
+
+def _dtype(name: str):
+    got = _DTYPES.get(name)
+    if got is None:
+        import torch
+        got = _DTYPES[name] = getattr(torch, name)
+    return got
+
+
+def _launch_stream(device, stream):
+    """The raw stream of a launch on ``device``, which has to be the current one (the library launches there)."""
+    import torch
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the arrays are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    return _stream_ptr(stream)
+
+
+class DeviceBatch:
+    """A batch description whose arrays are int32 CUDA tensors (kept alive here): what ``mv_step_tables_build`` takes.
+    The tensors' contents may change between builds; their sizes and addresses may not."""
+
+    def __init__(self, n_req, node_off, node_len, node_new, parent_off, parent_idx, page_off, page_idx, num_pages, max_req_nodes,
+                 vis_mode=0, pos_mode=0, page_size=16):
+        n_nodes = node_len.numel()
+        self.device = node_off.device
+        sizes = (("node_off", node_off, int(n_req) + 1), ("node_len", node_len, n_nodes), ("node_new", node_new, n_nodes),
+                 ("parent_off", parent_off, n_nodes + 1), ("parent_idx", parent_idx, 0), ("page_off", page_off, n_nodes + 1),
+                 ("page_idx", page_idx, 0))
+        ptrs = [_arr(t, name, "int32", least, self.device) for name, t, least in sizes]
+        self._keep = [t for _, t, _ in sizes]
+        self.n_req = int(n_req)
+        self.c_batch = _DagBatch(self.n_req, *ptrs, int(page_size), int(vis_mode), int(pos_mode))
+        self.c_shape = _StepShape(n_nodes, parent_idx.numel(), page_idx.numel(), int(max_req_nodes), int(num_pages))
+        self._ref = (C.byref(self.c_batch), C.byref(self.c_shape))
+
+
+class StepTables:
+    """The tables of a step: caller-owned CUDA tensors whose sizes are the capacities (see ``mv_step_tables`` in the header).
+    Without the group arrays only positions and slots are built."""
+
+    def __init__(self, pos_id, slot, counts, group_row_off=None, group_ent_off=None, group_tile_off=None, entries=None, rows_per_group=1):
+        self.device = counts.device
+        self.max_rows = pos_id.numel()
+        groups = 0 if group_row_off is None else group_row_off.numel() - 1
+        ents = 0 if entries is None else entries.numel() // 4
+        p = [_arr(pos_id, "pos_id", "int32", 0, self.device), _arr(slot, "slot", "int64", self.max_rows, self.device)]
+        if groups > 0:
+            p += [_arr(t, name, "int32", groups + 1, self.device) for name, t in (("group_row_off", group_row_off),
+                                                                                 ("group_ent_off", group_ent_off), ("group_tile_off", group_tile_off))]
+            p.append(_arr(entries, "entries", "int32", 4, self.device))
+        else:
+            p += [None] * 4
+            groups = ents = 0
+        p.append(_arr(counts, "counts", "int32", 8, self.device))
+        self._keep = (pos_id, slot, counts, group_row_off, group_ent_off, group_tile_off, entries)
+        self.c_tables = _StepTables(self.max_rows, groups, ents, int(rows_per_group), *p)
+        self._ref = C.byref(self.c_tables)
+
+
+def mv_step_tables_workspace_bytes(batch) -> int:
+    return int(lib.mv_step_tables_workspace_bytes(batch.n_req))
+
+
+def mv_step_tables_build(batch: DeviceBatch, tables: StepTables, workspace, stream=None):
+    """Positions, slots and block tables of a step from its batch on the device; the outcome is in ``counts`` (asynchronous)."""
+    s = _launch_stream(tables.device, stream)
+    ws = _arr(workspace, "workspace", "uint8", 0, tables.device)
+    if batch.device != tables.device:
+        raise ValueError(f"the batch is on {batch.device}, the tables on {tables.device}")
+    _check(lib.mv_step_tables_build(*batch._ref, tables._ref, ws, workspace.numel(), s), "mv_step_tables_build")
+
+
+def mv_step_tables_read_status(tables: StepTables, stream=None) -> int:
+    """Status word of the step (0 = fine); synchronises the stream."""
+    out = C.c_int32(-1)
+    _check(lib.mv_step_tables_read_status(tables._ref, _launch_stream(tables.device, stream), C.byref(out)), "mv_step_tables_read_status")
+    return int(out.value)
+
+
+def mv_rope_write_kv_fp8_blk(tables: StepTables, geom: _Geom, q, k, v, q_rot, k_rot, k_pages8, v_pages8, kv_scale, stream=None):
+    d, n = tables.device, tables.max_rows
+    s = _launch_stream(d, stream)
+    nq, nk = n * geom.n_q_heads * geom.head_dim, n * geom.n_kv_heads * geom.head_dim
+    block = geom.num_pages * geom.n_kv_heads
+    _check(lib.mv_rope_write_kv_fp8_blk(
+        tables._ref, C.byref(geom), None if q is None else _arr(q, "q", "bfloat16", nq, d), _arr(k, "k", "bfloat16", nk, d),
+        _arr(v, "v", "bfloat16", nk, d), None if q_rot is None else _arr(q_rot, "q_rot", "bfloat16", nq, d),
+        None if k_rot is None else _arr(k_rot, "k_rot", "bfloat16", nk, d), _arr(k_pages8, "k_pages8", "uint8", block * 16 * geom.head_dim, d),
+        _arr(v_pages8, "v_pages8", "uint8", block * 16 * geom.head_dim, d), _arr(kv_scale, "kv_scale", "float32", block * 2, d), s),
+        "mv_rope_write_kv_fp8_blk")
+
+
+def mv_decode_fp8_blk_workspace_bytes(geom: _Geom) -> int:
+    return int(lib.mv_decode_fp8_blk_workspace_bytes(C.byref(geom)))
+
+
+def mv_dag_decode_attn_fp8_blk(tables: StepTables, geom: _Geom, q_rot, k_pages8, v_pages8, kv_scale, out, workspace, stream=None):
+    d, n = tables.device, tables.max_rows
+    s = _launch_stream(d, stream)
+    nq, block = n * geom.n_q_heads * geom.head_dim, geom.num_pages * geom.n_kv_heads
+    _check(lib.mv_dag_decode_attn_fp8_blk(
+        tables._ref, C.byref(geom), _arr(q_rot, "q_rot", "bfloat16", nq, d), _arr(k_pages8, "k_pages8", "uint8", block * 16 * geom.head_dim, d),
+        _arr(v_pages8, "v_pages8", "uint8", block * 16 * geom.head_dim, d), _arr(kv_scale, "kv_scale", "float32", block * 2, d),
+        _arr(out, "out", "bfloat16", nq, d), _arr(workspace, "workspace", "uint8", 0, d), workspace.numel(), s), "mv_dag_decode_attn_fp8_blk")
 
 
 def mv_static_workspace_bytes() -> int:

@@ -10,9 +10,13 @@
 // HBM-bound elementwise kernel: one or four tokens per CTA, 16-byte vector loads and stores, the cos/sin
 // rows of the CTA's tokens are computed once into shared memory and reused by all heads.
 #include "common.cuh"
+#include "rope.cuh"
 #include "trace.h"
 
 namespace {
+
+using mv::rope_cos_sin;
+using mv::ThetaTable;
 
 template <typename T>
 struct Vec16;  // 16 bytes of T
@@ -58,33 +62,6 @@ __device__ __forceinline__ void store_e4m3(unsigned char* dst, const float (&x)[
     w[i] = mv::pack_e4m3x2(x[4 * i] * inv, x[4 * i + 1] * inv) | (mv::pack_e4m3x2(x[4 * i + 2] * inv, x[4 * i + 3] * inv) << 16);
   if (N == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[N / 4 - 1]);
   else *reinterpret_cast<uint32_t*>(dst) = w[0];
-}
-
-// theta_i = base^(-2i/d) for i < d/2, evaluated once per launch on the host in double precision
-struct ThetaTable {
-  double theta[64];
-};
-
-// cos and sin of pos * theta.  The angle and its reduction to [-pi/4, pi/4] (two-term Cody-Waite with a 53-bit and a
-// residual piece of pi/2; pos * theta stays below 2^25, so k * PIO2_HI is exact to well under 1e-12) are double
-// precision; the reduced angle is rounded to float and its cosine and sine come from the accurate float routine
-// (no fast-math intrinsics), so both agree with the double-precision values to within two units in the last place
-// of a float.  Six double-precision instructions per (token, i) instead of a double-precision sincos: with the
-// latter the arithmetic, not HBM, bounded the kernel at prefill sizes.
-__device__ __forceinline__ void rope_cos_sin(int pos, double theta, float& c, float& s) {
-  constexpr double TWO_OVER_PI = 0.63661977236758134308;
-  constexpr double PIO2_HI = 1.57079632679489655800e+00;  // pi/2 rounded to double
-  constexpr double PIO2_LO = 6.12323399573676603587e-17;  // pi/2 - PIO2_HI
-  const double a = double(pos) * theta;
-  const double kf = rint(a * TWO_OVER_PI);
-  double r = fma(-kf, PIO2_HI, a);
-  r = fma(-kf, PIO2_LO, r);
-  float sr, cr;
-  sincosf(float(r), &sr, &cr);
-  const int k = int(kf) & 3;  // quadrant: angle = r + k * pi/2
-  const float ss = (k & 1) ? cr : sr, cc = (k & 1) ? sr : cr;
-  s = (k & 2) ? -ss : ss;
-  c = ((k + 1) & 2) ? -cc : cc;
 }
 
 // TPC tokens per CTA.  Phase 1: the CTA's (token, i) pairs get their cos / sin, one pair per thread, while the first

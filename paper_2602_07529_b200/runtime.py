@@ -162,6 +162,80 @@ class DecodeStateFP8(DecodeState):
         return self.out
 
 
+class StepOnDevice:
+    """A step planned on the device: the batch's arrays as CUDA tensors, the tables built from them, and their workspace.
+    ``build()`` may be called (or replayed) again after the tensors in ``self.arrays`` have changed; the capacities are
+    those of the batch given here unless stated.  ``blocks=False``: positions and slots only."""
+
+    ARRAYS = ("node_off", "node_len", "node_new", "parent_off", "parent_idx", "page_off", "page_idx")
+
+    def __init__(self, batch, group: int, device="cuda", blocks: bool = True, max_rows: int | None = None,
+                 max_groups: int | None = None, max_entries: int | None = None):
+        i32 = lambda x: torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(device)
+        self.arrays = {n: i32(getattr(batch, n)) for n in self.ARRAYS}
+        per = max(1, 64 // group)
+        off, new = np.asarray(batch.node_off), np.asarray(batch.node_new)
+        rows = np.asarray([int(new[off[r]:off[r + 1]].sum()) for r in range(batch.n_req)], np.int64)
+        groups = (rows + per - 1) // per
+        if max_rows is None:
+            max_rows = int(rows.sum())
+        if max_groups is None:
+            max_groups = max(1, int(groups.sum()))
+        if max_entries is None:   # every page once per group, and at most one more entry for every new token
+            pages = np.asarray(batch.page_off)[off[1:]] - np.asarray(batch.page_off)[off[:-1]]
+            max_entries = int((pages * groups).sum() + rows.sum())
+        empty = lambda n, dt: torch.zeros(int(n), dtype=dt, device=device)
+        t = {"pos_id": empty(max_rows, torch.int32), "slot": empty(max_rows, torch.int64), "counts": empty(8, torch.int32)}
+        if blocks:
+            t.update({n: empty(max_groups + 1, torch.int32) for n in ("group_row_off", "group_ent_off", "group_tile_off")})
+            t["entries"] = empty(4 * max(1, max_entries), torch.int32).view(-1, 4)
+        self.t = t
+        self.batch = B.DeviceBatch(batch.n_req, **self.arrays, num_pages=batch.num_pages, vis_mode=batch.vis_mode,
+                                   max_req_nodes=max(1, int(np.diff(off).max()) if batch.n_req else 1), pos_mode=batch.pos_mode)
+        self.tables = B.StepTables(**t, rows_per_group=per)
+        self.workspace = _dev_bytes(B.mv_step_tables_workspace_bytes(self.batch), device)
+
+    def build(self, stream=None):
+        B.mv_step_tables_build(self.batch, self.tables, self.workspace, stream)
+        return self.tables
+
+    def read_status(self, stream=None) -> int:
+        return B.mv_step_tables_read_status(self.tables, stream)
+
+
+class DecodeStateFP8Blk(DecodeState):
+    """The same decode workload planned on the device, with the KV history in FP8 pools that carry a scale per (page, KV head)."""
+
+    def __init__(self, wl: synth.Workload, device="cuda"):
+        assert wl.kind == "decode" and wl.geom.dtype == "bf16"
+        self.wl, self.device = wl, device
+        g, b = wl.geom, wl.batch
+        self.local_geom = g
+        self.geom = B.make_geom(g.n_q_heads, g.n_kv_heads, g.head_dim, b.num_pages, g.dtype, g.page_size, 0.0, g.rope_base)
+        shape = (b.num_pages, g.n_kv_heads, g.page_size, g.head_dim)
+        self.k_pages, self.v_pages = (torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2))
+        self.kv_scale = torch.zeros(b.num_pages, g.n_kv_heads, 2, dtype=torch.float32, device=device)
+        hist = synth.DagBatch(b.n_req, b.node_off, np.zeros_like(b.node_len), b.node_len, b.parent_off, b.parent_idx,
+                              b.page_off, b.page_idx, b.page_size, b.num_pages, b.vis_mode, b.pos_mode)
+        _, kh, vh = _stack_values(wl, "history", device)
+        hs = StepOnDevice(hist, g.group, device, blocks=False)
+        B.mv_rope_write_kv_fp8_blk(hs.build(), self.geom, None, kh, vh, None, None, self.k_pages, self.v_pages, self.kv_scale)
+        torch.cuda.synchronize()
+        assert hs.read_status() == 0
+        del kh, vh, hs
+        self.q, self.k, self.v = _stack_values(wl, "new", device)
+        self.steps = StepOnDevice(b, g.group, device)
+        self.q_rot = torch.empty_like(self.q)
+        self.out = torch.empty_like(self.q)
+        self.workspace = _dev_bytes(B.mv_decode_fp8_blk_workspace_bytes(self.geom), device)
+
+    def step(self, stream=None):
+        t = self.steps.build(stream)
+        B.mv_rope_write_kv_fp8_blk(t, self.geom, self.q, self.k, self.v, self.q_rot, None, self.k_pages, self.v_pages, self.kv_scale, stream)
+        B.mv_dag_decode_attn_fp8_blk(t, self.geom, self.q_rot, self.k_pages, self.v_pages, self.kv_scale, self.out, self.workspace, stream)
+        return self.out
+
+
 class PrefillState:
     def __init__(self, wl: synth.Workload, device="cuda", with_pool: bool = True):
         assert wl.kind == "prefill"
