@@ -19,6 +19,10 @@
 #include "blk_stream.cuh"
 #include "trace.h"
 
+namespace mv {
+mv_status decode_blk_tc(const blk::Args& a, cudaStream_t st);
+}
+
 namespace {
 
 using bf16 = __nv_bfloat16;
@@ -157,12 +161,10 @@ __global__ void __launch_bounds__(NT) decode_blk_kernel(const Args a) {
         const int page = __shfl_sync(0xffffffffu, we.x, src);
         p.tokens = __shfl_sync(0xffffffffu, we.y, src);
         p.mask = (uint64_t(uint32_t(__shfl_sync(0xffffffffu, we.w, src))) << 32) | uint32_t(__shfl_sync(0xffffffffu, we.z, src));
-        p.ks = __shfl_sync(0xffffffffu, ws.x, src);
+        const int ek = mv::blk::scale_exponent(__shfl_sync(0xffffffffu, ws.x, src));
         p.ev = mv::blk::scale_exponent(__shfl_sync(0xffffffffu, ws.y, src));
-        if (p.ev == 128) {
-          p.ks = __uint_as_float(0x7fc00000u);
-          p.ev = 0;
-        }
+        p.ks = ek == 128 || p.ev == 128 ? __uint_as_float(0x7fc00000u) : mv::blk::exp2_int(ek);
+        if (p.ev == 128) p.ev = 0;
         if (page < 0) {
           p.tokens = 0;
           return;
@@ -477,6 +479,10 @@ extern "C" mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* t, const m
   a.G = G;
   a.scale_log2 = mv::softmax_scale(g) * 1.4426950408889634f;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  const bool ok = g->head_dim == 128 ? launch<128, 2>(a, s) : launch<64, 4>(a, s);
-  return ok ? MV_OK : MV_ERR_CUDA;
+  if (g->head_dim == 128) {
+    const mv_status e = mv::decode_blk_tc(a, s);
+    if (e != MV_OK) return e;
+    return launch_pdl(decode_blk_merge_kernel<128>, dim3(SHARES, 4), 128, 0, a, s) ? MV_OK : MV_ERR_CUDA;
+  }
+  return launch<64, 4>(a, s) ? MV_OK : MV_ERR_CUDA;
 }
