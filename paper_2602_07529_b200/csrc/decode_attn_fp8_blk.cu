@@ -32,6 +32,7 @@ using mv::blk::PS;
 using mv::blk::SHARES;
 
 constexpr int NT = 128, NW = NT / 32;
+constexpr int MERGE_Y = 8;  // CTAs that share the q-vectors of a cut stream
 
 __device__ __forceinline__ uint32_t half2_of_e4m3x2(uint32_t v) {
   uint32_t h;
@@ -77,22 +78,12 @@ __global__ void __launch_bounds__(NT) decode_blk_kernel(const Args a) {
   const int fr = lane >> 2, fc = lane & 3;  // fragment row / column of the lane
   mv::grid_dependency_wait();
   mv::grid_dependency_launch_dependents();
-  const mv::blk::Step st = mv::blk::step_of(a);
-  if (st.n_tiles == 0) return;
-  const int share = blockIdx.x;
-  int64_t x = mv::blk::share_begin(st.n_tiles, share);
-  const int64_t x_end = mv::blk::share_begin(st.n_tiles, share + 1);
-  if (x >= x_end) return;
-  int g = mv::blk::find_group(a.t.tile_off, st.n_groups, int(x / a.Hkv));
-  while (x < x_end) {
-    while (g + 1 < st.n_groups && int64_t(a.t.tile_off[g + 1]) * a.Hkv <= x) ++g;
-    if (a.t.tile_off[g + 1] <= a.t.tile_off[g]) return;  // offsets that do not count up: nothing sound to do
-    const mv::blk::Segment s = mv::blk::segment_at(a, st, share, x, x_end, g);
-    x += s.n_tiles;
-    if (!s.ok) {
-      if (tid == 0) atomicExch(a.t.counts + 4, int(MV_ERR_INVALID_ARG));
-      continue;
-    }
+  mv::blk::Walk walk;
+  walk.begin(a, blockIdx.x);
+  mv::blk::Segment s;
+  mv::blk::CutLog cuts;
+  while (walk.next(a, s, tid == 0)) {
+    cuts.add(a, s);
     // ---- q-vectors as half precision, scaled by a power of two to magnitudes below 2 (exact for what is within 2^-14 of the
     // largest element): a warp per q-vector
     __syncthreads();
@@ -349,67 +340,101 @@ __global__ void __launch_bounds__(NT) decode_blk_kernel(const Args a) {
       }
     }
   }
+  if (tid == 0) cuts.store(a, blockIdx.x);
 }
 
-// Merge of the cut streams: CTA (c, y) takes the stream whose first cut lies at the start of share c, if there is one, and
-// of its q-vectors y, y + gridDim.y, ...  out = sum_i w_i O_i / sum_i w_i l_i,  w_i = 2^(m_i - max m).  Bound by latency: a handful of
-// dependent loads, then each partial once.
+// Merge of the cut streams: CTA (c, y) takes the stream that starts in share c and ends in a later one, if there is one, and of
+// its q-vectors y, y + gridDim.y, ...  out = sum_i w_i O_i / sum_i w_i l_i,  w_i = 2^(m_i - max m).  Bound by latency, three
+// dependent round trips: the shares' records, the references, the parts, which the four warps deal out among themselves with eight loads
+// in flight each.
 template <int D>
 __global__ void __launch_bounds__(128) decode_blk_merge_kernel(const Args a) {
-  constexpr int LPV = D / 4;  // lanes per q-vector
+  constexpr int VEC = D / 32;  // elements of the head vector per lane
+  __shared__ float so[NW][D], ssum[NW];
   mv::grid_dependency_wait();
-  const mv::blk::Step st = mv::blk::step_of(a);
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = blockIdx.x;
+  const int4* const cuts = reinterpret_cast<const int4*>(a.cuts);
+  auto first_of = [&](int i) { return i < SHARES ? __ldcg(cuts + 2 * i) : make_int4(-1, 0, 0, 0); };
+  int4 r = first_of(c + 1 + lane);
+  const int4 own = __ldcg(cuts + 2 * c + 1);
+  if (own.x >= 0) {
+    // The shares behind that hold something of the stream (at most the last holds more than it: shares that hold nothing at all may lie between)
+    unsigned parts = 0;  // of the 32 shares behind c
+    int c1 = c;
+    for (int i0 = c + 1; i0 < SHARES; i0 += 32) {
+      if (i0 > c + 1) r = first_of(i0 + lane);
+      const unsigned all = __ballot_sync(0xffffffffu, r.x == own.x), last = __ballot_sync(0xffffffffu, r.x == own.x && r.w != 0);
+      if (i0 == c + 1) parts = all;
+      if (all) c1 = i0 + 31 - __clz(all);
+      if (last) break;
+    }
+    auto holds = [&](int i) {  // share i >= c
+      return i == c || (i - c <= 32 ? ((parts >> (i - c - 1)) & 1) != 0 : __ldcg(&a.cuts[2 * i].stream) == own.x);
+    };
+    const int head = own.x % a.Hkv;
+    for (int v = blockIdx.y; v < own.z; v += gridDim.y) {
+      // part i of the stream: slot 2 c + 1, then slots 2 i of the shares behind
+      float top = -INFINITY;
+      for (int i = c + lane; i <= c1; i += 32)
+        if (holds(i)) top = fmaxf(top, __ldcg(&a.part_ml[(2 * i + (i == c)) * MAXQV + v]).x);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      float acc[VEC] = {}, sum = 0.f;
+      for (int i0 = c + warp; i0 <= c1; i0 += NW * 8) {
+        float2 ml[8];
+        float y[8][VEC];
+        bool there[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int i = i0 + k * NW;
+          there[k] = i <= c1 && holds(i);
+          ml[k] = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) y[k][e] = 0.f;
+          if (there[k]) {
+            const int at = (2 * i + (i == c)) * MAXQV + v;
+            ml[k] = __ldcg(&a.part_ml[at]);
+            const float* src = a.part_o + int64_t(at) * D + lane * VEC;
+            if (VEC == 4) {
+              const float4 z = __ldcg(reinterpret_cast<const float4*>(src));
+              y[k][0] = z.x; y[k][1] = z.y; y[k][VEC - 2] = z.z; y[k][VEC - 1] = z.w;
+            } else {
+              const float2 z = __ldcg(reinterpret_cast<const float2*>(src));
+              y[k][0] = z.x; y[k][1] = z.y;
+            }
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (!there[k]) continue;
+          const float w = ml[k].x == -INFINITY ? 1.f : mv::fast_exp2(ml[k].x - top);  // nothing seen: zeros (or NaN)
+          sum = fmaf(w, ml[k].y, sum);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) acc[e] = fmaf(w, y[k][e], acc[e]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) so[warp][lane * VEC + e] = acc[e];
+      if (lane == 0) ssum[warp] = sum;
+      __syncthreads();
+      if (tid < D / 2) {
+        const float total = (ssum[0] + ssum[1]) + (ssum[2] + ssum[3]);
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        const float x0 = (so[0][2 * tid] + so[1][2 * tid]) + (so[2][2 * tid] + so[3][2 * tid]);
+        const float x1 = (so[0][2 * tid + 1] + so[1][2 * tid + 1]) + (so[2][2 * tid + 1] + so[3][2 * tid + 1]);
+        reinterpret_cast<uint32_t*>(a.out + (int64_t(own.y + v / a.G) * a.Hq + head * a.G + v % a.G) * D)[tid] = mv::pack_bf16(x0 * inv, x1 * inv);
+      }
+      __syncthreads();
+    }
+  }
   // groups that have rows but no entries see nothing: zeros
-  for (int g = blockIdx.x; g < st.n_groups; g += gridDim.x)
-    if (a.t.tile_off[g + 1] == a.t.tile_off[g]) {
+  const int n_groups = max(0, min(__ldcg(a.t.counts + 1), a.t.max_groups));
+  for (int g = c; g < n_groups; g += gridDim.x)
+    if (a.t.tile_off[g + 1] <= a.t.tile_off[g]) {
       const int r0 = max(0, a.t.row_off[g]), r1 = min(a.t.max_rows, a.t.row_off[g + 1]);
       for (int64_t i = int64_t(r0) * a.Hq * D / 8 + blockIdx.y * blockDim.x + tid; i < int64_t(r1) * a.Hq * D / 8; i += int64_t(gridDim.y) * blockDim.x)
         reinterpret_cast<uint4*>(a.out)[i] = make_uint4(0, 0, 0, 0);
     }
-  const int c = blockIdx.x;
-  if (st.n_tiles == 0 || c == 0) return;
-  const int64_t x = mv::blk::share_begin(st.n_tiles, c);
-  if (x >= st.n_tiles || x == mv::blk::share_begin(st.n_tiles, c + 1)) return;
-  const int g = mv::blk::find_group(a.t.tile_off, st.n_groups, int(x / a.Hkv));
-  const int t0 = a.t.tile_off[g], tiles = a.t.tile_off[g + 1] - t0;
-  if (tiles <= 0 || int64_t(t0) * a.Hkv > x) return;
-  const int64_t in_group = x - int64_t(t0) * a.Hkv;
-  const int head = int(in_group / tiles);
-  if (head >= a.Hkv) return;
-  const int64_t first = int64_t(t0) * a.Hkv + int64_t(head) * tiles;
-  if (x == first) return;  // the stream starts with this share
-  const int c0 = mv::blk::share_of(st.n_tiles, first), c1 = mv::blk::share_of(st.n_tiles, first + tiles - 1);
-  // the first cut only: no share that holds something lies between c0 and this one
-  if (mv::blk::share_begin(st.n_tiles, c0 + 1) != x) return;
-  const int r0 = a.t.row_off[g], r1 = a.t.row_off[g + 1];
-  if (r0 < 0 || r1 < r0 || r1 > a.t.max_rows || r1 - r0 > MAXQV / a.G) return;
-  const int n_qv = (r1 - r0) * a.G;
-  const int e0 = a.t.ent_off[g], e1 = a.t.ent_off[g + 1];
-  if (e0 < 0 || e1 > a.t.max_entries || e1 - e0 <= (tiles - 1) * mv::blk::TILE_ENTRIES) return;  // the shares left nothing
-  const int lane = tid % LPV;
-  const int per = blockDim.x / LPV;
-  for (int v = blockIdx.y * per + tid / LPV; v < n_qv; v += gridDim.y * per) {
-    float top = -INFINITY;
-    for (int i = c0; i <= c1; ++i)
-      if (i == c0 || mv::blk::share_begin(st.n_tiles, i) < mv::blk::share_begin(st.n_tiles, i + 1))
-        top = fmaxf(top, __ldcg(&a.part_ml[(2 * i + (i == c0)) * MAXQV + v]).x);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-#pragma unroll 4
-    for (int i = c0; i <= c1; ++i) {
-      if (i != c0 && mv::blk::share_begin(st.n_tiles, i) >= mv::blk::share_begin(st.n_tiles, i + 1)) continue;
-      const int at = (2 * i + (i == c0)) * MAXQV + v;
-      const float2 ml = __ldcg(&a.part_ml[at]);
-      const float w = ml.x == -INFINITY ? 1.f : mv::fast_exp2(ml.x - top);  // nothing seen: zeros (or NaN)
-      const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part_o + int64_t(at) * D) + lane);
-      acc.x = fmaf(w, y.x, acc.x); acc.y = fmaf(w, y.y, acc.y); acc.z = fmaf(w, y.z, acc.z); acc.w = fmaf(w, y.w, acc.w);
-      sum = fmaf(w, ml.y, sum);
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const uint2 pk = make_uint2(mv::pack_bf16(acc.x * inv, acc.y * inv), mv::pack_bf16(acc.z * inv, acc.w * inv));
-    *reinterpret_cast<uint2*>(a.out + (int64_t(r0 + v / a.G) * a.Hq + head * a.G + v % a.G) * D + lane * 4) = pk;
-  }
 }
 
 bool launch_pdl(void (*kernel)(const Args), dim3 grid, int threads, int smem, const Args& a, cudaStream_t st) {
@@ -435,7 +460,7 @@ bool launch(const Args& a, cudaStream_t st) {
   constexpr int smem = smem_bytes<D>();
   if (smem > 48 * 1024 && !mv::opt_in_smem(decode_blk_kernel<D, MT>, smem, opted)) return false;
   if (!launch_pdl(decode_blk_kernel<D, MT>, dim3(SHARES), NT, smem, a, st)) return false;
-  return launch_pdl(decode_blk_merge_kernel<D>, dim3(SHARES, 4), 128, 0, a, st);
+  return launch_pdl(decode_blk_merge_kernel<D>, dim3(SHARES, MERGE_Y), 128, 0, a, st);
 }
 
 }  // namespace
@@ -471,6 +496,7 @@ extern "C" mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* t, const m
   a.out = static_cast<bf16*>(out);
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + mv::blk::part_o_bytes(g->head_dim));
+  a.cuts = reinterpret_cast<mv::blk::Cut*>(static_cast<char*>(workspace) + mv::blk::part_o_bytes(g->head_dim) + mv::blk::part_ml_bytes());
   a.t = mv::blk::Tables{t->group_row_off, t->group_ent_off, t->group_tile_off, reinterpret_cast<const int4*>(t->entries), t->counts,
                         t->max_rows, t->max_groups, t->max_entries};
   a.num_pages = g->num_pages;
@@ -482,7 +508,7 @@ extern "C" mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* t, const m
   if (g->head_dim == 128) {
     const mv_status e = mv::decode_blk_tc(a, s);
     if (e != MV_OK) return e;
-    return launch_pdl(decode_blk_merge_kernel<128>, dim3(SHARES, 4), 128, 0, a, s) ? MV_OK : MV_ERR_CUDA;
+    return launch_pdl(decode_blk_merge_kernel<128>, dim3(SHARES, MERGE_Y), 128, 0, a, s) ? MV_OK : MV_ERR_CUDA;
   }
   return launch<64, 4>(a, s) ? MV_OK : MV_ERR_CUDA;
 }

@@ -16,12 +16,13 @@
 //   - The reference exponent of a q-vector moves only when a weight would pass the format's largest value (448): every
 //     thread looks at its own weights and one barrier votes, so the maximum over the tokens (a reduction across lanes) is taken only
 //     on a stream's first tile and in the rare tile that lifts it.
-// The softmax warps keep the sums of a token (one per q-vector) in tensor memory as well, and walk the columns sixteen at a time
-// in a loop that is not unrolled: four warps on four quarters of the SM share no instruction fetches, and with the columns unrolled
-// (per-thread arrays, a code path per number of columns) misses of the SM's instruction cache cost three cycles per instruction.
-// A CTA is four softmax warps, a producer warp (TMA) and an issuer warp (products); two CTAs per SM hide each other's
-// hand-overs.  K and V tiles (16 KB each) share a ring of five slots; the scores of tile t + 1 are computed into the other
-// of two score buffers while the weights of tile t are.
+// The softmax warps keep the sums of a token (one per q-vector) in tensor memory as well, and walk the columns eight at a time
+// in a loop that is not unrolled: with the columns unrolled (per-thread arrays, a code path per number of columns) misses of
+// the SM's instruction cache cost three cycles per instruction.
+// A CTA is two groups of four softmax warps (a token has one thread in each; the groups take alternate blocks of columns), a
+// producer warp each for K and V and an issuer warp for either product; two CTAs per SM hide each other's hand-overs.  K
+// and V tiles (16 KB each) have two slots apiece, scores and weights two buffers, so that the products of one tile overlap the weights
+// of the next.
 // Every wait is bounded; the softmax warps vote once per tile, and the vote carries a failed wait, so that they leave together.
 #include "blk_stream.cuh"
 #include "tmap_cache.h"
@@ -39,30 +40,41 @@ using mv::blk::TILE_ENTRIES;
 constexpr int D = 128;
 constexpr int TILE = 128;                 // tokens per tile
 constexpr int PIECE = TILE * D;           // 16 KB: K or V of a tile
-constexpr int RING = 5;
-constexpr int METAS = 3;                  // tiles whose descriptions are live: K of tile j waits for the second product of tile j - 3
-constexpr int OFF_P = RING * PIECE;       // weights: [128 tokens][128 bytes], 128-byte swizzle
-constexpr int OFF_Q = OFF_P + PIECE;      // Q values [64][128], then Q remainders
+constexpr int RING = 4;                   // K in slots 0 and 2, V in slots 1 and 3
+constexpr int METAS = 4;                  // descriptions that may be live: K of tile j waits for the scores of tile j - 2, which wait for the weights of tile j - 4
+constexpr int OFF_P = RING * PIECE;       // weights of two tiles: [128 tokens][128 bytes] each, 128-byte swizzle
+constexpr int OFF_Q = OFF_P + 2 * PIECE;  // Q values [64][128], then Q remainders
 constexpr int Q_BYTES = MAXQV * D;
 constexpr int OFF_META = OFF_Q + 2 * Q_BYTES;
-constexpr int NT = 192;
+constexpr int GROUPS = 1;                // groups of four softmax warps, each with every other block of eight columns
+constexpr int SOFTMAX = GROUPS * 128;
+constexpr int NT = SOFTMAX + 128;        // and four warps: K, V, first products, second products
 constexpr float TOP = 448.f;              // largest 8-bit float
 constexpr float HEADROOM = 5.f;           // a reference that moves puts the largest weight at 2^5
 constexpr float LO_SCALE = 16.f;
 
-struct Entry {       // one page of a tile, as the softmax threads need it
+template <int N>
+struct Width {
+  static constexpr int value = N;
+};
+
+struct alignas(16) Entry {  // one page of a tile, as the softmax threads need it
   uint32_t see_lo, see_hi;  // q-vectors that see it
-  uint32_t rest;            // tokens | (exponent of V's scale + 127) << 8 | (exponent of K's scale + 127) << 16; K's is 255 (NaN) if either scale is NaN
+  float ks;                 // K's scale; NaN if either scale is
+  uint32_t vs;              // V's scale, a power of two, with the tokens in the mantissa's low byte; bit 8: sixteen tokens that every q-vector sees
 };
 struct Meta {
-  float factor[MAXQV];      // of a score
-  float minus_ref[MAXQV];   // minus the reference (+infinity: none yet; -infinity: no such q-vector)
+  alignas(16) float minus_ref[MAXQV];  // minus the reference of a q-vector (+infinity: none yet; -infinity: no such q-vector); read four at a time
+  float factor;                        // of a score
+  uint32_t largest;                    // magnitude among the segment's finite q-vectors (bf16 bits)
   Entry entry[METAS][TILE_ENTRIES];
-  uint64_t full[RING], empty[RING], described[METAS], s_full[2], q_full, p_full, pv_done, drained;
+  uint2 seen[METAS];                   // q-vectors that see some page of the tile
+  uint64_t full[RING], empty[RING], described[METAS], s_full[2], q_full, p_full[2], pv_done[2], drained[2];
   int abort;
   uint32_t tmem;
 };
 static_assert(sizeof(Meta) <= 1024, "meta area");
+static_assert(offsetof(Meta, minus_ref) % 16 == 0, "vector loads");
 constexpr int SMEM = OFF_META + 1024;
 static_assert(2 * (SMEM + 1024) <= 228 * 1024, "two CTAs per SM");
 
@@ -93,162 +105,149 @@ __device__ __forceinline__ bool wait_or_flag(const Cta& c, uint32_t b, uint32_t 
 __device__ __forceinline__ bool warp_wait(const Cta& c, uint32_t b, uint32_t parity) {
   return __all_sync(0xffffffffu, wait_or_flag(c, b, parity));
 }
-// Barriers of the four softmax warps that carry a predicate.
+// Barriers of the softmax warps that carry a predicate.
 __device__ __forceinline__ bool vote_any(bool p) {
   uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(uint32_t(p)) : "memory");
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(uint32_t(p)), "n"(SOFTMAX) : "memory");
   return r != 0;
 }
 __device__ __forceinline__ bool vote_all(bool p) {
   uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(uint32_t(p)) : "memory");
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 2, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(uint32_t(p)), "n"(SOFTMAX) : "memory");
   return r != 0;
 }
 
-// two floats -> two 8-bit floats each: value, and 16 times the remainder (bytes 0 and 1 of the results)
-__device__ __forceinline__ void split_e4m3x2(float x, float y, uint32_t& hi, uint32_t& lo) {
-  const __half2 h = __floats2half2_rn(x, y);
-  const uint32_t hb = *reinterpret_cast<const uint32_t*>(&h);
-  uint16_t w, v;
-  uint32_t back;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;\n" : "=h"(w) : "r"(hb));
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(back) : "h"(w));
-  const __half2 r = __hmul2(__hsub2(h, *reinterpret_cast<const __half2*>(&back)), __float2half2_rn(LO_SCALE));
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;\n" : "=h"(v) : "r"(*reinterpret_cast<const uint32_t*>(&r)));
-  hi = w;
-  lo = v;
+// four floats -> four 8-bit floats each: values, and 16 times the remainders.  The values are unpacked from the packed word: with
+// the 16-bit halves unpacked first and packed afterwards, the code that ptxas 12.9 makes unpacks zeros.
+__device__ __forceinline__ void split_e4m3x4(float x0, float x1, float x2, float x3, uint32_t& hi, uint32_t& lo) {
+  asm("{\n\t.reg .b16 a, b, c, d, e, f;\n\t.reg .b32 h0, h1, r0, r1, k;\n\t"
+      "cvt.rn.f16x2.f32 h0, %3, %2;\n\tcvt.rn.f16x2.f32 h1, %5, %4;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 a, h0;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, h1;\n\t"
+      "mov.b32 %0, {a, b};\n\tmov.b32 {e, f}, %0;\n\t"
+      "cvt.rn.f16x2.e4m3x2 r0, e;\n\tcvt.rn.f16x2.e4m3x2 r1, f;\n\t"
+      "mov.b32 k, 0x4c004c00;\n\t"
+      "sub.f16x2 r0, h0, r0;\n\tsub.f16x2 r1, h1, r1;\n\tmul.f16x2 r0, r0, k;\n\tmul.f16x2 r1, r1, k;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 c, r0;\n\tcvt.rn.satfinite.e4m3x2.f16x2 d, r1;\n\t"
+      "mov.b32 %1, {c, d};\n\t}"
+      : "=&r"(hi), "=r"(lo)
+      : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
 }
+static_assert(LO_SCALE == 16.f, "0x4c00 is 16 in half precision");
 
-// The share's segments, walked in the same way by both roles.
-struct Walk {
-  mv::blk::Step st;
-  int64_t x, x_end;
-  int share, g;
-  __device__ __forceinline__ void begin(const Args& a, int c) {
-    st = mv::blk::step_of(a);
-    share = c;
-    x = st.n_tiles > 0 ? mv::blk::share_begin(st.n_tiles, c) : 0;
-    x_end = st.n_tiles > 0 ? mv::blk::share_begin(st.n_tiles, c + 1) : 0;
-    g = x < x_end ? mv::blk::find_group(a.t.tile_off, st.n_groups, int(x / a.Hkv)) : 0;
-  }
-  // the next sound segment; false at the end of the share
-  __device__ __forceinline__ bool next(const Args& a, mv::blk::Segment& s, bool report) {
-    while (x < x_end) {
-      while (g + 1 < st.n_groups && int64_t(a.t.tile_off[g + 1]) * a.Hkv <= x) ++g;
-      if (a.t.tile_off[g + 1] <= a.t.tile_off[g]) return false;  // offsets that do not count up
-      s = mv::blk::segment_at(a, st, share, x, x_end, g);
-      x += s.n_tiles;
-      if (s.ok) return true;
-      if (report) atomicExch(a.t.counts + 4, int(MV_ERR_INVALID_ARG));
-    }
-    return false;
-  }
-};
-
-// ---- producer warp ---------------------------------------------------------------------------------------
-__device__ __forceinline__ void producer(const Cta& c, const CUtensorMap* tm_k, const CUtensorMap* tm_v) {
+// ---- producer warps: one for K and the tiles' descriptions, one for V ---------------------------------------
+// Eight boxes of 2 KB make a piece; one lane sends them all, with the rows in uniform registers.  Sending a box occupies its
+// warp for about 75 cycles: a warp that sent K and V of a tile could not keep up with the stream.
+template <bool IS_K>
+__device__ __forceinline__ void producer(const Cta& c, const CUtensorMap* map) {
   const Args& a = *c.a;
   Meta* const meta = c.meta;
   const int lane = threadIdx.x & 31;
+  const bool lead = mv::um::elect_one();
   const uint64_t policy = mv::l2_policy_evict_first();  // the cache is read once per call
-  Walk w;
+  mv::blk::Walk w;
   w.begin(a, blockIdx.x);
-  mv::blk::Segment s;
-  int piece = 0, tile = 0;
+  mv::blk::Segment s{};
+  int tile = 0;
   bool ok = true;
-  while (ok && w.next(a, s, lane == 0)) {
-    const uint64_t live = s.n_qv >= 64 ? ~0ull : (1ull << s.n_qv) - 1;
-    const uint64_t one_row = a.G >= 64 ? ~0ull : (1ull << a.G) - 1;
-    const int rows = s.n_qv / a.G;
-    // a window of 32 entries, one per lane: entries a window ahead of their scales, scales a window ahead of their use
-    auto entry_at = [&](int i0) {
-      int4 e = make_int4(-1, 0, 0, 0);
-      if (i0 + lane < s.n_ent) {
-        e = __ldcg(a.t.entries + s.ent0 + i0 + lane);
-        if (e.x < 0 || e.x >= a.num_pages || e.y < 1 || e.y > PS) {
-          atomicExch(a.t.counts + 4, int(MV_ERR_INVALID_ARG));
-          e = make_int4(-1, 0, 0, 0);
-        }
+  // a window of 32 entries, one per lane
+  auto entry_at = [&](int i0) {
+    int4 e = make_int4(-1, 0, 0, 0);
+    if (i0 + lane < s.n_ent) {
+      e = __ldcg(a.t.entries + s.ent0 + i0 + lane);
+      if (e.x < 0 || e.x >= a.num_pages || e.y < 1 || e.y > PS) {
+        atomicExch(a.t.counts + 4, int(MV_ERR_INVALID_ARG));
+        e = make_int4(-1, 0, 0, 0);
       }
-      return e;
-    };
-    auto scale_at = [&](const int4& e) {
-      return e.x >= 0 ? __ldcg(reinterpret_cast<const float2*>(a.scale) + int64_t(e.x) * a.Hkv + s.head) : make_float2(0.f, 1.f);
+    }
+    return e;
+  };
+  auto scale_at = [&](const int4& e) {
+    return e.x >= 0 ? __ldcg(reinterpret_cast<const float2*>(a.scale) + int64_t(e.x) * a.Hkv + s.head) : make_float2(0.f, 1.f);
+  };
+  while (ok && w.next(a, s, IS_K && lane == 0)) {
+    // what the softmax threads need of an entry
+    auto describe = [&](const int4& e, const float2& sc) {
+      Entry d{0, 0, 0.f, 127u << 23};
+      if (e.x >= 0) {
+        const int rows = s.n_qv / a.G;
+        const uint64_t all_rows = rows >= 64 ? ~0ull : (1ull << rows) - 1;
+        const uint64_t mask = ((uint64_t(uint32_t(e.w)) << 32) | uint32_t(e.z)) & all_rows;
+        uint64_t see = 0;
+        if (mask == all_rows) {
+          see = s.n_qv >= 64 ? ~0ull : (1ull << s.n_qv) - 1;
+        } else {
+          const uint64_t one_row = a.G >= 64 ? ~0ull : (1ull << a.G) - 1;
+#pragma unroll 1
+          for (int r = 0; r < rows; ++r)
+            if ((mask >> r) & 1) see |= one_row << (r * a.G);
+        }
+        const uint32_t ek = uint32_t(mv::blk::scale_exponent(sc.x) + 127), ev = uint32_t(mv::blk::scale_exponent(sc.y) + 127);
+        d.see_lo = uint32_t(see);
+        d.see_hi = uint32_t(see >> 32);
+        d.ks = ek == 255 || ev == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float(ek << 23);
+        d.vs = (ev == 255 ? 127u : ev) << 23 | (mask == all_rows && e.y == PS ? 256u : 0u) | uint32_t(e.y);
+      }
+      return d;
     };
     int4 e0 = entry_at(0), e1 = entry_at(32);
-    float2 s0 = scale_at(e0), s1 = make_float2(0.f, 1.f);
-    for (int t = 0; t < s.n_tiles && ok; ++t, ++tile) {
+    float2 s0 = make_float2(0.f, 1.f);
+    if (IS_K) s0 = scale_at(e0);
+    Entry d0;
+#pragma unroll 1
+    for (int t = 0; t < s.n_tiles; ++t, ++tile) {
       const int at = (t * TILE_ENTRIES) & 31;
       if (at == 0 && t > 0) {
         e0 = e1;
-        s0 = s1;
         e1 = entry_at(t * TILE_ENTRIES + 32);
       }
-      if (at == 16) s1 = scale_at(e1);
-      const int page = __shfl_sync(0xffffffffu, e0.x, at + (lane & 7));
-      const unsigned present = __ballot_sync(0xffffffffu, lane < 8 && page >= 0);
-      const uint32_t bytes = uint32_t(__popc(present)) * (PS * D);
-      const int row = (page * a.Hkv + s.head) * PS;
+      const unsigned present = (__ballot_sync(0xffffffffu, e0.x >= 0) >> at) & 0xffu;
+      const int my_row = (e0.x * a.Hkv + s.head) * PS;
+      const int piece = 2 * tile + (IS_K ? 0 : 1), slot = piece % RING;
+      ok = warp_wait(c, bar(&meta->empty[slot]), ((piece / RING) & 1) ^ 1);
+      if (!ok) break;
+      const uint32_t fb = bar(&meta->full[slot]), dst = c.base + slot * PIECE;
+      if (lead) mv::mbar_arrive_expect_tx(fb, uint32_t(__popc(present)) * (PS * D));
 #pragma unroll
-      for (int kv = 0; kv < 2; ++kv, ++piece) {
-        const int slot = piece % RING;
-        int go = 1;
-        if (lane == 0) go = wait_or_flag(c, bar(&meta->empty[slot]), ((piece / RING) & 1) ^ 1) ? 1 : 0;
-        ok = __shfl_sync(0xffffffffu, go, 0) != 0;
-        if (!ok) break;
-        if (kv == 0) {
-          if (lane >= at && lane < at + TILE_ENTRIES) {
-            Entry d;
-            d.see_lo = d.see_hi = 0;
-            d.rest = 127 << 8 | 127 << 16;
-            if (e0.x >= 0) {
-              const uint64_t mask = (uint64_t(uint32_t(e0.w)) << 32) | uint32_t(e0.z);
-              uint64_t see = 0;
-              if ((mask & ((rows >= 64 ? 0ull : (1ull << rows)) - 1)) == (rows >= 64 ? ~0ull : (1ull << rows) - 1)) see = live;
-              else
-                for (int r = 0; r < rows; ++r)
-                  if ((mask >> r) & 1) see |= one_row << (r * a.G);
-              uint32_t ek = uint32_t(mv::blk::scale_exponent(s0.x) + 127), ev = uint32_t(mv::blk::scale_exponent(s0.y) + 127);
-              if (ev == 255) {
-                ek = 255;
-                ev = 127;
-              }
-              d.see_lo = uint32_t(see);
-              d.see_hi = uint32_t(see >> 32);
-              d.rest = uint32_t(e0.y) | ev << 8 | ek << 16;
-            }
-            meta->entry[tile % METAS][lane - at] = d;
-          }
-          __syncwarp();
-          if (lane == 0) mv::mbar_arrive(bar(&meta->described[tile % METAS]));
-        }
-        const uint32_t fb = bar(&meta->full[slot]);
-        if (lane == 0) mv::mbar_arrive_expect_tx(fb, bytes);
+      for (int j = 0; j < TILE_ENTRIES; ++j) {
+        const int row = __shfl_sync(0xffffffffu, my_row, at + j);
+        if (lead && ((present >> j) & 1)) mv::tma_load_2d_hint(dst + j * (PS * D), map, 0, row, fb, policy);
+      }
+      __syncwarp();
+      if (IS_K) {
+        if (at == 0) d0 = describe(e0, s0);
+        const bool mine = lane >= at && lane < at + TILE_ENTRIES;
+        const uint32_t any_lo = __reduce_or_sync(0xffffffffu, mine ? d0.see_lo : 0), any_hi = __reduce_or_sync(0xffffffffu, mine ? d0.see_hi : 0);
+        if (mine) meta->entry[tile % METAS][lane - at] = d0;
+        if (lane == 0) meta->seen[tile % METAS] = make_uint2(any_lo, any_hi);
         __syncwarp();
-        if (lane < 8 && page >= 0)
-          mv::tma_load_2d_hint(c.base + slot * PIECE + lane * (PS * D), kv ? tm_v : tm_k, 0, row, fb, policy);
+        if (lane == 0) mv::mbar_arrive(bar(&meta->described[tile % METAS]));
+        if (at == 16) s0 = scale_at(e1);  // of the next window
       }
     }
   }
   if (!ok) {
-    // what is in flight must land before the CTA may leave
+    // what is in flight must land before the CTA may leave: this warp's last two fills
     if (lane == 0)
-      for (int k = 1; k <= min(piece, RING); ++k)
-        (void)mv::mbar_wait_bounded(bar(&meta->full[(piece - k) % RING]), ((piece - k) / RING) & 1, 20000000ull);
+      for (int k = max(0, tile - 2); k < tile; ++k) {
+        const int piece = 2 * k + (IS_K ? 0 : 1);
+        (void)mv::mbar_wait_bounded(bar(&meta->full[piece % RING]), (piece / RING) & 1, 20000000ull);
+      }
     __syncwarp();
   }
 }
 
 // ---- softmax warps ---------------------------------------------------------------------------------------
 // q-vectors of the segment to the two K-major tiles (128-byte rows, 16-byte pieces XOR-swizzled with row % 8), eight threads per
-// q-vector; factors and references of the segment
+// q-vector; factor and references of the segment.  One power of two scales them all: what it costs a small q-vector in
+// relative precision is, in its scores, no more than the largest one's rounding.
 __device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s, int cols) {
   const Args& a = *c.a;
   const int tid = threadIdx.x, x0 = tid >> 3, ch = tid & 7;
-  uint4 raw[4][2];
+  constexpr int ROWS = SOFTMAX / 8, STEPS = MAXQV / ROWS;  // q-vectors at a time
+  uint4 raw[STEPS][2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int x = i * 16 + x0;
+  for (int i = 0; i < STEPS; ++i) {
+    const int x = i * ROWS + x0;
     raw[i][0] = raw[i][1] = make_uint4(0, 0, 0, 0);
     if (x < s.n_qv) {
       const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t(s.row0 + x / a.G) * a.Hq + s.head * a.G + x % a.G) * D + ch * 16);
@@ -256,20 +255,35 @@ __device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s,
       raw[i][1] = __ldcg(src + 1);
     }
   }
+  if (tid == 0) c.meta->largest = 0;
+  if (tid < cols) c.meta->minus_ref[tid] = tid < s.n_qv ? INFINITY : -INFINITY;
+  (void)vote_all(true);
+  bool finite[STEPS];
+  uint32_t most = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int x = i * 16 + x0;
-    if (i * 16 >= cols) break;
+  for (int i = 0; i < STEPS; ++i) {
+    const uint4 x = raw[i][0], y = raw[i][1];
+    uint32_t m = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+    m = __vmaxu2(m, __vmaxu2(__vmaxu2(y.x & 0x7fff7fffu, y.y & 0x7fff7fffu), __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu)));
+    m = max(m & 0xffffu, m >> 16);
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    finite[i] = m < 0x7f80u;
+    if (finite[i]) most = max(most, m);
+  }
+  most = __reduce_max_sync(0xffffffffu, most);
+  if ((tid & 31) == 0) atomicMax(&c.meta->largest, most);
+  (void)vote_all(true);
+  // largest element into [128, 256)
+  const int e = max(-120, max(int(c.meta->largest >> 7), 1) - 127 - 7);
+  const float inv = mv::blk::exp2_int(-e);
+  if (tid == 0) c.meta->factor = mv::blk::exp2_int(e) * a.scale_log2;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const int x = i * ROWS + x0;
+    if (x >= cols) break;
     const uint32_t w[8] = {raw[i][0].x, raw[i][0].y, raw[i][0].z, raw[i][0].w, raw[i][1].x, raw[i][1].y, raw[i][1].z, raw[i][1].w};
-    uint32_t most = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) most = __vmaxu2(most, w[k] & 0x7fff7fffu);
-    uint32_t amax = max(most & 0xffffu, most >> 16);
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    // largest element into [128, 256)
-    const int e = max(int(amax >> 7), 1) - 127 - 7;
-    const float inv = amax < 0x7f80u ? mv::blk::exp2_int(-e) : __uint_as_float(0x7fc00000u);  // not finite: NaN
+    const float scale = finite[i] ? inv : __uint_as_float(0x7fc00000u);  // a q-vector that is not finite: NaN
     uint32_t hi[4], lo[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -277,7 +291,7 @@ __device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s,
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const uint32_t v = w[2 * k + j];
-        const float p = __uint_as_float(v << 16) * inv, q = __uint_as_float(v & 0xffff0000u) * inv;
+        const float p = __uint_as_float(v << 16) * scale, q = __uint_as_float(v & 0xffff0000u) * scale;
         h2[j] = mv::pack_e4m3x2(p, q);
         const float2 back = mv::unpack_e4m3x2(h2[j]);
         l2[j] = mv::pack_e4m3x2(p - back.x, q - back.y);
@@ -288,10 +302,6 @@ __device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s,
     unsigned char* dst = c.smem + OFF_Q + x * 128 + ((ch ^ (x & 7)) << 4);
     *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
     *reinterpret_cast<uint4*>(dst + Q_BYTES) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-    if (ch == 0) {
-      c.meta->factor[x] = x < s.n_qv ? mv::blk::exp2_int(max(-126, min(e, 126))) * a.scale_log2 : 0.f;
-      c.meta->minus_ref[x] = x < s.n_qv ? INFINITY : -INFINITY;
-    }
   }
 }
 
@@ -306,140 +316,168 @@ struct Columns {
 __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment& s, int& tile) {
   const Args& a = *c.a;
   Meta* const meta = c.meta;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int nb = (s.n_qv + 15) / 16, cols = nb * 16;
+  const int tid = threadIdx.x, token = tid & 127, group = tid >> 7, quarter = (tid >> 5) & 3, lane = tid & 31;
+  const int nb = (s.n_qv + 15) / 16, cols = nb * 16, n8 = cols / 8;
+  // The groups of warps take alternate blocks of sixteen columns; where their number is odd they share the last one.  own(f) calls f for
+  // every eight columns of this group.
+  auto own = [&](auto f) {
+#pragma unroll 1
+    for (int u = group; u < nb; u += GROUPS) {
+      f(2 * u);
+      if (GROUPS == 1 || u + 1 < nb || (nb & 1) == 0) f(2 * u + 1);
+    }
+    if (group == 1 && (nb & 1)) f(2 * nb - 1);
+  };
   const Columns at(cols);
-  const uint32_t lanes = meta->tmem + (uint32_t(warp * 32) << 16);  // this warp's lanes
-  float* const xch = reinterpret_cast<float*>(c.smem + OFF_P);       // exchange area: the weight tile while no product reads it
-  const uint64_t live = s.n_qv >= 64 ? ~0ull : (1ull << s.n_qv) - 1;
-  unsigned char* const p_row = c.smem + OFF_P + tid * 128;
-  const int sw = tid & 7;
+  const uint32_t lanes = meta->tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
+  float* const xch = reinterpret_cast<float*>(c.smem + OFF_P);          // exchange area: the weight tiles while no product reads them
+  const int sw = token & 7;
   bool ok = true;
+  uint64_t referenced = 0;  // q-vectors that have a reference (or saw scores that were not numbers)
 #pragma unroll 1
   for (int t = 0; t < s.n_tiles; ++t, ++tile) {
-    ok = ok && warp_wait(c, bar(&meta->described[tile % METAS]), (tile / METAS) & 1);
-    const Entry en = meta->entry[tile % METAS][tid >> 4];
-    const int tokens = en.rest & 0xff, ev = int((en.rest >> 8) & 0xff) - 127;
-    const float ks = (en.rest >> 16) == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((en.rest >> 16) << 23);
-    const bool valid = (tid & 15) < tokens;
-    const uint64_t see = valid ? (uint64_t(en.see_hi) << 32) | en.see_lo : 0;
-    const float evf = float(ev);
-    const uint64_t ks2 = mv::pack_f32x2(ks, ks), ev2 = mv::pack_f32x2(evf, evf);
-    const bool plain = __all_sync(0xffffffffu, see == live);
-    const uint32_t s_t = lanes + ((tile & 1) ? at.s1 : 0);
-    ok = ok && warp_wait(c, bar(&meta->s_full[tile & 1]), (tile >> 1) & 1);
-    if (tile > 0) ok = ok && warp_wait(c, bar(&meta->pv_done), (tile - 1) & 1);  // the weight tile is free
+    // the tile's description and scores, and a weight tile that no product reads any more
+    const bool arrived = ok && wait_or_flag(c, bar(&meta->described[tile % METAS]), (tile / METAS) & 1) &&
+                         wait_or_flag(c, bar(&meta->s_full[tile & 1]), (tile >> 1) & 1) &&
+                         (tile < 2 || wait_or_flag(c, bar(&meta->pv_done[tile & 1]), ((tile - 2) >> 1) & 1));
+    ok = __all_sync(0xffffffffu, arrived);
     mv::um::fence_after();
+    const Entry en = meta->entry[tile % METAS][token >> 4];
+    const bool plain = __all_sync(0xffffffffu, en.vs & 256u);
+    const uint32_t vs_bits = en.vs & 0x7f800000u;
+    const float evf = float(int(vs_bits >> 23) - 127), vinv = __uint_as_float((254u << 23) - vs_bits);  // exponent; 2^-exponent
+    const float fk = meta->factor * en.ks;
+    const uint64_t fk2 = mv::pack_f32x2(fk, fk), ev2 = mv::pack_f32x2(evf, evf);
+    const uint32_t s_t = lanes + ((tile & 1) ? at.s1 : 0);
+    unsigned char* const p_row = c.smem + OFF_P + (tile & 1) * PIECE + token * 128;
+    bool valid = true;
+    uint64_t see = ~0ull;
+    if (!plain) {
+      valid = (token & 15) < int(en.vs & 255u);
+      see = valid ? (uint64_t(en.see_hi) << 32) | en.see_lo : 0;
+    }
     // Weights of the thread's token against the references as they stand, into the weight tile (row = token; values, then
     // remainders) and, times `sign` 2^(-e), into the token's sums.  Returns the largest weight.
     auto pass = [&](float sign, bool first) {
       float top = 0.f;
-      const float vinv = sign * mv::blk::exp2_int(-ev);
-      const uint64_t vinv2 = mv::pack_f32x2(vinv, vinv);
-#pragma unroll 1
-      for (int b = 0; b < nb; ++b) {
-        uint32_t sc[16], l[16];
-        mv::um::ld16(s_t + b * 16, sc);
-        mv::um::ld16(lanes + at.sums + b * 16, l);
+      const uint64_t vinv2 = mv::pack_f32x2(sign * vinv, sign * vinv);
+      mv::um::wait_st();  // the sums as the last pass left them
+      auto columns = [&](auto width, int col) {
+        constexpr int W = decltype(width)::value;
+        uint32_t sc[W];
+        if constexpr (W == 16) mv::um::ld16(s_t + col, sc);
+        else mv::um::ld8(s_t + col, sc);
+        const float4* const mr = reinterpret_cast<const float4*>(meta->minus_ref + col);
+        float p[W];
         mv::um::wait_ld();
-        float p[16];
-        const float4* const fa = reinterpret_cast<const float4*>(meta->factor + b * 16);
-        const float4* const mr = reinterpret_cast<const float4*>(meta->minus_ref + b * 16);
 #pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-          const float4 f = fa[j / 4], m = mr[j / 4];
-          mv::unpack_f32x2(mv::fma_f32x2(mv::pack_u32x2(sc[j], sc[j + 1]), mv::mul_f32x2(mv::pack_f32x2(f.x, f.y), ks2), mv::add_f32x2(mv::pack_f32x2(m.x, m.y), ev2)), p[j], p[j + 1]);
-          mv::unpack_f32x2(mv::fma_f32x2(mv::pack_u32x2(sc[j + 2], sc[j + 3]), mv::mul_f32x2(mv::pack_f32x2(f.z, f.w), ks2), mv::add_f32x2(mv::pack_f32x2(m.z, m.w), ev2)), p[j + 2], p[j + 3]);
+        for (int j = 0; j < W; j += 4) {
+          const float4 y = mr[j / 4];
+          mv::unpack_f32x2(mv::fma_f32x2(mv::pack_u32x2(sc[j], sc[j + 1]), fk2, mv::add_f32x2(mv::pack_f32x2(y.x, y.y), ev2)), p[j], p[j + 1]);
+          mv::unpack_f32x2(mv::fma_f32x2(mv::pack_u32x2(sc[j + 2], sc[j + 3]), fk2, mv::add_f32x2(mv::pack_f32x2(y.z, y.w), ev2)), p[j + 2], p[j + 3]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) p[j + i] = mv::fast_exp2(p[j + i]);
         }
         if (!plain) {
-          const uint32_t mine = uint32_t(see >> (b * 16));
+          const uint32_t mine = uint32_t(see >> col);
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
+          for (int j = 0; j < W; ++j)
             if (!((mine >> j) & 1)) p[j] = 0.f;
         }
         float most = 0.f;
 #pragma unroll
-        for (int j = 0; j < 16; j += 2) most = mv::max3(most, p[j], p[j + 1]);
+        for (int j = 0; j < W; j += 2) most = mv::max3(most, p[j], p[j + 1]);
         top = fmaxf(top, most);
-        uint32_t hi[4], lo[4];
+        uint32_t hi[W / 4], lo[W / 4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t h0, l0, h1, l1;
-          split_e4m3x2(p[k * 4], p[k * 4 + 1], h0, l0);
-          split_e4m3x2(p[k * 4 + 2], p[k * 4 + 3], h1, l1);
-          hi[k] = h0 | (h1 << 16);
-          lo[k] = l0 | (l1 << 16);
+        for (int k = 0; k < W / 4; ++k) {
+          split_e4m3x4(p[k * 4], p[k * 4 + 1], p[k * 4 + 2], p[k * 4 + 3], hi[k], lo[k]);
         }
-        *reinterpret_cast<uint4*>(p_row + ((b ^ sw) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(p_row + (((b + nb) ^ sw) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        unsigned char* const at_hi = p_row + (((col >> 4) ^ sw) << 4);
+        unsigned char* const at_lo = p_row + ((((col >> 4) + nb) ^ sw) << 4);
+        if constexpr (W == 16) {
+          *reinterpret_cast<uint4*>(at_hi) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(at_lo) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        } else {
+          *reinterpret_cast<uint2*>(at_hi + (col & 8)) = make_uint2(hi[0], hi[1]);
+          *reinterpret_cast<uint2*>(at_lo + (col & 8)) = make_uint2(lo[0], lo[1]);
+        }
         // A weight past the format's range only says that the references have to move; what it adds here is taken back then, so it must
         // not overflow (capped, it still exceeds what the move leaves of it, and the sum loses nothing but a rounding).
         if (most > 0x1p60f)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) p[j] = p[j] > 0x1p60f ? 0x1p60f : p[j];
-        if (first)
+          for (int j = 0; j < W; ++j) p[j] = p[j] > 0x1p60f ? 0x1p60f : p[j];
+        uint32_t l[W];
+        if constexpr (W == 16) mv::um::ld16(lanes + at.sums + col, l);
+        else mv::um::ld8(lanes + at.sums + col, l);
+        mv::um::wait_ld();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) l[j] = 0;
-#pragma unroll
-        for (int j = 0; j < 16; j += 2) {
+        for (int j = 0; j < W; j += 2) {
           float x, y;
-          mv::unpack_f32x2(mv::fma_f32x2(mv::pack_f32x2(p[j], p[j + 1]), vinv2, mv::pack_u32x2(l[j], l[j + 1])), x, y);
+          mv::unpack_f32x2(mv::fma_f32x2(mv::pack_f32x2(p[j], p[j + 1]), vinv2, first ? 0ull : mv::pack_u32x2(l[j], l[j + 1])), x, y);
           l[j] = __float_as_uint(x);
           l[j + 1] = __float_as_uint(y);
         }
-        mv::um::st16(lanes + at.sums + b * 16, l);
-      }
-      mv::um::wait_st();
+        if constexpr (W == 16) mv::um::st16(lanes + at.sums + col, l);
+        else mv::um::st8(lanes + at.sums + col, l);
+      };
+#pragma unroll 1
+      for (int u = group; u < (GROUPS == 2 ? nb & ~1 : nb); u += GROUPS) columns(Width<16>{}, u * 16);
+      if (GROUPS == 2 && (nb & 1)) columns(Width<8>{}, (nb - 1) * 16 + group * 8);
       return top;
     };
     float sign = 1.f;
-    bool lift = t == 0;  // no references yet
+    const uint2 seen2 = meta->seen[tile % METAS];
+    const uint64_t seen = (uint64_t(seen2.y) << 32) | seen2.x;
+    bool lift = (seen & ~referenced) != 0;  // some q-vector sees its first tokens
+    referenced |= seen;
     for (;;) {
       if (lift) {
         // ---- references move: the largest exponent of every q-vector over the tile's tokens
+        if (t > 0) ok = ok && warp_wait(c, bar(&meta->pv_done[(tile - 1) & 1]), ((tile - 1) >> 1) & 1);  // O and the exchange area are free
         if (!vote_all(ok)) return false;
-#pragma unroll 1
-        for (int b = 0; b < nb; ++b) {
-          uint32_t sc[16];
-          mv::um::ld16(s_t + b * 16, sc);
+        mv::um::fence_after();
+        own([&](int b) {
+          uint32_t sc[8];
+          mv::um::ld8(s_t + b * 8, sc);
           mv::um::wait_ld();
           int best = 0;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int q = b * 16 + j;
-            float y = fmaf(__uint_as_float(sc[j]), meta->factor[q] * ks, evf);
-            if (!((see >> q) & 1) || y != y) y = -INFINITY;
+          for (int j = 0; j < 8; ++j) {
+            const int q = b * 8 + j;
+            float y = fmaf(__uint_as_float(sc[j]), fk, evf);
+            if (!((see >> q) & 1) || q >= s.n_qv || y != y) y = -INFINITY;
             const int k = __float_as_int(y);
             const int m = __reduce_max_sync(0xffffffffu, k < 0 ? k ^ 0x7fffffff : k);  // ordered as the floats are
             if (lane == j) best = m;
           }
-          if (lane < 16) xch[warp * MAXQV + b * 16 + lane] = __int_as_float(best < 0 ? best ^ 0x7fffffff : best);
-        }
+          if (lane < 8) xch[quarter * MAXQV + b * 8 + lane] = __int_as_float(best < 0 ? best ^ 0x7fffffff : best);
+        });
         (void)vote_all(true);
+        float f = 1.f;
         if (tid < cols) {
           const float m = fmaxf(fmaxf(xch[tid], xch[MAXQV + tid]), fmaxf(xch[2 * MAXQV + tid], xch[3 * MAXQV + tid]));
           const float now = meta->minus_ref[tid], want = HEADROOM - m;
-          float f = 1.f;
           if (tid < s.n_qv && m > -INFINITY && want < now) {
-            f = mv::fast_exp2(want - now);  // 0 where there was none
+            f = mv::fast_exp2(want - now);  // 0 where there was none: O and the sums are zero (or NaN) there
             meta->minus_ref[tid] = want;
           }
           xch[4 * MAXQV + tid] = f;
         }
-        (void)vote_all(true);
-        if (t > 0) {
+        if (vote_any(f != 1.f && f != 0.f)) {
+          mv::um::wait_st();
+          own([&](int b) {
+            const float* const f = xch + 4 * MAXQV + b * 8;
 #pragma unroll 1
-          for (int b = 0; b < 3 * nb; ++b) {  // O and the sums, which lie side by side
-            uint32_t o[16];
-            mv::um::ld16(lanes + at.o + b * 16, o);
-            mv::um::wait_ld();
-            const float* f = xch + 4 * MAXQV + (b % nb) * 16;
+            for (int k = 0; k < 3; ++k) {  // O (values, remainders) and the sums, which lie side by side
+              uint32_t o[8];
+              mv::um::ld8(lanes + at.o + k * cols + b * 8, o);
+              mv::um::wait_ld();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f[j]);
-            mv::um::st16(lanes + at.o + b * 16, o);
-          }
+              for (int j = 0; j < 8; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f[j]);
+              mv::um::st8(lanes + at.o + k * cols + b * 8, o);
+            }
+          });
           mv::um::wait_st();
         }
         (void)vote_all(true);  // every thread has read the exchange area
@@ -454,36 +492,36 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
       if (!vote_any(top > TOP || !ok)) break;
       sign = -1.f;
     }
-    if (!__all_sync(0xffffffffu, valid)) {
+    if (!plain && !__all_sync(0xffffffffu, valid)) {
       // no token here: whatever the slot holds meets a weight of zero, so it must be finite
       const int vp = 2 * tile + 1, vslot = vp % RING;
       ok = ok && warp_wait(c, bar(&meta->full[vslot]), (vp / RING) & 1);
       if (!valid) {
-        uint4* const row = reinterpret_cast<uint4*>(c.smem + vslot * PIECE + tid * 128);
+        uint4* const row = reinterpret_cast<uint4*>(c.smem + vslot * PIECE + token * 128);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) row[k] = make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < 8 / GROUPS; ++k) row[group * (8 / GROUPS) + k] = make_uint4(0, 0, 0, 0);
       }
     }
     mv::fence_proxy_async();
     mv::um::fence_before();
     __syncwarp();
-    if (lane == 0 && ok) mv::mbar_arrive(bar(&meta->p_full));
+    if (lane == 0 && ok) mv::mbar_arrive(bar(&meta->p_full[tile & 1]));
   }
   // ---- the segment's result: sums over the tokens, then the head vectors (thread = element)
-  ok = ok && warp_wait(c, bar(&meta->pv_done), (tile - 1) & 1);
+  ok = ok && warp_wait(c, bar(&meta->pv_done[(tile - 1) & 1]), ((tile - 1) >> 1) & 1);  // (products complete in order)
   if (!vote_all(ok)) return false;
   mv::um::fence_after();
-#pragma unroll 1
-  for (int b = 0; b < nb; ++b) {
-    // sixteen columns over 32 lanes by halving: after four steps a lane holds one column's sum over half the lanes
-    uint32_t l[16];
-    mv::um::ld16(lanes + at.sums + b * 16, l);
+  mv::um::wait_st();
+  own([&](int b) {
+    // eight columns over 32 lanes by halving: after three steps a lane holds one column's sum over eight lanes
+    uint32_t l[8];
+    mv::um::ld8(lanes + at.sums + b * 8, l);
     mv::um::wait_ld();
-    float y[16];
+    float y[8];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) y[j] = __uint_as_float(l[j]);
+    for (int j = 0; j < 8; ++j) y[j] = __uint_as_float(l[j]);
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) {
+    for (int o = 4; o > 0; o >>= 1) {
       const bool up = (lane & o) != 0;
 #pragma unroll
       for (int j = 0; j < o; ++j) {
@@ -491,9 +529,10 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
         y[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
       }
     }
+    y[0] += __shfl_xor_sync(0xffffffffu, y[0], 8);
     y[0] += __shfl_xor_sync(0xffffffffu, y[0], 16);
-    if (lane < 16) xch[warp * MAXQV + b * 16 + lane] = y[0];
-  }
+    if (lane < 8) xch[quarter * MAXQV + b * 8 + lane] = y[0];
+  });
   (void)vote_all(true);
   if (tid < s.n_qv) {
     const float sum = (xch[tid] + xch[MAXQV + tid]) + (xch[2 * MAXQV + tid] + xch[3 * MAXQV + tid]);
@@ -501,55 +540,67 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
     if (s.slot >= 0) a.part_ml[s.slot * MAXQV + tid] = make_float2(-meta->minus_ref[tid], sum);  // no token seen: reference -infinity, sum 0
   }
   (void)vote_all(true);
-  int r = 0, h = 0;  // row and head of q-vector q
-#pragma unroll 1
-  for (int b = 0; b < nb; ++b) {
-    uint32_t o0[16], o1[16];
-    mv::um::ld16(lanes + at.o + b * 16, o0);
-    mv::um::ld16(lanes + at.o + (nb + b) * 16, o1);
+  own([&](int b) {
+    uint32_t o0[8], o1[8];
+    mv::um::ld8(lanes + at.o + b * 8, o0);
+    mv::um::ld8(lanes + at.o + (n8 + b) * 8, o1);
+    const int left = s.n_qv - b * 8;
+    int h = (b * 8) % a.G;  // head of the q-vector inside the group
+    bf16* out = a.out + (int64_t(s.row0 + b * 8 / a.G) * a.Hq + s.head * a.G + h) * D + token;
+    float* part = a.part_o + (int64_t(s.slot) * MAXQV + b * 8) * D + token;
+    const int next_row = (a.Hq - a.G) * D;
     mv::um::wait_ld();
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const int q = b * 16 + j;
-      if (q < s.n_qv) {
-        const float y = fmaf(__uint_as_float(o1[j]), 1.f / LO_SCALE, __uint_as_float(o0[j]));
-        if (s.slot >= 0) a.part_o[(int64_t(s.slot) * MAXQV + q) * D + tid] = y;
-        else a.out[(int64_t(s.row0 + r) * a.Hq + s.head * a.G + h) * D + tid] = __float2bfloat16_rn(y * xch[4 * MAXQV + q]);
-        if (++h == a.G) {
-          h = 0;
-          ++r;
-        }
+    for (int j = 0; j < 8; ++j) {
+      const float y = fmaf(__uint_as_float(o1[j]), 1.f / LO_SCALE, __uint_as_float(o0[j]));
+      if (j < left) {
+        if (s.slot >= 0) part[j * D] = y;
+        else *out = __float2bfloat16_rn(y * xch[4 * MAXQV + b * 8 + j]);
+      }
+      out += D;
+      if (++h == a.G) {
+        h = 0;
+        out += next_row;
       }
     }
-  }
+  });
   mv::um::fence_before();
   (void)vote_all(true);  // O and the exchange area have been read
   return true;
 }
 
 __device__ __forceinline__ void softmax_warps(const Cta& c) {
-  Walk w;
+  mv::blk::Walk w;
   w.begin(*c.a, blockIdx.x);
   mv::blk::Segment s;
+  mv::blk::CutLog cuts;
   int tile = 0;  // tiles of the share so far: ring position, score buffer and phases follow from it
   bool ok = true;
   while (ok && w.next(*c.a, s, false)) {
+    cuts.add(*c.a, s);
     stage_q(c, s, (s.n_qv + 15) / 16 * 16);
     mv::fence_proxy_async();
     (void)vote_all(true);  // the factors are there for all
     if ((threadIdx.x & 31) == 0) mv::mbar_arrive(bar(&c.meta->q_full));
     ok = run_segment(c, s, tile);
   }
+  if (threadIdx.x == 0) cuts.store(*c.a, blockIdx.x);
 }
 
-// ---- issuer warp: the whole warp walks and waits, one elected lane issues ----------------------------------
-__device__ __forceinline__ void issuer(const Cta& c) {
+// ---- issuer warps: the whole warp walks and waits, one elected lane issues ----------------------------------
+// After a wait has run out, products may still be in flight: they must have completed before the CTA frees its tensor memory.
+__device__ __forceinline__ void drain(const Cta& c, int which, bool lead) {
+  if (lead) mv::um::commit(bar(&c.meta->drained[which]));
+  (void)mv::mbar_wait_bounded(bar(&c.meta->drained[which]), 0, 20000000ull);
+  __syncwarp();
+}
+
+// S^T = K Q^T of every tile into score buffer tile & 1: K is the 128-row operand, values of Q then remainders
+__device__ __forceinline__ void score_issuer(const Cta& c) {
   Meta* const meta = c.meta;
   const bool lead = mv::um::elect_one();
-  const uint32_t tmem = meta->tmem;
   const uint64_t q_desc = mv::um::smem_desc(c.base + OFF_Q, 16, 1024);
-  const uint64_t p_desc = mv::um::smem_desc(c.base + OFF_P, PIECE, 1024);
-  Walk w;
+  mv::blk::Walk w;
   w.begin(*c.a, blockIdx.x);
   mv::blk::Segment s;
   int tile = 0, segment = 0;
@@ -557,60 +608,68 @@ __device__ __forceinline__ void issuer(const Cta& c) {
   while (ok && w.next(*c.a, s, false)) {
     const int cols = (s.n_qv + 15) / 16 * 16;
     const Columns at(cols);
-    const uint32_t o_t = tmem + at.o;
-    const uint32_t idesc_s = mv::um::idesc_e4m3(128, cols, 0, 0), idesc_o = mv::um::idesc_e4m3(128, 2 * cols, 1, 1);
+    const uint32_t idesc = mv::um::idesc_e4m3(128, cols, 0, 0);
     ok = warp_wait(c, bar(&meta->q_full), segment & 1);
     ++segment;
-    // S^T = K Q^T of tile t of the share into score buffer t & 1: K is the 128-row operand, values of Q then remainders
-    auto scores = [&](int t) {
-      const int slot = (2 * t) % RING;
-      ok = ok && warp_wait(c, bar(&meta->full[slot]), ((2 * t) / RING) & 1);
-      if (!ok) return;
-      mv::um::fence_after();
-      if (lead) {
-        const uint64_t k_desc = mv::um::smem_desc(c.base + slot * PIECE, 16, 1024);
-        const uint32_t s_t = tmem + ((t & 1) ? at.s1 : 0);
-        mv::um::mma8_ss<false>(s_t, k_desc, q_desc, idesc_s);
-#pragma unroll
-        for (int k = 1; k < D / 32; ++k) mv::um::mma8_ss<true>(s_t, k_desc + uint32_t((k * 32) >> 4), q_desc + uint32_t((k * 32) >> 4), idesc_s);
-#pragma unroll
-        for (int k = 0; k < D / 32; ++k)
-          mv::um::mma8_ss<true>(s_t, k_desc + uint32_t((k * 32) >> 4), q_desc + uint32_t((Q_BYTES + k * 32) >> 4), idesc_s);
-        mv::um::commit(bar(&meta->s_full[t & 1]));
-        mv::um::commit(bar(&meta->empty[slot]));
-      }
-      __syncwarp();
-    };
-    scores(tile);
 #pragma unroll 1
     for (int t = 0; t < s.n_tiles && ok; ++t, ++tile) {
-      // the other score buffer was read before the weights of tile t - 1 were handed over; a single one before those of tile t are
-      if (t + 1 < s.n_tiles && cols < 64) scores(tile + 1);
-      const int vp = 2 * tile + 1, vslot = vp % RING;
-      ok = ok && warp_wait(c, bar(&meta->p_full), tile & 1);
-      if (t + 1 < s.n_tiles && cols == 64) scores(tile + 1);
-      ok = ok && warp_wait(c, bar(&meta->full[vslot]), (vp / RING) & 1);
+      // the buffer was read before the weights of the tile that last used it were handed over: two tiles ago, or one where there is room for one
+      const int last = tile - (cols < 64 ? 2 : 1), slot = (2 * tile) % RING;
+      if (t > 0 && last >= 0) ok = warp_wait(c, bar(&meta->p_full[last & 1]), (last >> 1) & 1);
+      ok = ok && warp_wait(c, bar(&meta->full[slot]), ((2 * tile) / RING) & 1);
       if (!ok) break;
       mv::um::fence_after();
       if (lead) {
-        // O^T += V^T P^T: V is the 128-row operand, read across its rows (32 tokens per instruction)
-        const uint64_t v_desc = mv::um::smem_desc(c.base + vslot * PIECE, PIECE, 1024);
-        if (t == 0) mv::um::mma8_ss<false>(o_t, v_desc, p_desc, idesc_o);
-        else mv::um::mma8_ss<true>(o_t, v_desc, p_desc, idesc_o);
+        const uint64_t k_desc = mv::um::smem_desc(c.base + slot * PIECE, 16, 1024);
+        const uint32_t s_t = meta->tmem + ((tile & 1) ? at.s1 : 0);
+        mv::um::mma8_ss<false>(s_t, k_desc, q_desc, idesc);
 #pragma unroll
-        for (int k = 1; k < TILE / 32; ++k) mv::um::mma8_ss<true>(o_t, v_desc + uint32_t((k * 4096) >> 4), p_desc + uint32_t((k * 4096) >> 4), idesc_o);
-        mv::um::commit(bar(&meta->pv_done));
+        for (int k = 1; k < D / 32; ++k) mv::um::mma8_ss<true>(s_t, k_desc + uint32_t((k * 32) >> 4), q_desc + uint32_t((k * 32) >> 4), idesc);
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k)
+          mv::um::mma8_ss<true>(s_t, k_desc + uint32_t((k * 32) >> 4), q_desc + uint32_t((Q_BYTES + k * 32) >> 4), idesc);
+        mv::um::commit(bar(&meta->s_full[tile & 1]));
+        mv::um::commit(bar(&meta->empty[slot]));
+      }
+      __syncwarp();
+    }
+  }
+  if (!ok) drain(c, 0, lead);
+}
+
+// O^T += V^T P^T of every tile: V is the 128-row operand, read across its rows (32 tokens per instruction)
+__device__ __forceinline__ void output_issuer(const Cta& c) {
+  Meta* const meta = c.meta;
+  const bool lead = mv::um::elect_one();
+  mv::blk::Walk w;
+  w.begin(*c.a, blockIdx.x);
+  mv::blk::Segment s;
+  int tile = 0;
+  bool ok = true;
+  while (ok && w.next(*c.a, s, false)) {
+    const int cols = (s.n_qv + 15) / 16 * 16;
+    const uint32_t o_t = meta->tmem + Columns(cols).o;
+    const uint32_t idesc = mv::um::idesc_e4m3(128, 2 * cols, 1, 1);
+#pragma unroll 1
+    for (int t = 0; t < s.n_tiles; ++t, ++tile) {
+      const int vp = 2 * tile + 1, vslot = vp % RING;
+      ok = warp_wait(c, bar(&meta->full[vslot]), (vp / RING) & 1) && warp_wait(c, bar(&meta->p_full[tile & 1]), (tile >> 1) & 1);
+      if (!ok) break;
+      mv::um::fence_after();
+      if (lead) {
+        const uint64_t v_desc = mv::um::smem_desc(c.base + vslot * PIECE, PIECE, 1024);
+        const uint64_t p_desc = mv::um::smem_desc(c.base + OFF_P + (tile & 1) * PIECE, PIECE, 1024);
+        if (t == 0) mv::um::mma8_ss<false>(o_t, v_desc, p_desc, idesc);
+        else mv::um::mma8_ss<true>(o_t, v_desc, p_desc, idesc);
+#pragma unroll
+        for (int k = 1; k < TILE / 32; ++k) mv::um::mma8_ss<true>(o_t, v_desc + uint32_t((k * 4096) >> 4), p_desc + uint32_t((k * 4096) >> 4), idesc);
+        mv::um::commit(bar(&meta->pv_done[tile & 1]));
         mv::um::commit(bar(&meta->empty[vslot]));
       }
       __syncwarp();
     }
   }
-  if (!ok) {
-    // products may still be in flight: they must have completed before the CTA frees its tensor memory
-    if (lead) mv::um::commit(bar(&meta->drained));
-    (void)mv::mbar_wait_bounded(bar(&meta->drained), 0, 20000000ull);
-    __syncwarp();
-  }
+  if (!ok) drain(c, 1, lead);
 }
 
 __global__ void __launch_bounds__(NT, 2) decode_blk_tc_kernel(const Args a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
@@ -619,7 +678,11 @@ __global__ void __launch_bounds__(NT, 2) decode_blk_tc_kernel(const Args a, cons
   const int tid = threadIdx.x, warp = tid >> 5;
   const uint32_t base = mv::smem_u32(smem);
   if ((base & 1023u) != 0) {  // the swizzle pattern is anchored at 1024-byte boundaries
-    if (tid == 0) atomicExch(a.t.counts + 4, int(MV_ERR_UNSUPPORTED));
+    mv::grid_dependency_wait();
+    if (tid == 0) {
+      atomicExch(a.t.counts + 4, int(MV_ERR_UNSUPPORTED));
+      mv::blk::CutLog().store(a, blockIdx.x);
+    }
     return;
   }
   if (tid == 0) {
@@ -629,11 +692,13 @@ __global__ void __launch_bounds__(NT, 2) decode_blk_tc_kernel(const Args a, cons
       mv::mbar_init(bar(&meta->empty[i]), 1);  // one tcgen05.commit after the product that read the piece
     }
     for (int i = 0; i < METAS; ++i) mv::mbar_init(bar(&meta->described[i]), 1);
-    for (int i = 0; i < 2; ++i) mv::mbar_init(bar(&meta->s_full[i]), 1);
-    mv::mbar_init(bar(&meta->q_full), 4);   // the softmax warps
-    mv::mbar_init(bar(&meta->p_full), 4);
-    mv::mbar_init(bar(&meta->pv_done), 1);
-    mv::mbar_init(bar(&meta->drained), 1);
+    for (int i = 0; i < 2; ++i) {
+      mv::mbar_init(bar(&meta->s_full[i]), 1);
+      mv::mbar_init(bar(&meta->p_full[i]), SOFTMAX / 32);
+      mv::mbar_init(bar(&meta->pv_done[i]), 1);
+      mv::mbar_init(bar(&meta->drained[i]), 1);
+    }
+    mv::mbar_init(bar(&meta->q_full), SOFTMAX / 32);
     mv::mbar_fence_init();
     mv::fence_proxy_async();
   }
@@ -648,9 +713,11 @@ __global__ void __launch_bounds__(NT, 2) decode_blk_tc_kernel(const Args a, cons
   mv::grid_dependency_wait();
   mv::grid_dependency_launch_dependents();
   Cta c{&a, smem, base, meta, a.t.counts + 4};
-  if (warp == 4) producer(c, &tm_k, &tm_v);
-  else if (warp == 5) issuer(c);
-  else softmax_warps(c);
+  if (warp < SOFTMAX / 32) softmax_warps(c);
+  else if (warp == SOFTMAX / 32) producer<true>(c, &tm_k);
+  else if (warp == SOFTMAX / 32 + 1) producer<false>(c, &tm_v);
+  else if (warp == SOFTMAX / 32 + 2) score_issuer(c);
+  else output_issuer(c);
   mv::um::fence_before();
   __syncthreads();
   if (warp == 0) mv::um::tmem_dealloc(meta->tmem, 256);
