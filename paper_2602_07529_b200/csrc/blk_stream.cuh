@@ -43,6 +43,7 @@ struct Args {
   int64_t num_pages;
   int Hq, Hkv, G;
   float scale_log2;    // softmax scale * log2 e
+  int cost_shift;      // see tile_cost
 };
 
 inline size_t part_o_bytes(int d) { return size_t(2) * SHARES * MAXQV * d * sizeof(float); }
@@ -51,13 +52,11 @@ inline size_t workspace_bytes(int d) { return part_o_bytes(d) + part_ml_bytes() 
 
 // Costs in units of about 0.3 us of a share, fitted to clock readings of the tensor kernel: a tile takes 1.2 us with 16
 // q-vectors (as long as its bytes take to arrive) and 0.5 to 0.6 more for every further 16, a stream's set-up, first references and
-// epilogue another 4 us.
-__device__ __forceinline__ int tile_cost(int n_qv) { return 2 + 2 * ((n_qv + 15) / 16); }
-__device__ __forceinline__ int stream_cost(int n_qv) { return 10 + 2 * ((n_qv + 15) / 16); }
-// quotient of non-negative numbers, in 32 bits where they fit
-__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
-  return ((x | y) >> 32) == 0 ? int64_t(uint32_t(x) / uint32_t(y)) : x / y;
-}
+// epilogue another 4 us.  In a step of more than some hundred million tiles the unit grows by 2^shift, so that 32 bits
+// hold the sum: 64-bit arithmetic would lengthen the start of every launch, which is instruction fetches for the most part.
+constexpr int COST_PER_TILE = 10, COST_PER_STREAM = 18;  // the largest
+__device__ __forceinline__ uint32_t tile_cost(int blocks, int shift) { return max(1, (2 + 2 * blocks) >> shift); }
+__device__ __forceinline__ uint32_t stream_cost(int blocks, int shift) { return (10 + 2 * blocks) >> shift; }
 
 // A run of tiles of one stream inside a share.
 struct Segment {
@@ -71,20 +70,20 @@ struct Segment {
 // The segments of one share, in order.  Every warp that needs them walks by itself; begin() is called by a whole warp.
 struct Walk {
   int n_groups, share, g, head, tile;
-  int r0, n_qv, e0, e1, tiles;       // of group g
-  int per, per_tile, per_stream;     // costs of one of its streams (per: all of it), of a tile, of the set-up
-  int64_t base, x_end;               // cost position of group g's first stream; end of the share
+  int r0, n_qv, e0, e1, tiles;            // of group g
+  uint32_t per, per_tile, per_stream;     // costs of one of its streams (per: all of it), of a tile, of the set-up
+  uint32_t base, x_end;                   // cost position of group g's first stream; end of the share
 
-  __device__ __forceinline__ void take_group(int row0, int row1, int ent0, int ent1, int n_tiles, int G) {
+  __device__ __forceinline__ void take_group(const Args& a, int row0, int row1, int ent0, int ent1, int n_tiles) {
     r0 = row0;
-    n_qv = (row1 - row0) * G;
+    n_qv = (row1 - row0) * a.G;
     e0 = ent0;
     e1 = ent1;
     tiles = n_tiles;
-    const int qv = max(1, min(MAXQV, n_qv));
-    per_tile = tile_cost(qv);
-    per_stream = stream_cost(qv);
-    per = tiles > 0 ? per_stream + int(min(int64_t(per_tile) * tiles, int64_t(1) << 30)) : 0;
+    const int blocks = max(1, min(MAXQV / 16, (n_qv + 15) / 16));
+    per_tile = tile_cost(blocks, a.cost_shift);
+    per_stream = stream_cost(blocks, a.cost_shift);
+    per = tiles > 0 ? per_stream + per_tile * uint32_t(tiles) : 0;
   }
   // Two passes over the groups, 32 at a time: the total cost, then the group that holds the share's first tile.  The loads of
   // a pass do not wait for anything (the arrays are as long as the capacities say), so a step of up to 32 groups costs one
@@ -93,7 +92,6 @@ struct Walk {
     const int lane = threadIdx.x & 31;
     share = c;
     const int counted = __ldcg(a.t.counts + 1);
-    int64_t total = 0;
     int row[2], ent[2], til[2];
     auto load = [&](int i) {
       const bool there = i < a.t.max_groups;
@@ -105,35 +103,37 @@ struct Walk {
       }
     };
     auto cost_of = [&](int i) {
-      if (i >= n_groups) return int64_t(0);
-      take_group(row[0], row[1], ent[0], ent[1], til[1] - til[0], a.G);
-      return int64_t(a.Hkv) * per;
+      take_group(a, row[0], row[1], ent[0], ent[1], til[1] - til[0]);
+      return i < n_groups ? uint32_t(a.Hkv) * per : 0u;
     };
     load(lane);
     n_groups = max(0, min(counted, a.t.max_groups));
+    uint32_t sum = 0;
+#pragma unroll 1
     for (int i = lane;;) {
-      total += cost_of(i);
+      sum += cost_of(i);
       i += 32;
       if (i - lane >= n_groups) break;
       load(i);
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    const int64_t x = total * c / SHARES;
-    x_end = total * (c + 1) / SHARES;
+    const uint32_t total = __reduce_add_sync(0xffffffffu, sum);
+    const uint32_t each = total / SHARES, more = total % SHARES;  // the first `more` shares hold one unit more
+    const uint32_t x = each * c + min(uint32_t(c), more);
+    x_end = x + each + (uint32_t(c) < more ? 1 : 0);
     g = n_groups;
-    base = 0;
     if (x >= x_end) {
       g = n_groups = 0;
       return;
     }
+    base = 0;
+#pragma unroll 1
     for (int i0 = 0; i0 < n_groups; i0 += 32) {
       if (n_groups > 32) load(i0 + lane);
-      const int64_t own = cost_of(i0 + lane);
-      int64_t upto = own;
+      const uint32_t own = cost_of(i0 + lane);
+      uint32_t upto = own;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, upto, o);
+        const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
         if (lane >= o) upto += y;
       }
       const unsigned past = __ballot_sync(0xffffffffu, base + upto > x);
@@ -141,35 +141,41 @@ struct Walk {
         const int l = __ffs(past) - 1;
         g = i0 + l;
         base += __shfl_sync(0xffffffffu, upto - own, l);
-        const int q0 = __shfl_sync(0xffffffffu, row[0], l), q1 = __shfl_sync(0xffffffffu, row[1], l);
-        const int f0 = __shfl_sync(0xffffffffu, ent[0], l), f1 = __shfl_sync(0xffffffffu, ent[1], l);
-        take_group(q0, q1, f0, f1, __shfl_sync(0xffffffffu, til[1] - til[0], l), a.G);
+        // the lane's members hold its own group
+        r0 = __shfl_sync(0xffffffffu, r0, l);
+        n_qv = __shfl_sync(0xffffffffu, n_qv, l);
+        e0 = __shfl_sync(0xffffffffu, e0, l);
+        e1 = __shfl_sync(0xffffffffu, e1, l);
+        tiles = __shfl_sync(0xffffffffu, tiles, l);
+        per = __shfl_sync(0xffffffffu, per, l);
+        per_tile = __shfl_sync(0xffffffffu, per_tile, l);
+        per_stream = __shfl_sync(0xffffffffu, per_stream, l);
         break;
       }
       base += __shfl_sync(0xffffffffu, upto, 31);
     }
     if (g >= n_groups) return;
-    const int64_t in_group = x - base;
-    head = int(quotient(in_group, per));
-    const int64_t behind = in_group - int64_t(head) * per - per_stream;  // the share starts at the first tile whose point is not before x
-    tile = behind > 0 ? int(quotient(behind + per_tile - 1, per_tile)) : 0;
+    head = int((x - base) / per);
+    base += uint32_t(head) * per;                 // from here on: of the stream
+    const uint32_t at = x - base;                 // the share starts at the first tile whose point is not before x
+    tile = at > per_stream ? int((at - per_stream + per_tile - 1) / per_tile) : 0;
   }
   // The next sound segment; false at the end of the share.
   __device__ __forceinline__ bool next(const Args& a, Segment& s, bool report) {
     while (g < n_groups) {
       if (tile >= tiles) {
         tile = 0;
+        base += per;
         if (++head >= a.Hkv || tiles <= 0) {
           head = 0;
-          base += int64_t(a.Hkv) * per;
           if (++g < n_groups)
-            take_group(__ldcg(a.t.row_off + g), __ldcg(a.t.row_off + g + 1), __ldcg(a.t.ent_off + g), __ldcg(a.t.ent_off + g + 1),
-                       __ldcg(a.t.tile_off + g + 1) - __ldcg(a.t.tile_off + g), a.G);
+            take_group(a, __ldcg(a.t.row_off + g), __ldcg(a.t.row_off + g + 1), __ldcg(a.t.ent_off + g), __ldcg(a.t.ent_off + g + 1),
+                       __ldcg(a.t.tile_off + g + 1) - __ldcg(a.t.tile_off + g));
         }
         continue;
       }
-      const int64_t left = x_end - (base + int64_t(head) * per + per_stream);  // tiles whose points lie before the share's end
-      const int end = left > 0 ? int(min(int64_t(tiles), quotient(left + per_tile - 1, per_tile))) : 0;
+      const uint32_t first = base + per_stream;  // point of the stream's first tile; the share holds the tiles whose points lie before its end
+      const int end = x_end > first ? min(tiles, int((x_end - first + per_tile - 1) / per_tile)) : 0;
       if (end <= tile) return false;
       s.group = g;
       s.head = head;

@@ -32,7 +32,6 @@ using mv::blk::PS;
 using mv::blk::SHARES;
 
 constexpr int NT = 128, NW = NT / 32;
-constexpr int MERGE_Y = 8;  // CTAs that share the q-vectors of a cut stream
 
 __device__ __forceinline__ uint32_t half2_of_e4m3x2(uint32_t v) {
   uint32_t h;
@@ -343,22 +342,24 @@ __global__ void __launch_bounds__(NT) decode_blk_kernel(const Args a) {
   if (tid == 0) cuts.store(a, blockIdx.x);
 }
 
-// Merge of the cut streams: CTA (c, y) takes the stream that starts in share c and ends in a later one, if there is one, and of
-// its q-vectors y, y + gridDim.y, ...  out = sum_i w_i O_i / sum_i w_i l_i,  w_i = 2^(m_i - max m).  Bound by latency, three
-// dependent round trips: the shares' records, the references, the parts, which the four warps deal out among themselves with eight loads
-// in flight each.
+// Merge of the cut streams: CTA c takes the stream that starts in share c and ends in a later one, if there is one.
+//   out = sum_i w_i O_i / sum_i w_i l_i,  w_i = 2^(m_i - max m) over the stream's parts i.
+// Bound by latency, two dependent round trips: the shares' records; references and parts.  Where a stream has fewer q-vectors than
+// the CTA has warps, several warps deal out the parts of one among themselves.
+constexpr int MERGE_WARPS = 16;
 template <int D>
-__global__ void __launch_bounds__(128) decode_blk_merge_kernel(const Args a) {
+__global__ void __launch_bounds__(MERGE_WARPS * 32, 2) decode_blk_merge_kernel(const Args a) {
   constexpr int VEC = D / 32;  // elements of the head vector per lane
-  __shared__ float so[NW][D], ssum[NW];
+  __shared__ float so[MERGE_WARPS][D], ssum[MERGE_WARPS], stop[MERGE_WARPS];
   mv::grid_dependency_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = blockIdx.x;
   const int4* const cuts = reinterpret_cast<const int4*>(a.cuts);
   auto first_of = [&](int i) { return i < SHARES ? __ldcg(cuts + 2 * i) : make_int4(-1, 0, 0, 0); };
   int4 r = first_of(c + 1 + lane);
   const int4 own = __ldcg(cuts + 2 * c + 1);
+  const int counted = __ldcg(a.t.counts + 1);
   if (own.x >= 0) {
-    // The shares behind that hold something of the stream (at most the last holds more than it: shares that hold nothing at all may lie between)
+    // the shares behind that hold something of the stream (shares that hold nothing at all may lie between)
     unsigned parts = 0;  // of the 32 shares behind c
     int c1 = c;
     for (int i0 = c + 1; i0 < SHARES; i0 += 32) {
@@ -371,24 +372,23 @@ __global__ void __launch_bounds__(128) decode_blk_merge_kernel(const Args a) {
     auto holds = [&](int i) {  // share i >= c
       return i == c || (i - c <= 32 ? ((parts >> (i - c - 1)) & 1) != 0 : __ldcg(&a.cuts[2 * i].stream) == own.x);
     };
-    const int head = own.x % a.Hkv;
-    for (int v = blockIdx.y; v < own.z; v += gridDim.y) {
-      // part i of the stream: slot 2 c + 1, then slots 2 i of the shares behind
-      float top = -INFINITY;
-      for (int i = c + lane; i <= c1; i += 32)
-        if (holds(i)) top = fmaxf(top, __ldcg(&a.part_ml[(2 * i + (i == c)) * MAXQV + v]).x);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      float acc[VEC] = {}, sum = 0.f;
-      for (int i0 = c + warp; i0 <= c1; i0 += NW * 8) {
+    const int n_qv = own.z, head = own.x % a.Hkv;
+    int per = 1;  // warps of one q-vector
+    while (per < MERGE_WARPS && 2 * per * n_qv <= MERGE_WARPS && 4 * per <= c1 - c + 1) per *= 2;
+    const int sub = warp % per;
+    for (int v0 = 0; v0 < n_qv; v0 += MERGE_WARPS / per) {
+      const int v = v0 + warp / per;
+      // parts sub, sub + per, ... of the stream (part i: slot 2 c + 1, then slots 2 i of the shares behind), against the warp's own reference
+      float top = -INFINITY, sum = 0.f, acc[VEC] = {};
+      for (int i0 = c + sub; i0 <= c1 && v < n_qv; i0 += per * 8) {
         float2 ml[8];
         float y[8][VEC];
         bool there[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const int i = i0 + k * NW;
+          const int i = i0 + k * per;
           there[k] = i <= c1 && holds(i);
-          ml[k] = make_float2(0.f, 0.f);
+          ml[k] = make_float2(-INFINITY, 0.f);
 #pragma unroll
           for (int e = 0; e < VEC; ++e) y[k][e] = 0.f;
           if (there[k]) {
@@ -404,36 +404,58 @@ __global__ void __launch_bounds__(128) decode_blk_merge_kernel(const Args a) {
             }
           }
         }
+        float now = top;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) now = fmaxf(now, ml[k].x);
+        const float f = top == -INFINITY ? 1.f : mv::fast_exp2(top - now);  // nothing seen so far: zeros (or NaN)
+        sum *= f;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) acc[e] *= f;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          if (!there[k]) continue;
-          const float w = ml[k].x == -INFINITY ? 1.f : mv::fast_exp2(ml[k].x - top);  // nothing seen: zeros (or NaN)
+          const float w = ml[k].x == -INFINITY ? 1.f : mv::fast_exp2(ml[k].x - now);
           sum = fmaf(w, ml[k].y, sum);
 #pragma unroll
           for (int e = 0; e < VEC; ++e) acc[e] = fmaf(w, y[k][e], acc[e]);
         }
+        top = now;
       }
+      if (per > 1) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) so[warp][lane * VEC + e] = acc[e];
-      if (lane == 0) ssum[warp] = sum;
-      __syncthreads();
-      if (tid < D / 2) {
-        const float total = (ssum[0] + ssum[1]) + (ssum[2] + ssum[3]);
-        const float inv = total == 0.f ? 0.f : 1.f / total;
-        const float x0 = (so[0][2 * tid] + so[1][2 * tid]) + (so[2][2 * tid] + so[3][2 * tid]);
-        const float x1 = (so[0][2 * tid + 1] + so[1][2 * tid + 1]) + (so[2][2 * tid + 1] + so[3][2 * tid + 1]);
-        reinterpret_cast<uint32_t*>(a.out + (int64_t(own.y + v / a.G) * a.Hq + head * a.G + v % a.G) * D)[tid] = mv::pack_bf16(x0 * inv, x1 * inv);
+        for (int e = 0; e < VEC; ++e) so[warp][lane * VEC + e] = acc[e];
+        if (lane == 0) {
+          ssum[warp] = sum;
+          stop[warp] = top;
+        }
+        __syncthreads();
+        float all = -INFINITY;
+        for (int k = 0; k < per; ++k) all = fmaxf(all, stop[warp - sub + k]);
+        sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+        for (int k = 0; k < per; ++k) {
+          const int o = warp - sub + k;
+          const float w = stop[o] == -INFINITY ? 1.f : mv::fast_exp2(stop[o] - all);
+          sum = fmaf(w, ssum[o], sum);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) acc[e] = fmaf(w, so[o][lane * VEC + e], acc[e]);
+        }
+        __syncthreads();
       }
-      __syncthreads();
+      if (sub == 0 && v < n_qv) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        uint32_t* const out = reinterpret_cast<uint32_t*>(a.out + (int64_t(own.y + v / a.G) * a.Hq + head * a.G + v % a.G) * D + lane * VEC);
+        if (VEC == 4) *reinterpret_cast<uint2*>(out) = make_uint2(mv::pack_bf16(acc[0] * inv, acc[1] * inv), mv::pack_bf16(acc[VEC - 2] * inv, acc[VEC - 1] * inv));
+        else *out = mv::pack_bf16(acc[0] * inv, acc[1] * inv);
+      }
     }
   }
   // groups that have rows but no entries see nothing: zeros
-  const int n_groups = max(0, min(__ldcg(a.t.counts + 1), a.t.max_groups));
+  const int n_groups = max(0, min(counted, a.t.max_groups));
   for (int g = c; g < n_groups; g += gridDim.x)
     if (a.t.tile_off[g + 1] <= a.t.tile_off[g]) {
       const int r0 = max(0, a.t.row_off[g]), r1 = min(a.t.max_rows, a.t.row_off[g + 1]);
-      for (int64_t i = int64_t(r0) * a.Hq * D / 8 + blockIdx.y * blockDim.x + tid; i < int64_t(r1) * a.Hq * D / 8; i += int64_t(gridDim.y) * blockDim.x)
-        reinterpret_cast<uint4*>(a.out)[i] = make_uint4(0, 0, 0, 0);
+      for (int64_t i = int64_t(r0) * a.Hq * D / 8 + tid; i < int64_t(r1) * a.Hq * D / 8; i += blockDim.x) reinterpret_cast<uint4*>(a.out)[i] = make_uint4(0, 0, 0, 0);
     }
 }
 
@@ -460,7 +482,7 @@ bool launch(const Args& a, cudaStream_t st) {
   constexpr int smem = smem_bytes<D>();
   if (smem > 48 * 1024 && !mv::opt_in_smem(decode_blk_kernel<D, MT>, smem, opted)) return false;
   if (!launch_pdl(decode_blk_kernel<D, MT>, dim3(SHARES), NT, smem, a, st)) return false;
-  return launch_pdl(decode_blk_merge_kernel<D>, dim3(SHARES, MERGE_Y), 128, 0, a, st);
+  return launch_pdl(decode_blk_merge_kernel<D>, dim3(SHARES), MERGE_WARPS * 32, 0, a, st);
 }
 
 }  // namespace
@@ -504,11 +526,16 @@ extern "C" mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* t, const m
   a.Hkv = g->n_kv_heads;
   a.G = G;
   a.scale_log2 = mv::softmax_scale(g) * 1.4426950408889634f;
+  a.cost_shift = 0;
+  const int64_t tiles = (int64_t(t->max_entries) / mv::blk::TILE_ENTRIES + t->max_groups) * g->n_kv_heads;  // the most there may be
+  while (((tiles * mv::blk::COST_PER_TILE + int64_t(t->max_groups) * g->n_kv_heads * mv::blk::COST_PER_STREAM) >> a.cost_shift) >= (int64_t(1) << 31))
+    ++a.cost_shift;
+  if (a.cost_shift > 3) return MV_ERR_UNSUPPORTED;  // a tile costs at least 1
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   if (g->head_dim == 128) {
     const mv_status e = mv::decode_blk_tc(a, s);
     if (e != MV_OK) return e;
-    return launch_pdl(decode_blk_merge_kernel<128>, dim3(SHARES, MERGE_Y), 128, 0, a, s) ? MV_OK : MV_ERR_CUDA;
+    return launch_pdl(decode_blk_merge_kernel<128>, dim3(SHARES), MERGE_WARPS * 32, 0, a, s) ? MV_OK : MV_ERR_CUDA;
   }
   return launch<64, 4>(a, s) ? MV_OK : MV_ERR_CUDA;
 }

@@ -66,7 +66,7 @@ struct alignas(16) Entry {  // one page of a tile, as the softmax threads need i
 struct Meta {
   alignas(16) float minus_ref[MAXQV];  // minus the reference of a q-vector (+infinity: none yet; -infinity: no such q-vector); read four at a time
   float factor;                        // of a score
-  uint32_t largest;                    // magnitude among the segment's finite q-vectors (bf16 bits)
+  uint32_t largest[2];                 // magnitude among a segment's finite q-vectors (bf16 bits), segments in turn
   Entry entry[METAS][TILE_ENTRIES];
   uint2 seen[METAS];                   // q-vectors that see some page of the tile
   uint64_t full[RING], empty[RING], described[METAS], s_full[2], q_full, p_full[2], pv_done[2], drained[2];
@@ -138,15 +138,12 @@ static_assert(LO_SCALE == 16.f, "0x4c00 is 16 in half precision");
 // Eight boxes of 2 KB make a piece; one lane sends them all, with the rows in uniform registers.  Sending a box occupies its
 // warp for about 75 cycles: a warp that sent K and V of a tile could not keep up with the stream.
 template <bool IS_K>
-__device__ __forceinline__ void producer(const Cta& c, const CUtensorMap* map) {
+__device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk::Segment& s, bool more, const CUtensorMap* map) {
   const Args& a = *c.a;
   Meta* const meta = c.meta;
   const int lane = threadIdx.x & 31;
   const bool lead = mv::um::elect_one();
   const uint64_t policy = mv::l2_policy_evict_first();  // the cache is read once per call
-  mv::blk::Walk w;
-  w.begin(a, blockIdx.x);
-  mv::blk::Segment s{};
   int tile = 0;
   bool ok = true;
   // a window of 32 entries, one per lane
@@ -164,7 +161,7 @@ __device__ __forceinline__ void producer(const Cta& c, const CUtensorMap* map) {
   auto scale_at = [&](const int4& e) {
     return e.x >= 0 ? __ldcg(reinterpret_cast<const float2*>(a.scale) + int64_t(e.x) * a.Hkv + s.head) : make_float2(0.f, 1.f);
   };
-  while (ok && w.next(a, s, IS_K && lane == 0)) {
+  for (; ok && more; more = ok && w.next(a, s, IS_K && lane == 0)) {
     // what the softmax threads need of an entry
     auto describe = [&](const int4& e, const float2& sc) {
       Entry d{0, 0, 0.f, 127u << 23};
@@ -240,59 +237,60 @@ __device__ __forceinline__ void producer(const Cta& c, const CUtensorMap* map) {
 // q-vectors of the segment to the two K-major tiles (128-byte rows, 16-byte pieces XOR-swizzled with row % 8), eight threads per
 // q-vector; factor and references of the segment.  One power of two scales them all: what it costs a small q-vector in
 // relative precision is, in its scores, no more than the largest one's rounding.
-__device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s, int cols) {
+__device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s, int cols, int turn) {
   const Args& a = *c.a;
-  const int tid = threadIdx.x, x0 = tid >> 3, ch = tid & 7;
   constexpr int ROWS = SOFTMAX / 8, STEPS = MAXQV / ROWS;  // q-vectors at a time
-  uint4 raw[STEPS][2];
+  const int tid = threadIdx.x, x0 = tid >> 3, ch = tid & 7;
+  uint4* const raw = reinterpret_cast<uint4*>(c.smem + OFF_P);  // the q-vectors as they are, in the weight tiles
+  uint32_t most = 0;
+  uint4 in[STEPS][2];
 #pragma unroll
   for (int i = 0; i < STEPS; ++i) {
     const int x = i * ROWS + x0;
-    raw[i][0] = raw[i][1] = make_uint4(0, 0, 0, 0);
+    in[i][0] = in[i][1] = make_uint4(0, 0, 0, 0);
     if (x < s.n_qv) {
       const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t(s.row0 + x / a.G) * a.Hq + s.head * a.G + x % a.G) * D + ch * 16);
-      raw[i][0] = __ldcg(src);
-      raw[i][1] = __ldcg(src + 1);
+      in[i][0] = __ldcg(src);
+      in[i][1] = __ldcg(src + 1);
     }
   }
-  if (tid == 0) c.meta->largest = 0;
   if (tid < cols) c.meta->minus_ref[tid] = tid < s.n_qv ? INFINITY : -INFINITY;
-  (void)vote_all(true);
-  bool finite[STEPS];
-  uint32_t most = 0;
-#pragma unroll
-  for (int i = 0; i < STEPS; ++i) {
-    const uint4 x = raw[i][0], y = raw[i][1];
-    uint32_t m = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
-    m = __vmaxu2(m, __vmaxu2(__vmaxu2(y.x & 0x7fff7fffu, y.y & 0x7fff7fffu), __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu)));
-    m = max(m & 0xffffu, m >> 16);
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-    finite[i] = m < 0x7f80u;
-    if (finite[i]) most = max(most, m);
-  }
-  most = __reduce_max_sync(0xffffffffu, most);
-  if ((tid & 31) == 0) atomicMax(&c.meta->largest, most);
-  (void)vote_all(true);
-  // largest element into [128, 256)
-  const int e = max(-120, max(int(c.meta->largest >> 7), 1) - 127 - 7);
-  const float inv = mv::blk::exp2_int(-e);
-  if (tid == 0) c.meta->factor = mv::blk::exp2_int(e) * a.scale_log2;
 #pragma unroll
   for (int i = 0; i < STEPS; ++i) {
     const int x = i * ROWS + x0;
-    if (x >= cols) break;
-    const uint32_t w[8] = {raw[i][0].x, raw[i][0].y, raw[i][0].z, raw[i][0].w, raw[i][1].x, raw[i][1].y, raw[i][1].z, raw[i][1].w};
-    const float scale = finite[i] ? inv : __uint_as_float(0x7fc00000u);  // a q-vector that is not finite: NaN
+    if (x < cols) {
+      const uint4 u = in[i][0], v = in[i][1];
+      raw[x * 16 + ch * 2] = u;
+      raw[x * 16 + ch * 2 + 1] = v;
+      uint32_t m = __vmaxu2(__vmaxu2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), __vmaxu2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu));
+      m = __vmaxu2(m, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
+      m = max(m & 0xffffu, m >> 16);
+      if (m < 0x7f80u) most = max(most, m);  // (of a q-vector that is not finite, any part that is may count)
+    }
+  }
+  most = __reduce_max_sync(0xffffffffu, most);
+  if ((tid & 31) == 0) atomicMax(&c.meta->largest[turn], most);
+  (void)vote_all(true);
+  // largest element into [128, 256)
+  const int e = max(-120, max(int(c.meta->largest[turn] >> 7), 1) - 127 - 7);
+  const float inv = mv::blk::exp2_int(-e);
+  if (tid == 0) {
+    c.meta->factor = mv::blk::exp2_int(e) * a.scale_log2;
+    c.meta->largest[turn ^ 1] = 0;  // for the next segment
+  }
+#pragma unroll 1
+  for (int x = x0; x < cols; x += ROWS) {
+    const uint4 u = raw[x * 16 + ch * 2], v = raw[x * 16 + ch * 2 + 1];
+    const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
     uint32_t hi[4], lo[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       uint32_t h2[2], l2[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const uint32_t v = w[2 * k + j];
-        const float p = __uint_as_float(v << 16) * scale, q = __uint_as_float(v & 0xffff0000u) * scale;
-        h2[j] = mv::pack_e4m3x2(p, q);
+        const float p = __uint_as_float(w[2 * k + j] << 16) * inv, q = __uint_as_float(w[2 * k + j] & 0xffff0000u) * inv;
+        // infinities become NaN: inf * 0
+        h2[j] = mv::pack_e4m3x2(fmaf(p, 0.f, p), fmaf(q, 0.f, q));
         const float2 back = mv::unpack_e4m3x2(h2[j]);
         l2[j] = mv::pack_e4m3x2(p - back.x, q - back.y);
       }
@@ -569,20 +567,18 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
   return true;
 }
 
-__device__ __forceinline__ void softmax_warps(const Cta& c) {
-  mv::blk::Walk w;
-  w.begin(*c.a, blockIdx.x);
-  mv::blk::Segment s;
+__device__ __forceinline__ void softmax_warps(const Cta& c, mv::blk::Walk& w, mv::blk::Segment& s, bool more) {
   mv::blk::CutLog cuts;
   int tile = 0;  // tiles of the share so far: ring position, score buffer and phases follow from it
   bool ok = true;
-  while (ok && w.next(*c.a, s, false)) {
+  for (int turn = 0; more; turn ^= 1) {
     cuts.add(*c.a, s);
-    stage_q(c, s, (s.n_qv + 15) / 16 * 16);
+    stage_q(c, s, (s.n_qv + 15) / 16 * 16, turn);
     mv::fence_proxy_async();
     (void)vote_all(true);  // the factors are there for all
     if ((threadIdx.x & 31) == 0) mv::mbar_arrive(bar(&c.meta->q_full));
     ok = run_segment(c, s, tile);
+    more = ok && w.next(*c.a, s, false);
   }
   if (threadIdx.x == 0) cuts.store(*c.a, blockIdx.x);
 }
@@ -596,16 +592,13 @@ __device__ __forceinline__ void drain(const Cta& c, int which, bool lead) {
 }
 
 // S^T = K Q^T of every tile into score buffer tile & 1: K is the 128-row operand, values of Q then remainders
-__device__ __forceinline__ void score_issuer(const Cta& c) {
+__device__ __forceinline__ void score_issuer(const Cta& c, mv::blk::Walk& w, mv::blk::Segment& s, bool more) {
   Meta* const meta = c.meta;
   const bool lead = mv::um::elect_one();
   const uint64_t q_desc = mv::um::smem_desc(c.base + OFF_Q, 16, 1024);
-  mv::blk::Walk w;
-  w.begin(*c.a, blockIdx.x);
-  mv::blk::Segment s;
   int tile = 0, segment = 0;
   bool ok = true;
-  while (ok && w.next(*c.a, s, false)) {
+  for (; more; more = ok && w.next(*c.a, s, false)) {
     const int cols = (s.n_qv + 15) / 16 * 16;
     const Columns at(cols);
     const uint32_t idesc = mv::um::idesc_e4m3(128, cols, 0, 0);
@@ -638,15 +631,12 @@ __device__ __forceinline__ void score_issuer(const Cta& c) {
 }
 
 // O^T += V^T P^T of every tile: V is the 128-row operand, read across its rows (32 tokens per instruction)
-__device__ __forceinline__ void output_issuer(const Cta& c) {
+__device__ __forceinline__ void output_issuer(const Cta& c, mv::blk::Walk& w, mv::blk::Segment& s, bool more) {
   Meta* const meta = c.meta;
   const bool lead = mv::um::elect_one();
-  mv::blk::Walk w;
-  w.begin(*c.a, blockIdx.x);
-  mv::blk::Segment s;
   int tile = 0;
   bool ok = true;
-  while (ok && w.next(*c.a, s, false)) {
+  for (; more; more = ok && w.next(*c.a, s, false)) {
     const int cols = (s.n_qv + 15) / 16 * 16;
     const uint32_t o_t = meta->tmem + Columns(cols).o;
     const uint32_t idesc = mv::um::idesc_e4m3(128, 2 * cols, 1, 1);
@@ -687,6 +677,7 @@ __global__ void __launch_bounds__(NT, 2) decode_blk_tc_kernel(const Args a, cons
   }
   if (tid == 0) {
     meta->abort = 0;
+    meta->largest[0] = meta->largest[1] = 0;
     for (int i = 0; i < RING; ++i) {
       mv::mbar_init(bar(&meta->full[i]), 1);   // the producer's arrive (+ the bytes TMA reports)
       mv::mbar_init(bar(&meta->empty[i]), 1);  // one tcgen05.commit after the product that read the piece
@@ -713,11 +704,16 @@ __global__ void __launch_bounds__(NT, 2) decode_blk_tc_kernel(const Args a, cons
   mv::grid_dependency_wait();
   mv::grid_dependency_launch_dependents();
   Cta c{&a, smem, base, meta, a.t.counts + 4};
-  if (warp < SOFTMAX / 32) softmax_warps(c);
-  else if (warp == SOFTMAX / 32) producer<true>(c, &tm_k);
-  else if (warp == SOFTMAX / 32 + 1) producer<false>(c, &tm_v);
-  else if (warp == SOFTMAX / 32 + 2) score_issuer(c);
-  else output_issuer(c);
+  // every role walks the share's segments by itself; the beginning, common to all, is one piece of code that the warps fetch together
+  mv::blk::Walk w;
+  mv::blk::Segment s;
+  w.begin(a, blockIdx.x);
+  const bool more = w.next(a, s, tid == 0);
+  if (warp < SOFTMAX / 32) softmax_warps(c, w, s, more);
+  else if (warp == SOFTMAX / 32) producer<true>(c, w, s, more, &tm_k);
+  else if (warp == SOFTMAX / 32 + 1) producer<false>(c, w, s, more, &tm_v);
+  else if (warp == SOFTMAX / 32 + 2) score_issuer(c, w, s, more);
+  else output_issuer(c, w, s, more);
   mv::um::fence_before();
   __syncthreads();
   if (warp == 0) mv::um::tmem_dealloc(meta->tmem, 256);
