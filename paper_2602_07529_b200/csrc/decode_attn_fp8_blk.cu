@@ -342,13 +342,15 @@ __global__ void __launch_bounds__(NT) decode_blk_kernel(const Args a) {
   if (tid == 0) cuts.store(a, blockIdx.x);
 }
 
-// Merge of the cut streams: CTA c takes the stream that starts in share c and ends in a later one, if there is one.
+// Merge of the cut streams: CTA (c, y) takes the stream that starts in share c and ends in a later one, if there is one, and of
+// its q-vectors y, y + MERGE_Y, ...
 //   out = sum_i w_i O_i / sum_i w_i l_i,  w_i = 2^(m_i - max m) over the stream's parts i.
-// Bound by latency, two dependent round trips: the shares' records; references and parts.  Where a stream has fewer q-vectors than
-// the CTA has warps, several warps deal out the parts of one among themselves.
-constexpr int MERGE_WARPS = 16;
+// Bound by latency: two dependent round trips (the shares' records; references and parts) and the instructions' own arrival, which is why the
+// code is short and four loads in flight per warp have to do.  Where there are fewer q-vectors than warps, several warps
+// deal out the parts of one among themselves.
+constexpr int MERGE_WARPS = 8, MERGE_Y = 4, MERGE_LOADS = 4;
 template <int D>
-__global__ void __launch_bounds__(MERGE_WARPS * 32, 2) decode_blk_merge_kernel(const Args a) {
+__global__ void __launch_bounds__(MERGE_WARPS * 32) decode_blk_merge_kernel(const Args a) {
   constexpr int VEC = D / 32;  // elements of the head vector per lane
   __shared__ float so[MERGE_WARPS][D], ssum[MERGE_WARPS], stop[MERGE_WARPS];
   mv::grid_dependency_wait();
@@ -373,19 +375,20 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32, 2) decode_blk_merge_kernel(c
       return i == c || (i - c <= 32 ? ((parts >> (i - c - 1)) & 1) != 0 : __ldcg(&a.cuts[2 * i].stream) == own.x);
     };
     const int n_qv = own.z, head = own.x % a.Hkv;
+    const int mine = (n_qv - int(blockIdx.y) + MERGE_Y - 1) / MERGE_Y;  // q-vectors of this CTA
     int per = 1;  // warps of one q-vector
-    while (per < MERGE_WARPS && 2 * per * n_qv <= MERGE_WARPS && 4 * per <= c1 - c + 1) per *= 2;
+    while (per < MERGE_WARPS && 2 * per * mine <= MERGE_WARPS && 4 * per <= c1 - c + 1) per *= 2;
     const int sub = warp % per;
-    for (int v0 = 0; v0 < n_qv; v0 += MERGE_WARPS / per) {
-      const int v = v0 + warp / per;
+    for (int v0 = 0; v0 < mine; v0 += MERGE_WARPS / per) {
+      const int v = blockIdx.y + (v0 + warp / per) * MERGE_Y;
       // parts sub, sub + per, ... of the stream (part i: slot 2 c + 1, then slots 2 i of the shares behind), against the warp's own reference
       float top = -INFINITY, sum = 0.f, acc[VEC] = {};
-      for (int i0 = c + sub; i0 <= c1 && v < n_qv; i0 += per * 8) {
-        float2 ml[8];
-        float y[8][VEC];
-        bool there[8];
+      for (int i0 = c + sub; i0 <= c1 && v < n_qv; i0 += per * MERGE_LOADS) {
+        float2 ml[MERGE_LOADS];
+        float y[MERGE_LOADS][VEC];
+        bool there[MERGE_LOADS];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < MERGE_LOADS; ++k) {
           const int i = i0 + k * per;
           there[k] = i <= c1 && holds(i);
           ml[k] = make_float2(-INFINITY, 0.f);
@@ -406,13 +409,13 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32, 2) decode_blk_merge_kernel(c
         }
         float now = top;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) now = fmaxf(now, ml[k].x);
+        for (int k = 0; k < MERGE_LOADS; ++k) now = fmaxf(now, ml[k].x);
         const float f = top == -INFINITY ? 1.f : mv::fast_exp2(top - now);  // nothing seen so far: zeros (or NaN)
         sum *= f;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) acc[e] *= f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < MERGE_LOADS; ++k) {
           const float w = ml[k].x == -INFINITY ? 1.f : mv::fast_exp2(ml[k].x - now);
           sum = fmaf(w, ml[k].y, sum);
 #pragma unroll
@@ -455,7 +458,7 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32, 2) decode_blk_merge_kernel(c
   for (int g = c; g < n_groups; g += gridDim.x)
     if (a.t.tile_off[g + 1] <= a.t.tile_off[g]) {
       const int r0 = max(0, a.t.row_off[g]), r1 = min(a.t.max_rows, a.t.row_off[g + 1]);
-      for (int64_t i = int64_t(r0) * a.Hq * D / 8 + tid; i < int64_t(r1) * a.Hq * D / 8; i += blockDim.x) reinterpret_cast<uint4*>(a.out)[i] = make_uint4(0, 0, 0, 0);
+      for (int64_t i = int64_t(r0) * a.Hq * D / 8 + blockIdx.y * blockDim.x + tid; i < int64_t(r1) * a.Hq * D / 8; i += int64_t(gridDim.y) * blockDim.x) reinterpret_cast<uint4*>(a.out)[i] = make_uint4(0, 0, 0, 0);
     }
 }
 
@@ -482,7 +485,7 @@ bool launch(const Args& a, cudaStream_t st) {
   constexpr int smem = smem_bytes<D>();
   if (smem > 48 * 1024 && !mv::opt_in_smem(decode_blk_kernel<D, MT>, smem, opted)) return false;
   if (!launch_pdl(decode_blk_kernel<D, MT>, dim3(SHARES), NT, smem, a, st)) return false;
-  return launch_pdl(decode_blk_merge_kernel<D>, dim3(SHARES), MERGE_WARPS * 32, 0, a, st);
+  return launch_pdl(decode_blk_merge_kernel<D>, dim3(SHARES, MERGE_Y), MERGE_WARPS * 32, 0, a, st);
 }
 
 }  // namespace
@@ -535,7 +538,7 @@ extern "C" mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* t, const m
   if (g->head_dim == 128) {
     const mv_status e = mv::decode_blk_tc(a, s);
     if (e != MV_OK) return e;
-    return launch_pdl(decode_blk_merge_kernel<128>, dim3(SHARES), MERGE_WARPS * 32, 0, a, s) ? MV_OK : MV_ERR_CUDA;
+    return launch_pdl(decode_blk_merge_kernel<128>, dim3(SHARES, MERGE_Y), MERGE_WARPS * 32, 0, a, s) ? MV_OK : MV_ERR_CUDA;
   }
   return launch<64, 4>(a, s) ? MV_OK : MV_ERR_CUDA;
 }

@@ -328,7 +328,6 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
   };
   const Columns at(cols);
   const uint32_t lanes = meta->tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
-  float* const xch = reinterpret_cast<float*>(c.smem + OFF_P);          // exchange area: the weight tiles while no product reads them
   const int sw = token & 7;
   bool ok = true;
   uint64_t referenced = 0;  // q-vectors that have a reference (or saw scores that were not numbers)
@@ -347,7 +346,9 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
     const float fk = meta->factor * en.ks;
     const uint64_t fk2 = mv::pack_f32x2(fk, fk), ev2 = mv::pack_f32x2(evf, evf);
     const uint32_t s_t = lanes + ((tile & 1) ? at.s1 : 0);
-    unsigned char* const p_row = c.smem + OFF_P + (tile & 1) * PIECE + token * 128;
+    unsigned char* const p_tile = c.smem + OFF_P + (tile & 1) * PIECE;
+    unsigned char* const p_row = p_tile + token * 128;
+    float* const xch = reinterpret_cast<float*>(p_tile);  // exchange area until the weights stand
     bool valid = true;
     uint64_t see = ~0ull;
     if (!plain) {
@@ -424,18 +425,20 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
       if (GROUPS == 2 && (nb & 1)) columns(Width<8>{}, (nb - 1) * 16 + group * 8);
       return top;
     };
-    float sign = 1.f;
+    // q-vectors that see their first tokens need a reference; once one has it, it moves (all of them do) only where a weight passes
+    // the format's range
     const uint2 seen2 = meta->seen[tile % METAS];
     const uint64_t seen = (uint64_t(seen2.y) << 32) | seen2.x;
-    bool lift = (seen & ~referenced) != 0;  // some q-vector sees its first tokens
+    uint64_t todo = seen & ~referenced;
     referenced |= seen;
+    float sign = 1.f;
+    bool fresh = t == 0, moving = false;
     for (;;) {
-      if (lift) {
-        // ---- references move: the largest exponent of every q-vector over the tile's tokens
-        if (t > 0) ok = ok && warp_wait(c, bar(&meta->pv_done[(tile - 1) & 1]), ((tile - 1) >> 1) & 1);  // O and the exchange area are free
-        if (!vote_all(ok)) return false;
-        mv::um::fence_after();
+      if (todo) {
+        // ---- references: the largest exponent of these q-vectors over the tile's tokens
+        if (moving) (void)vote_all(true);  // the exchange area is the weight tile
         own([&](int b) {
+          if (((todo >> (b * 8)) & 0xff) == 0) return;
           uint32_t sc[8];
           mv::um::ld8(s_t + b * 8, sc);
           mv::um::wait_ld();
@@ -444,25 +447,27 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
           for (int j = 0; j < 8; ++j) {
             const int q = b * 8 + j;
             float y = fmaf(__uint_as_float(sc[j]), fk, evf);
-            if (!((see >> q) & 1) || q >= s.n_qv || y != y) y = -INFINITY;
+            if (!((see >> q) & 1) || y != y) y = -INFINITY;
             const int k = __float_as_int(y);
             const int m = __reduce_max_sync(0xffffffffu, k < 0 ? k ^ 0x7fffffff : k);  // ordered as the floats are
             if (lane == j) best = m;
           }
           if (lane < 8) xch[quarter * MAXQV + b * 8 + lane] = __int_as_float(best < 0 ? best ^ 0x7fffffff : best);
         });
-        (void)vote_all(true);
+        if (!vote_all(ok)) return false;
         float f = 1.f;
-        if (tid < cols) {
+        if (tid < s.n_qv && ((todo >> tid) & 1)) {
           const float m = fmaxf(fmaxf(xch[tid], xch[MAXQV + tid]), fmaxf(xch[2 * MAXQV + tid], xch[3 * MAXQV + tid]));
-          const float now = meta->minus_ref[tid], want = HEADROOM - m;
-          if (tid < s.n_qv && m > -INFINITY && want < now) {
+          const float now = meta->minus_ref[tid], want = HEADROOM - m;  // minus the references, old and new
+          if (m > -INFINITY && want < now) {
             f = mv::fast_exp2(want - now);  // 0 where there was none: O and the sums are zero (or NaN) there
             meta->minus_ref[tid] = want;
           }
-          xch[4 * MAXQV + tid] = f;
         }
+        if (tid < cols) xch[4 * MAXQV + tid] = f;
         if (vote_any(f != 1.f && f != 0.f)) {
+          ok = ok && warp_wait(c, bar(&meta->pv_done[(tile - 1) & 1]), ((tile - 1) >> 1) & 1);  // (some reference is older: t > 0)
+          mv::um::fence_after();
           mv::um::wait_st();
           own([&](int b) {
             const float* const f = xch + 4 * MAXQV + b * 8;
@@ -477,17 +482,22 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
             }
           });
           mv::um::wait_st();
+          if (!vote_all(ok)) return false;  // every thread has read the exchange area
         }
-        (void)vote_all(true);  // every thread has read the exchange area
       }
-      const float top = ok ? pass(sign, t == 0) : 0.f;
-      if (lift) break;
+      const float top = ok ? pass(sign, fresh) : 0.f;
+      fresh = false;
+      if (moving) break;
       if (sign < 0.f) {  // the weights taken back
         sign = 1.f;
-        lift = true;
+        todo = ~0ull;
+        moving = true;
         continue;
       }
+      mv::um::fence_before();
       if (!vote_any(top > TOP || !ok)) break;
+      if (!vote_all(ok)) return false;
+      todo = 0;
       sign = -1.f;
     }
     if (!plain && !__all_sync(0xffffffffu, valid)) {
@@ -510,6 +520,7 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
   if (!vote_all(ok)) return false;
   mv::um::fence_after();
   mv::um::wait_st();
+  float* const xch = reinterpret_cast<float*>(c.smem + OFF_P);
   own([&](int b) {
     // eight columns over 32 lanes by halving: after three steps a lane holds one column's sum over eight lanes
     uint32_t l[8];
