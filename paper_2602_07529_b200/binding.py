@@ -316,33 +316,41 @@ def mv_dag_decode_attn_fp8(plan: Plan, geom: _Geom, q_rot, k_pages8, v_pages8, k
 
 # ---- decode steps planned on the device, over the block-scaled 8-bit cache
 
-def _arr(t, name: str, dtype: str, least: int, device):
-    """Device pointer of a contiguous CUDA tensor of the given dtype with at least ``least`` elements on ``device``."""
-    if t is None or not t.is_cuda or t.dtype is not _dtype(dtype) or t.numel() < least or not t.is_contiguous() or t.device != device:
-        raise ValueError(f"{name}: a contiguous CUDA tensor of {dtype} with at least {least} elements on {device} is needed, got "
+class _Torch:
+    """The few names of torch that the checks below need, looked up once (the module itself loads without torch)."""
+    loaded = False
+
+    @classmethod
+    def load(cls):
+        import torch
+        cls.int32, cls.int64, cls.uint8, cls.float32, cls.bfloat16 = torch.int32, torch.int64, torch.uint8, torch.float32, torch.bfloat16
+        cls.device = staticmethod(torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device)
+        cls.stream = staticmethod(torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream")
+                                  else lambda i: torch.cuda.current_stream(i).cuda_stream)
+        cls.loaded = True
+
+
+def _torch():
+    if not _Torch.loaded:
+        _Torch.load()
+    return _Torch
+
+
+def _arr(t, name: str, dtype, least: int, index: int):
+    """Device pointer of a contiguous tensor of ``dtype`` with at least ``least`` elements on GPU ``index``."""
+    if t is None or t.dtype is not dtype or t.get_device() != index or t.numel() < least or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous tensor of {dtype} with at least {least} elements on cuda:{index} is needed, got "
                          + ("None" if t is None else f"{tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}"))
     return t.data_ptr()
 
 
-_DTYPES: dict = {}
-
-
-def _dtype(name: str):
-    got = _DTYPES.get(name)
-    if got is None:
-        import torch
-        got = _DTYPES[name] = getattr(torch, name)
-    return got
-
-
-def _launch_stream(device, stream):
-    """The raw stream of a launch on ``device``, which has to be the current one (the library launches there)."""
-    import torch
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"the arrays are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+def _launch_stream(index: int, stream):
+    """The raw stream of a launch on GPU ``index``, which has to be the current one (the library launches there)."""
+    if index != _Torch.device():
+        raise ValueError(f"the arrays are on cuda:{index}, the current device is cuda:{_Torch.device()}")
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device.index)
-    return _stream_ptr(stream)
+        return _Torch.stream(index)
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 class DeviceBatch:
@@ -352,11 +360,11 @@ class DeviceBatch:
     def __init__(self, n_req, node_off, node_len, node_new, parent_off, parent_idx, page_off, page_idx, num_pages, max_req_nodes,
                  vis_mode=0, pos_mode=0, page_size=16):
         n_nodes = node_len.numel()
-        self.device = node_off.device
+        self.index = node_off.get_device()
         sizes = (("node_off", node_off, int(n_req) + 1), ("node_len", node_len, n_nodes), ("node_new", node_new, n_nodes),
                  ("parent_off", parent_off, n_nodes + 1), ("parent_idx", parent_idx, 0), ("page_off", page_off, n_nodes + 1),
                  ("page_idx", page_idx, 0))
-        ptrs = [_arr(t, name, "int32", least, self.device) for name, t, least in sizes]
+        ptrs = [_arr(t, name, _torch().int32, least, max(0, self.index)) for name, t, least in sizes]
         self._keep = [t for _, t, _ in sizes]
         self.n_req = int(n_req)
         self.c_batch = _DagBatch(self.n_req, *ptrs, int(page_size), int(vis_mode), int(pos_mode))
@@ -369,19 +377,21 @@ class StepTables:
     Without the group arrays only positions and slots are built."""
 
     def __init__(self, pos_id, slot, counts, group_row_off=None, group_ent_off=None, group_tile_off=None, entries=None, rows_per_group=1):
-        self.device = counts.device
+        T = _torch()
+        self.index = counts.get_device()
+        i = max(0, self.index)
         self.max_rows = pos_id.numel()
         groups = 0 if group_row_off is None else group_row_off.numel() - 1
         ents = 0 if entries is None else entries.numel() // 4
-        p = [_arr(pos_id, "pos_id", "int32", 0, self.device), _arr(slot, "slot", "int64", self.max_rows, self.device)]
+        p = [_arr(pos_id, "pos_id", T.int32, 0, i), _arr(slot, "slot", T.int64, self.max_rows, i)]
         if groups > 0:
-            p += [_arr(t, name, "int32", groups + 1, self.device) for name, t in (("group_row_off", group_row_off),
-                                                                                 ("group_ent_off", group_ent_off), ("group_tile_off", group_tile_off))]
-            p.append(_arr(entries, "entries", "int32", 4, self.device))
+            p += [_arr(t, name, T.int32, groups + 1, i) for name, t in (("group_row_off", group_row_off), ("group_ent_off", group_ent_off),
+                                                                       ("group_tile_off", group_tile_off))]
+            p.append(_arr(entries, "entries", T.int32, 4, i))
         else:
             p += [None] * 4
             groups = ents = 0
-        p.append(_arr(counts, "counts", "int32", 8, self.device))
+        p.append(_arr(counts, "counts", T.int32, 8, i))
         self._keep = (pos_id, slot, counts, group_row_off, group_ent_off, group_tile_off, entries)
         self.c_tables = _StepTables(self.max_rows, groups, ents, int(rows_per_group), *p)
         self._ref = C.byref(self.c_tables)
@@ -393,31 +403,31 @@ def mv_step_tables_workspace_bytes(batch) -> int:
 
 def mv_step_tables_build(batch: DeviceBatch, tables: StepTables, workspace, stream=None):
     """Positions, slots and block tables of a step from its batch on the device; the outcome is in ``counts`` (asynchronous)."""
-    s = _launch_stream(tables.device, stream)
-    ws = _arr(workspace, "workspace", "uint8", 0, tables.device)
-    if batch.device != tables.device:
-        raise ValueError(f"the batch is on {batch.device}, the tables on {tables.device}")
+    i = tables.index
+    s = _launch_stream(i, stream)
+    ws = _arr(workspace, "workspace", _Torch.uint8, 0, i)
+    if batch.index != i:
+        raise ValueError(f"the batch is on cuda:{batch.index}, the tables on cuda:{i}")
     _check(lib.mv_step_tables_build(*batch._ref, tables._ref, ws, workspace.numel(), s), "mv_step_tables_build")
 
 
 def mv_step_tables_read_status(tables: StepTables, stream=None) -> int:
     """Status word of the step (0 = fine); synchronises the stream."""
     out = C.c_int32(-1)
-    _check(lib.mv_step_tables_read_status(tables._ref, _launch_stream(tables.device, stream), C.byref(out)), "mv_step_tables_read_status")
+    _check(lib.mv_step_tables_read_status(tables._ref, _launch_stream(tables.index, stream), C.byref(out)), "mv_step_tables_read_status")
     return int(out.value)
 
 
 def mv_rope_write_kv_fp8_blk(tables: StepTables, geom: _Geom, q, k, v, q_rot, k_rot, k_pages8, v_pages8, kv_scale, stream=None):
-    d, n = tables.device, tables.max_rows
-    s = _launch_stream(d, stream)
-    nq, nk = n * geom.n_q_heads * geom.head_dim, n * geom.n_kv_heads * geom.head_dim
-    block = geom.num_pages * geom.n_kv_heads
+    i, T = tables.index, _Torch
+    s = _launch_stream(i, stream)
+    hkv, d, blocks = geom.n_kv_heads, geom.head_dim, geom.num_pages * geom.n_kv_heads
+    nq, nk, pool = tables.max_rows * geom.n_q_heads * d, tables.max_rows * hkv * d, blocks * 16 * d
     _check(lib.mv_rope_write_kv_fp8_blk(
-        tables._ref, C.byref(geom), None if q is None else _arr(q, "q", "bfloat16", nq, d), _arr(k, "k", "bfloat16", nk, d),
-        _arr(v, "v", "bfloat16", nk, d), None if q_rot is None else _arr(q_rot, "q_rot", "bfloat16", nq, d),
-        None if k_rot is None else _arr(k_rot, "k_rot", "bfloat16", nk, d), _arr(k_pages8, "k_pages8", "uint8", block * 16 * geom.head_dim, d),
-        _arr(v_pages8, "v_pages8", "uint8", block * 16 * geom.head_dim, d), _arr(kv_scale, "kv_scale", "float32", block * 2, d), s),
-        "mv_rope_write_kv_fp8_blk")
+        tables._ref, C.byref(geom), None if q is None else _arr(q, "q", T.bfloat16, nq, i), _arr(k, "k", T.bfloat16, nk, i),
+        _arr(v, "v", T.bfloat16, nk, i), None if q_rot is None else _arr(q_rot, "q_rot", T.bfloat16, nq, i),
+        None if k_rot is None else _arr(k_rot, "k_rot", T.bfloat16, nk, i), _arr(k_pages8, "k_pages8", T.uint8, pool, i),
+        _arr(v_pages8, "v_pages8", T.uint8, pool, i), _arr(kv_scale, "kv_scale", T.float32, blocks * 2, i), s), "mv_rope_write_kv_fp8_blk")
 
 
 def mv_decode_fp8_blk_workspace_bytes(geom: _Geom) -> int:
@@ -425,13 +435,14 @@ def mv_decode_fp8_blk_workspace_bytes(geom: _Geom) -> int:
 
 
 def mv_dag_decode_attn_fp8_blk(tables: StepTables, geom: _Geom, q_rot, k_pages8, v_pages8, kv_scale, out, workspace, stream=None):
-    d, n = tables.device, tables.max_rows
-    s = _launch_stream(d, stream)
-    nq, block = n * geom.n_q_heads * geom.head_dim, geom.num_pages * geom.n_kv_heads
+    i, T = tables.index, _Torch
+    s = _launch_stream(i, stream)
+    d, blocks = geom.head_dim, geom.num_pages * geom.n_kv_heads
+    nq, pool = tables.max_rows * geom.n_q_heads * d, blocks * 16 * d
     _check(lib.mv_dag_decode_attn_fp8_blk(
-        tables._ref, C.byref(geom), _arr(q_rot, "q_rot", "bfloat16", nq, d), _arr(k_pages8, "k_pages8", "uint8", block * 16 * geom.head_dim, d),
-        _arr(v_pages8, "v_pages8", "uint8", block * 16 * geom.head_dim, d), _arr(kv_scale, "kv_scale", "float32", block * 2, d),
-        _arr(out, "out", "bfloat16", nq, d), _arr(workspace, "workspace", "uint8", 0, d), workspace.numel(), s), "mv_dag_decode_attn_fp8_blk")
+        tables._ref, C.byref(geom), _arr(q_rot, "q_rot", T.bfloat16, nq, i), _arr(k_pages8, "k_pages8", T.uint8, pool, i),
+        _arr(v_pages8, "v_pages8", T.uint8, pool, i), _arr(kv_scale, "kv_scale", T.float32, blocks * 2, i),
+        _arr(out, "out", T.bfloat16, nq, i), _arr(workspace, "workspace", T.uint8, 0, i), workspace.numel(), s), "mv_dag_decode_attn_fp8_blk")
 
 
 def mv_static_workspace_bytes() -> int:

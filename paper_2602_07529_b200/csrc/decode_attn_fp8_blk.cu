@@ -31,7 +31,7 @@ using mv::blk::MAXQV;
 using mv::blk::PS;
 using mv::blk::SHARES;
 
-constexpr int NT = 128, NW = NT / 32;
+constexpr int NT = 256, NW = NT / 32;
 
 __device__ __forceinline__ uint32_t half2_of_e4m3x2(uint32_t v) {
   uint32_t h;
@@ -64,7 +64,7 @@ constexpr int smem_bytes() { return MAXQV * (D + 8) * 2 + MAXQV * 4 + NW * 16 * 
 
 // MT blocks of 16 q-vectors at a time; a stream with more is walked again for the rest.
 template <int D, int MT>
-__global__ void __launch_bounds__(NT) decode_blk_kernel(const Args a) {
+__global__ void __launch_bounds__(NT, 2) decode_blk_kernel(const Args a) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int QS = D + 8;  // halves per q-vector in shared memory
   constexpr int OS = D + 4;
@@ -346,9 +346,9 @@ __global__ void __launch_bounds__(NT) decode_blk_kernel(const Args a) {
 // its q-vectors y, y + MERGE_Y, ...
 //   out = sum_i w_i O_i / sum_i w_i l_i,  w_i = 2^(m_i - max m) over the stream's parts i.
 // Bound by latency: two dependent round trips (the shares' records; references and parts) and the instructions' own arrival, which is why the
-// code is short and four loads in flight per warp have to do.  Where there are fewer q-vectors than warps, several warps
+// CTAs are few.  Where there are fewer q-vectors than warps, several warps
 // deal out the parts of one among themselves.
-constexpr int MERGE_WARPS = 8, MERGE_Y = 4, MERGE_LOADS = 4;
+constexpr int MERGE_WARPS = 8, MERGE_Y = 2, MERGE_LOADS = 8;
 template <int D>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) decode_blk_merge_kernel(const Args a) {
   constexpr int VEC = D / 32;  // elements of the head vector per lane
@@ -540,5 +540,5 @@ extern "C" mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* t, const m
     if (e != MV_OK) return e;
     return launch_pdl(decode_blk_merge_kernel<128>, dim3(SHARES, MERGE_Y), MERGE_WARPS * 32, 0, a, s) ? MV_OK : MV_ERR_CUDA;
   }
-  return launch<64, 4>(a, s) ? MV_OK : MV_ERR_CUDA;
+  return launch<64, 1>(a, s) ? MV_OK : MV_ERR_CUDA;
 }
