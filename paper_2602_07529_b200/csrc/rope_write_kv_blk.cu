@@ -137,7 +137,7 @@ __device__ __forceinline__ void write_block(const Args& a, int row0, int L, int6
 }
 
 template <int D, int TPC>
-__global__ void __launch_bounds__(NT) rope_write_kv_blk_kernel(const Args a, const __grid_constant__ mv::ThetaTable tt) {
+__global__ void __launch_bounds__(NT, 4) rope_write_kv_blk_kernel(const Args a, const __grid_constant__ mv::ThetaTable tt) {
   constexpr int HALF = D / 2, CH = HALF / 8;
   constexpr int ROWS = TPC + PS - 1;  // the chunk and what the last run may hold beyond it
   __shared__ __align__(16) float cs[ROWS][HALF], sn[ROWS][HALF];
@@ -201,35 +201,52 @@ __global__ void __launch_bounds__(NT) rope_write_kv_blk_kernel(const Args a, con
     if (x & 1) write_block<D, false>(a, t0 + i, len, sl >> 4, int(sl & 15), h, cs + i, sn + i);
     else write_block<D, true>(a, t0 + i, len, sl >> 4, int(sl & 15), h, cs + i, sn + i);
   }
-  // q: 16-byte pieces of both halves
+  // q: 16-byte pieces of both halves, UNITS of them per thread at a time so that their loads are in flight together
   if (a.q) {
-    const int here = min(TPC, a.max_rows - t0);
-    for (int x = tid; x < here * a.Hq * CH; x += NT) {
-      const int tl = x / (a.Hq * CH), u = x % (a.Hq * CH), h = u / CH, c = (u % CH) * 8;
-      if (s_slot[tl + 1] < 0) continue;
-      const int64_t at = (int64_t(t0 + tl) * a.Hq + h) * D + c;
-      const uint4 lo = *reinterpret_cast<const uint4*>(a.q + at), hi = *reinterpret_cast<const uint4*>(a.q + at + HALF);
-      const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w}, hw[4] = {hi.x, hi.y, hi.z, hi.w};
-      uint32_t ol[4], oh[4];
+    constexpr int UNITS = TPC == 1 ? 1 : 4;
+    const int here = min(TPC, a.max_rows - t0), units = here * a.Hq * CH;
+#pragma unroll 1
+    for (int x0 = tid; x0 < units; x0 += NT * UNITS) {
+      uint4 lo[UNITS], hi[UNITS];
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const float2 l = bf2(lw[n]), r = bf2(hw[n]);
-        const float2 cc = *reinterpret_cast<const float2*>(&cs[tl][c + 2 * n]), ss = *reinterpret_cast<const float2*>(&sn[tl][c + 2 * n]);
-        ol[n] = mv::pack_bf16(l.x * cc.x - r.x * ss.x, l.y * cc.y - r.y * ss.y);
-        oh[n] = mv::pack_bf16(r.x * cc.x + l.x * ss.x, r.y * cc.y + l.y * ss.y);
+      for (int i = 0; i < UNITS; ++i) {
+        const int x = x0 + i * NT;
+        if (x < units) {
+          const int64_t at = int64_t(t0) * a.Hq * D + int64_t(x / CH) * D + (x % CH) * 8;
+          lo[i] = *reinterpret_cast<const uint4*>(a.q + at);
+          hi[i] = *reinterpret_cast<const uint4*>(a.q + at + HALF);
+        }
       }
-      *reinterpret_cast<uint4*>(a.q_rot + at) = make_uint4(ol[0], ol[1], ol[2], ol[3]);
-      *reinterpret_cast<uint4*>(a.q_rot + at + HALF) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) {
+        const int x = x0 + i * NT;
+        if (x >= units) break;
+        const int tl = x / (a.Hq * CH), c = (x % CH) * 8;
+        if (s_slot[tl + 1] < 0) continue;
+        const int64_t at = int64_t(t0) * a.Hq * D + int64_t(x / CH) * D + c;
+        const uint32_t lw[4] = {lo[i].x, lo[i].y, lo[i].z, lo[i].w}, hw[4] = {hi[i].x, hi[i].y, hi[i].z, hi[i].w};
+        uint32_t ol[4], oh[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          const float2 l = bf2(lw[n]), r = bf2(hw[n]);
+          const float2 cc = *reinterpret_cast<const float2*>(&cs[tl][c + 2 * n]), ss = *reinterpret_cast<const float2*>(&sn[tl][c + 2 * n]);
+          ol[n] = mv::pack_bf16(l.x * cc.x - r.x * ss.x, l.y * cc.y - r.y * ss.y);
+          oh[n] = mv::pack_bf16(r.x * cc.x + l.x * ss.x, r.y * cc.y + l.y * ss.y);
+        }
+        *reinterpret_cast<uint4*>(a.q_rot + at) = make_uint4(ol[0], ol[1], ol[2], ol[3]);
+        *reinterpret_cast<uint4*>(a.q_rot + at + HALF) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
+      }
     }
   }
 }
 
+constexpr int MANY = 8;  // rows per CTA of a prompt
 template <int D>
 void launch(const Args& a, double rope_base, cudaStream_t st) {
   const mv::ThetaTable tt = mv::theta_table(rope_base, D);
   // few rows (a decode step): one per CTA spreads them over the SMs; many (a prompt): a page's worth per CTA
   if (a.max_rows < 2048) rope_write_kv_blk_kernel<D, 1><<<a.max_rows, NT, 0, st>>>(a, tt);
-  else rope_write_kv_blk_kernel<D, 16><<<(a.max_rows + 15) / 16, NT, 0, st>>>(a, tt);
+  else rope_write_kv_blk_kernel<D, MANY><<<(a.max_rows + MANY - 1) / MANY, NT, 0, st>>>(a, tt);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
