@@ -51,12 +51,13 @@ inline size_t part_ml_bytes() { return size_t(2) * SHARES * MAXQV * sizeof(float
 inline size_t workspace_bytes(int d) { return part_o_bytes(d) + part_ml_bytes() + ((2 * SHARES * sizeof(Cut) + 255) & ~size_t(255)); }
 
 // Costs in units of about 0.3 us of a share, fitted to clock readings of the tensor kernel: a tile takes 1.2 us with 16
-// q-vectors (as long as its bytes take to arrive) and 0.5 to 0.6 more for every further 16, a stream's set-up, first references and
-// epilogue another 4 us.  In a step of more than some hundred million tiles the unit grows by 2^shift, so that 32 bits
-// hold the sum: 64-bit arithmetic would lengthen the start of every launch, which is instruction fetches for the most part.
-constexpr int COST_PER_TILE = 10, COST_PER_STREAM = 18;  // the largest
+// q-vectors (as long as its bytes take to arrive) and 0.5 to 0.6 more for every further 16; a stream's set-up, first
+// references and epilogue, and what else delays a share that holds two, another 6 us.  In a step of more than some hundred
+// million tiles the unit grows by 2^shift, so that 32 bits hold the sum: 64-bit arithmetic would lengthen the start of every
+// launch, which is instruction fetches for the most part.
+constexpr int COST_PER_TILE = 10, COST_PER_STREAM = 26;  // the largest
 __device__ __forceinline__ uint32_t tile_cost(int blocks, int shift) { return max(1, (2 + 2 * blocks) >> shift); }
-__device__ __forceinline__ uint32_t stream_cost(int blocks, int shift) { return (10 + 2 * blocks) >> shift; }
+__device__ __forceinline__ uint32_t stream_cost(int blocks, int shift) { return (18 + 2 * blocks) >> shift; }
 
 // A run of tiles of one stream inside a share.
 struct Segment {
