@@ -155,8 +155,9 @@ namespace mv {
 // Builds a 2-D tiled tensor map over a row-major bf16 matrix [rows][cols] with a [box_rows][64] box and the
 // 128-byte shared-memory swizzle.  Host call, no CUDA context state; false if the driver entry is missing.
 bool make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
-// The same over a byte matrix [rows][128] (one 8-bit element per byte) with a [box_rows][128] box.
-bool make_tmap_u8_2d(CUtensorMap* map, const void* base, uint64_t rows, uint32_t box_rows);
+// The same over a byte matrix [rows][cols] (one 8-bit element per byte; 128 or 64 columns) with a [box_rows][cols] box and the
+// swizzle of `cols` bytes.
+bool make_tmap_u8_2d(CUtensorMap* map, const void* base, uint64_t rows, uint32_t box_rows, uint32_t cols = 128);
 
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(bar), "r"(count) : "memory");

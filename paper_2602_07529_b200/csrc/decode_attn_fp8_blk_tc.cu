@@ -1,6 +1,13 @@
-// Decode attention over the block-scaled 8-bit cache on the tensor cores with accumulators in tensor memory (head_dim 128).
-// The mathematics is that of the register kernel (decode_attn_fp8_blk.cu): weights 2^(s + e - m) with the exponent e of V's
-// block scale folded in, denominators corrected by 2^(-e).
+// Decode attention over the block-scaled 8-bit cache on the tensor cores, accumulators in tensor memory.
+// For the q-vectors x of a stream (rows of a group x query heads of one KV head) and the tokens j its entries name,
+//   s_xj = <q_x, K_j> * sK[page] * c,  c = softmax scale * log2 e        (log2 units)
+//   out_x = sum_j 2^(s_xj) sV[page] V_j / sum_j 2^(s_xj)
+// The scale of V is a power of two, 2^e, so it goes into the exponent: weights p_xj = 2^(s_xj + e_j - m_x) multiply the
+// stored bytes, and the denominator takes p_xj 2^(-e_j).  The reference m_x follows the largest s + e, which
+// keeps the weights of whatever dominates the NUMERATOR near one however much the pages' scales differ; with
+// exponents in [-60, 40] a token that matters to the denominator alone still gets a weight above 2^-126.
+// Block scale NaN: the scores of the rows that see the page become NaN; a row that does not see it multiplies
+// finite bytes by zero.
 //
 // Both products run with the CACHE as the 128-row operand, straight on the pool's bytes: S^T = K Q^T puts a tile's 128 tokens
 // on the 128 lanes of tensor memory and the q-vectors on its columns, O^T = V^T P^T the 128 elements of the head vector on the
@@ -19,10 +26,11 @@
 // The softmax warps keep the sums of a token (one per q-vector) in tensor memory as well, and walk the columns eight at a time
 // in a loop that is not unrolled: with the columns unrolled (per-thread arrays, a code path per number of columns) misses of
 // the SM's instruction cache cost three cycles per instruction.
-// A CTA is two groups of four softmax warps (a token has one thread in each; the groups take alternate blocks of columns), a
-// producer warp each for K and V and an issuer warp for either product; two CTAs per SM hide each other's hand-overs.  K
-// and V tiles (16 KB each) have two slots apiece, scores and weights two buffers, so that the products of one tile overlap the weights
-// of the next.
+// A CTA is four softmax warps (a thread per token), a producer warp each for K and V and an issuer warp for either product; two
+// CTAs per SM hide each other's hand-overs.  K and V tiles have two slots apiece, scores and weights two buffers (one score buffer
+// at 64 columns), so that the products of one tile overlap the weights of the next.
+// With head_dim 64 a cache row is 64 bytes: everything is the same but for the swizzle, and the second product takes V's 64 elements
+// twice to fill the 128 lanes.
 // Every wait is bounded; the softmax warps vote once per tile, and the vote carries a failed wait, so that they leave together.
 #include "blk_stream.cuh"
 #include "tmap_cache.h"
@@ -37,26 +45,15 @@ using mv::blk::PS;
 using mv::blk::SHARES;
 using mv::blk::TILE_ENTRIES;
 
-constexpr int D = 128;
 constexpr int TILE = 128;                 // tokens per tile
-constexpr int PIECE = TILE * D;           // 16 KB: K or V of a tile
 constexpr int RING = 4;                   // K in slots 0 and 2, V in slots 1 and 3
 constexpr int METAS = 4;                  // descriptions that may be live: K of tile j waits for the scores of tile j - 2, which wait for the weights of tile j - 4
-constexpr int OFF_P = RING * PIECE;       // weights of two tiles: [128 tokens][128 bytes] each, 128-byte swizzle
-constexpr int OFF_Q = OFF_P + 2 * PIECE;  // Q values [64][128], then Q remainders
-constexpr int Q_BYTES = MAXQV * D;
-constexpr int OFF_META = OFF_Q + 2 * Q_BYTES;
-constexpr int GROUPS = 1;                // groups of four softmax warps, each with every other block of eight columns
-constexpr int SOFTMAX = GROUPS * 128;
-constexpr int NT = SOFTMAX + 128;        // and four warps: K, V, first products, second products
+constexpr int P_TILE = TILE * 128;        // weights of a tile: [128 tokens][128 bytes], 128-byte swizzle
+constexpr int SOFTMAX = 128;
+constexpr int NT = SOFTMAX + 128;         // and four warps: K, V, first products, second products
 constexpr float TOP = 448.f;              // largest 8-bit float
 constexpr float HEADROOM = 5.f;           // a reference that moves puts the largest weight at 2^5
 constexpr float LO_SCALE = 16.f;
-
-template <int N>
-struct Width {
-  static constexpr int value = N;
-};
 
 struct alignas(16) Entry {  // one page of a tile, as the softmax threads need it
   uint32_t see_lo, see_hi;  // q-vectors that see it
@@ -75,8 +72,24 @@ struct Meta {
 };
 static_assert(sizeof(Meta) <= 1024, "meta area");
 static_assert(offsetof(Meta, minus_ref) % 16 == 0, "vector loads");
-constexpr int SMEM = OFF_META + 1024;
-static_assert(2 * (SMEM + 1024) <= 228 * 1024, "two CTAs per SM");
+
+// Shared memory.  A row of the cache is a token's D bytes, and so is a row of the tiles: 128 bytes with the 128-byte swizzle, or 64
+// bytes with the 64-byte swizzle.
+template <int D>
+struct Lay {
+  static constexpr int PIECE = TILE * D;           // K or V of a tile
+  static constexpr int P = RING * PIECE;           // weights of two tiles
+  static constexpr int Q = P + 2 * P_TILE;         // Q values [64][D], then Q remainders
+  static constexpr int Q_BYTES = MAXQV * D;
+  static constexpr int META = Q + 2 * Q_BYTES;
+  static constexpr int SMEM = META + 1024;
+  static_assert(2 * (SMEM + 1024) <= 228 * 1024, "two CTAs per SM");
+  // operand of the cache or of Q: groups of eight rows follow one another; where a row is 64 bytes, the first operand of the second product, which
+  // is 128 elements high, takes the 64 elements twice (distance 0 between its blocks)
+  static __device__ __forceinline__ uint64_t desc(uint32_t addr) {
+    return D == 128 ? mv::um::smem_desc(addr, 16, 1024) : mv::um::smem_desc_64b(addr, 0, 512);
+  }
+};
 
 __device__ __forceinline__ uint32_t bar(const void* p) { return mv::smem_u32(p); }
 
@@ -135,9 +148,9 @@ __device__ __forceinline__ void split_e4m3x4(float x0, float x1, float x2, float
 static_assert(LO_SCALE == 16.f, "0x4c00 is 16 in half precision");
 
 // ---- producer warps: one for K and the tiles' descriptions, one for V ---------------------------------------
-// Eight boxes of 2 KB make a piece; one lane sends them all, with the rows in uniform registers.  Sending a box occupies its
+// Eight boxes, a page each, make a piece; one lane sends them all, with the rows in uniform registers.  Sending a box occupies its
 // warp for about 75 cycles: a warp that sent K and V of a tile could not keep up with the stream.
-template <bool IS_K>
+template <int D, bool IS_K>
 __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk::Segment& s, bool more, const CUtensorMap* map) {
   const Args& a = *c.a;
   Meta* const meta = c.meta;
@@ -202,7 +215,7 @@ __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk
       const int piece = 2 * tile + (IS_K ? 0 : 1), slot = piece % RING;
       ok = warp_wait(c, bar(&meta->empty[slot]), ((piece / RING) & 1) ^ 1);
       if (!ok) break;
-      const uint32_t fb = bar(&meta->full[slot]), dst = c.base + slot * PIECE;
+      const uint32_t fb = bar(&meta->full[slot]), dst = c.base + slot * Lay<D>::PIECE;
       if (lead) mv::mbar_arrive_expect_tx(fb, uint32_t(__popc(present)) * (PS * D));
 #pragma unroll
       for (int j = 0; j < TILE_ENTRIES; ++j) {
@@ -234,24 +247,27 @@ __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk
 }
 
 // ---- softmax warps ---------------------------------------------------------------------------------------
-// q-vectors of the segment to the two K-major tiles (128-byte rows, 16-byte pieces XOR-swizzled with row % 8), eight threads per
+// q-vectors of the segment to the two K-major tiles (16-byte pieces XOR-swizzled as TMA does it for the cache), eight threads per
 // q-vector; factor and references of the segment.  One power of two scales them all: what it costs a small q-vector in
 // relative precision is, in its scores, no more than the largest one's rounding.
+template <int D>
 __device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s, int cols, int turn) {
   const Args& a = *c.a;
   constexpr int ROWS = SOFTMAX / 8, STEPS = MAXQV / ROWS;  // q-vectors at a time
+  constexpr int LOADS = D / 64;                            // 16-byte loads of a thread
   const int tid = threadIdx.x, x0 = tid >> 3, ch = tid & 7;
-  uint4* const raw = reinterpret_cast<uint4*>(c.smem + OFF_P);  // the q-vectors as they are, in the weight tiles
+  uint4* const raw = reinterpret_cast<uint4*>(c.smem + Lay<D>::P);  // the q-vectors as they are, in the weight tiles
   uint32_t most = 0;
-  uint4 in[STEPS][2];
+  uint4 in[STEPS][LOADS];
 #pragma unroll
   for (int i = 0; i < STEPS; ++i) {
     const int x = i * ROWS + x0;
-    in[i][0] = in[i][1] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) in[i][k] = make_uint4(0, 0, 0, 0);
     if (x < s.n_qv) {
-      const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t(s.row0 + x / a.G) * a.Hq + s.head * a.G + x % a.G) * D + ch * 16);
-      in[i][0] = __ldcg(src);
-      in[i][1] = __ldcg(src + 1);
+      const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t(s.row0 + x / a.G) * a.Hq + s.head * a.G + x % a.G) * D + ch * (D / 8));
+#pragma unroll
+      for (int k = 0; k < LOADS; ++k) in[i][k] = __ldcg(src + k);
     }
   }
   if (tid < cols) c.meta->minus_ref[tid] = tid < s.n_qv ? INFINITY : -INFINITY;
@@ -259,11 +275,13 @@ __device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s,
   for (int i = 0; i < STEPS; ++i) {
     const int x = i * ROWS + x0;
     if (x < cols) {
-      const uint4 u = in[i][0], v = in[i][1];
-      raw[x * 16 + ch * 2] = u;
-      raw[x * 16 + ch * 2 + 1] = v;
-      uint32_t m = __vmaxu2(__vmaxu2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), __vmaxu2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu));
-      m = __vmaxu2(m, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
+      uint32_t m = 0;
+#pragma unroll
+      for (int k = 0; k < LOADS; ++k) {
+        const uint4 u = in[i][k];
+        raw[(x * 8 + ch) * LOADS + k] = u;
+        m = __vmaxu2(m, __vmaxu2(__vmaxu2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), __vmaxu2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu)));
+      }
       m = max(m & 0xffffu, m >> 16);
       if (m < 0x7f80u) most = max(most, m);  // (of a q-vector that is not finite, any part that is may count)
     }
@@ -280,11 +298,14 @@ __device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s,
   }
 #pragma unroll 1
   for (int x = x0; x < cols; x += ROWS) {
-    const uint4 u = raw[x * 16 + ch * 2], v = raw[x * 16 + ch * 2 + 1];
-    const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-    uint32_t hi[4], lo[4];
+    uint32_t w[4 * LOADS], hi[2 * LOADS], lo[2 * LOADS];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < LOADS; ++k) {
+      const uint4 u = raw[(x * 8 + ch) * LOADS + k];
+      w[4 * k] = u.x; w[4 * k + 1] = u.y; w[4 * k + 2] = u.z; w[4 * k + 3] = u.w;
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * LOADS; ++k) {
       uint32_t h2[2], l2[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -297,9 +318,16 @@ __device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s,
       hi[k] = h2[0] | (h2[1] << 16);
       lo[k] = l2[0] | (l2[1] << 16);
     }
-    unsigned char* dst = c.smem + OFF_Q + x * 128 + ((ch ^ (x & 7)) << 4);
-    *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-    *reinterpret_cast<uint4*>(dst + Q_BYTES) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    unsigned char* const row = c.smem + Lay<D>::Q + x * D;
+    if constexpr (D == 128) {
+      unsigned char* const dst = row + ((ch ^ (x & 7)) << 4);
+      *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4*>(dst + Lay<D>::Q_BYTES) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    } else {
+      unsigned char* const dst = row + ((((ch >> 1) ^ ((x >> 1) & 3)) << 4) | ((ch & 1) << 3));
+      *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint2*>(dst + Lay<D>::Q_BYTES) = make_uint2(lo[0], lo[1]);
+    }
   }
 }
 
@@ -311,20 +339,15 @@ struct Columns {
 };
 
 // The tiles of one segment and its result.  False: a wait ran out.
+template <int D>
 __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment& s, int& tile) {
   const Args& a = *c.a;
   Meta* const meta = c.meta;
-  const int tid = threadIdx.x, token = tid & 127, group = tid >> 7, quarter = (tid >> 5) & 3, lane = tid & 31;
+  const int tid = threadIdx.x, token = tid, quarter = tid >> 5, lane = tid & 31;
   const int nb = (s.n_qv + 15) / 16, cols = nb * 16, n8 = cols / 8;
-  // The groups of warps take alternate blocks of sixteen columns; where their number is odd they share the last one.  own(f) calls f for
-  // every eight columns of this group.
-  auto own = [&](auto f) {
+  auto each_eight = [&](auto f) {  // f for every eight columns
 #pragma unroll 1
-    for (int u = group; u < nb; u += GROUPS) {
-      f(2 * u);
-      if (GROUPS == 1 || u + 1 < nb || (nb & 1) == 0) f(2 * u + 1);
-    }
-    if (group == 1 && (nb & 1)) f(2 * nb - 1);
+    for (int b = 0; b < n8; ++b) f(b);
   };
   const Columns at(cols);
   const uint32_t lanes = meta->tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
@@ -346,7 +369,7 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
     const float fk = meta->factor * en.ks;
     const uint64_t fk2 = mv::pack_f32x2(fk, fk), ev2 = mv::pack_f32x2(evf, evf);
     const uint32_t s_t = lanes + ((tile & 1) ? at.s1 : 0);
-    unsigned char* const p_tile = c.smem + OFF_P + (tile & 1) * PIECE;
+    unsigned char* const p_tile = c.smem + Lay<D>::P + (tile & 1) * P_TILE;
     unsigned char* const p_row = p_tile + token * 128;
     float* const xch = reinterpret_cast<float*>(p_tile);  // exchange area until the weights stand
     bool valid = true;
@@ -361,11 +384,12 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
       float top = 0.f;
       const uint64_t vinv2 = mv::pack_f32x2(sign * vinv, sign * vinv);
       mv::um::wait_st();  // the sums as the last pass left them
-      auto columns = [&](auto width, int col) {
-        constexpr int W = decltype(width)::value;
+#pragma unroll 1
+      for (int u = 0; u < nb; ++u) {
+        constexpr int W = 16;
+        const int col = u * W;
         uint32_t sc[W];
-        if constexpr (W == 16) mv::um::ld16(s_t + col, sc);
-        else mv::um::ld8(s_t + col, sc);
+        mv::um::ld16(s_t + col, sc);
         const float4* const mr = reinterpret_cast<const float4*>(meta->minus_ref + col);
         float p[W];
         mv::um::wait_ld();
@@ -392,23 +416,15 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
         for (int k = 0; k < W / 4; ++k) {
           split_e4m3x4(p[k * 4], p[k * 4 + 1], p[k * 4 + 2], p[k * 4 + 3], hi[k], lo[k]);
         }
-        unsigned char* const at_hi = p_row + (((col >> 4) ^ sw) << 4);
-        unsigned char* const at_lo = p_row + ((((col >> 4) + nb) ^ sw) << 4);
-        if constexpr (W == 16) {
-          *reinterpret_cast<uint4*>(at_hi) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4*>(at_lo) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-        } else {
-          *reinterpret_cast<uint2*>(at_hi + (col & 8)) = make_uint2(hi[0], hi[1]);
-          *reinterpret_cast<uint2*>(at_lo + (col & 8)) = make_uint2(lo[0], lo[1]);
-        }
+        *reinterpret_cast<uint4*>(p_row + ((u ^ sw) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(p_row + (((u + nb) ^ sw) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         // A weight past the format's range only says that the references have to move; what it adds here is taken back then, so it must
         // not overflow (capped, it still exceeds what the move leaves of it, and the sum loses nothing but a rounding).
         if (most > 0x1p60f)
 #pragma unroll
           for (int j = 0; j < W; ++j) p[j] = p[j] > 0x1p60f ? 0x1p60f : p[j];
         uint32_t l[W];
-        if constexpr (W == 16) mv::um::ld16(lanes + at.sums + col, l);
-        else mv::um::ld8(lanes + at.sums + col, l);
+        mv::um::ld16(lanes + at.sums + col, l);
         mv::um::wait_ld();
 #pragma unroll
         for (int j = 0; j < W; j += 2) {
@@ -417,12 +433,8 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
           l[j] = __float_as_uint(x);
           l[j + 1] = __float_as_uint(y);
         }
-        if constexpr (W == 16) mv::um::st16(lanes + at.sums + col, l);
-        else mv::um::st8(lanes + at.sums + col, l);
-      };
-#pragma unroll 1
-      for (int u = group; u < (GROUPS == 2 ? nb & ~1 : nb); u += GROUPS) columns(Width<16>{}, u * 16);
-      if (GROUPS == 2 && (nb & 1)) columns(Width<8>{}, (nb - 1) * 16 + group * 8);
+        mv::um::st16(lanes + at.sums + col, l);
+      }
       return top;
     };
     // q-vectors that see their first tokens need a reference; once one has it, it moves (all of them do) only where a weight passes
@@ -437,7 +449,7 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
       if (todo) {
         // ---- references: the largest exponent of these q-vectors over the tile's tokens
         if (moving) (void)vote_all(true);  // the exchange area is the weight tile
-        own([&](int b) {
+        each_eight([&](int b) {
           if (((todo >> (b * 8)) & 0xff) == 0) return;
           uint32_t sc[8];
           mv::um::ld8(s_t + b * 8, sc);
@@ -469,7 +481,7 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
           ok = ok && warp_wait(c, bar(&meta->pv_done[(tile - 1) & 1]), ((tile - 1) >> 1) & 1);  // (some reference is older: t > 0)
           mv::um::fence_after();
           mv::um::wait_st();
-          own([&](int b) {
+          each_eight([&](int b) {
             const float* const f = xch + 4 * MAXQV + b * 8;
 #pragma unroll 1
             for (int k = 0; k < 3; ++k) {  // O (values, remainders) and the sums, which lie side by side
@@ -505,9 +517,9 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
       const int vp = 2 * tile + 1, vslot = vp % RING;
       ok = ok && warp_wait(c, bar(&meta->full[vslot]), (vp / RING) & 1);
       if (!valid) {
-        uint4* const row = reinterpret_cast<uint4*>(c.smem + vslot * PIECE + token * 128);
+        uint4* const row = reinterpret_cast<uint4*>(c.smem + vslot * Lay<D>::PIECE + token * D);
 #pragma unroll
-        for (int k = 0; k < 8 / GROUPS; ++k) row[group * (8 / GROUPS) + k] = make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < D / 16; ++k) row[k] = make_uint4(0, 0, 0, 0);
       }
     }
     mv::fence_proxy_async();
@@ -515,13 +527,13 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
     __syncwarp();
     if (lane == 0 && ok) mv::mbar_arrive(bar(&meta->p_full[tile & 1]));
   }
-  // ---- the segment's result: sums over the tokens, then the head vectors (thread = element)
+  // ---- the segment's result: sums over the tokens, then the head vectors (thread = element; at 64 elements the upper half of the lanes holds them once more)
   ok = ok && warp_wait(c, bar(&meta->pv_done[(tile - 1) & 1]), ((tile - 1) >> 1) & 1);  // (products complete in order)
   if (!vote_all(ok)) return false;
   mv::um::fence_after();
   mv::um::wait_st();
-  float* const xch = reinterpret_cast<float*>(c.smem + OFF_P);
-  own([&](int b) {
+  float* const xch = reinterpret_cast<float*>(c.smem + Lay<D>::P);
+  each_eight([&](int b) {
     // eight columns over 32 lanes by halving: after three steps a lane holds one column's sum over eight lanes
     uint32_t l[8];
     mv::um::ld8(lanes + at.sums + b * 8, l);
@@ -549,7 +561,7 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
     if (s.slot >= 0) a.part_ml[s.slot * MAXQV + tid] = make_float2(-meta->minus_ref[tid], sum);  // no token seen: reference -infinity, sum 0
   }
   (void)vote_all(true);
-  own([&](int b) {
+  each_eight([&](int b) {
     uint32_t o0[8], o1[8];
     mv::um::ld8(lanes + at.o + b * 8, o0);
     mv::um::ld8(lanes + at.o + (n8 + b) * 8, o1);
@@ -562,7 +574,7 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float y = fmaf(__uint_as_float(o1[j]), 1.f / LO_SCALE, __uint_as_float(o0[j]));
-      if (j < left) {
+      if (j < left && (D == 128 || token < D)) {
         if (s.slot >= 0) part[j * D] = y;
         else *out = __float2bfloat16_rn(y * xch[4 * MAXQV + b * 8 + j]);
       }
@@ -578,17 +590,18 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
   return true;
 }
 
+template <int D>
 __device__ __forceinline__ void softmax_warps(const Cta& c, mv::blk::Walk& w, mv::blk::Segment& s, bool more) {
   mv::blk::CutLog cuts;
   int tile = 0;  // tiles of the share so far: ring position, score buffer and phases follow from it
   bool ok = true;
   for (int turn = 0; more; turn ^= 1) {
     cuts.add(*c.a, s);
-    stage_q(c, s, (s.n_qv + 15) / 16 * 16, turn);
+    stage_q<D>(c, s, (s.n_qv + 15) / 16 * 16, turn);
     mv::fence_proxy_async();
     (void)vote_all(true);  // the factors are there for all
     if ((threadIdx.x & 31) == 0) mv::mbar_arrive(bar(&c.meta->q_full));
-    ok = run_segment(c, s, tile);
+    ok = run_segment<D>(c, s, tile);
     more = ok && w.next(*c.a, s, false);
   }
   if (threadIdx.x == 0) cuts.store(*c.a, blockIdx.x);
@@ -603,10 +616,11 @@ __device__ __forceinline__ void drain(const Cta& c, int which, bool lead) {
 }
 
 // S^T = K Q^T of every tile into score buffer tile & 1: K is the 128-row operand, values of Q then remainders
+template <int D>
 __device__ __forceinline__ void score_issuer(const Cta& c, mv::blk::Walk& w, mv::blk::Segment& s, bool more) {
   Meta* const meta = c.meta;
   const bool lead = mv::um::elect_one();
-  const uint64_t q_desc = mv::um::smem_desc(c.base + OFF_Q, 16, 1024);
+  const uint64_t q_desc = Lay<D>::desc(c.base + Lay<D>::Q);
   int tile = 0, segment = 0;
   bool ok = true;
   for (; more; more = ok && w.next(*c.a, s, false)) {
@@ -624,14 +638,14 @@ __device__ __forceinline__ void score_issuer(const Cta& c, mv::blk::Walk& w, mv:
       if (!ok) break;
       mv::um::fence_after();
       if (lead) {
-        const uint64_t k_desc = mv::um::smem_desc(c.base + slot * PIECE, 16, 1024);
+        const uint64_t k_desc = Lay<D>::desc(c.base + slot * Lay<D>::PIECE);
         const uint32_t s_t = meta->tmem + ((tile & 1) ? at.s1 : 0);
         mv::um::mma8_ss<false>(s_t, k_desc, q_desc, idesc);
 #pragma unroll
         for (int k = 1; k < D / 32; ++k) mv::um::mma8_ss<true>(s_t, k_desc + uint32_t((k * 32) >> 4), q_desc + uint32_t((k * 32) >> 4), idesc);
 #pragma unroll
         for (int k = 0; k < D / 32; ++k)
-          mv::um::mma8_ss<true>(s_t, k_desc + uint32_t((k * 32) >> 4), q_desc + uint32_t((Q_BYTES + k * 32) >> 4), idesc);
+          mv::um::mma8_ss<true>(s_t, k_desc + uint32_t((k * 32) >> 4), q_desc + uint32_t((Lay<D>::Q_BYTES + k * 32) >> 4), idesc);
         mv::um::commit(bar(&meta->s_full[tile & 1]));
         mv::um::commit(bar(&meta->empty[slot]));
       }
@@ -642,6 +656,7 @@ __device__ __forceinline__ void score_issuer(const Cta& c, mv::blk::Walk& w, mv:
 }
 
 // O^T += V^T P^T of every tile: V is the 128-row operand, read across its rows (32 tokens per instruction)
+template <int D>
 __device__ __forceinline__ void output_issuer(const Cta& c, mv::blk::Walk& w, mv::blk::Segment& s, bool more) {
   Meta* const meta = c.meta;
   const bool lead = mv::um::elect_one();
@@ -658,12 +673,12 @@ __device__ __forceinline__ void output_issuer(const Cta& c, mv::blk::Walk& w, mv
       if (!ok) break;
       mv::um::fence_after();
       if (lead) {
-        const uint64_t v_desc = mv::um::smem_desc(c.base + vslot * PIECE, PIECE, 1024);
-        const uint64_t p_desc = mv::um::smem_desc(c.base + OFF_P + (tile & 1) * PIECE, PIECE, 1024);
+        const uint64_t v_desc = Lay<D>::desc(c.base + vslot * Lay<D>::PIECE);
+        const uint64_t p_desc = mv::um::smem_desc(c.base + Lay<D>::P + (tile & 1) * P_TILE, 16, 1024);
         if (t == 0) mv::um::mma8_ss<false>(o_t, v_desc, p_desc, idesc);
         else mv::um::mma8_ss<true>(o_t, v_desc, p_desc, idesc);
 #pragma unroll
-        for (int k = 1; k < TILE / 32; ++k) mv::um::mma8_ss<true>(o_t, v_desc + uint32_t((k * 4096) >> 4), p_desc + uint32_t((k * 4096) >> 4), idesc);
+        for (int k = 1; k < TILE / 32; ++k) mv::um::mma8_ss<true>(o_t, v_desc + uint32_t((k * 32 * D) >> 4), p_desc + uint32_t((k * 4096) >> 4), idesc);
         mv::um::commit(bar(&meta->pv_done[tile & 1]));
         mv::um::commit(bar(&meta->empty[vslot]));
       }
@@ -673,9 +688,10 @@ __device__ __forceinline__ void output_issuer(const Cta& c, mv::blk::Walk& w, mv
   if (!ok) drain(c, 1, lead);
 }
 
+template <int D>
 __global__ void __launch_bounds__(NT, 2) decode_blk_tc_kernel(const Args a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
   extern __shared__ __align__(1024) unsigned char smem[];
-  Meta* const meta = reinterpret_cast<Meta*>(smem + OFF_META);
+  Meta* const meta = reinterpret_cast<Meta*>(smem + Lay<D>::META);
   const int tid = threadIdx.x, warp = tid >> 5;
   const uint32_t base = mv::smem_u32(smem);
   if ((base & 1023u) != 0) {  // the swizzle pattern is anchored at 1024-byte boundaries
@@ -720,11 +736,11 @@ __global__ void __launch_bounds__(NT, 2) decode_blk_tc_kernel(const Args a, cons
   mv::blk::Segment s;
   w.begin(a, blockIdx.x);
   const bool more = w.next(a, s, tid == 0);
-  if (warp < SOFTMAX / 32) softmax_warps(c, w, s, more);
-  else if (warp == SOFTMAX / 32) producer<true>(c, w, s, more, &tm_k);
-  else if (warp == SOFTMAX / 32 + 1) producer<false>(c, w, s, more, &tm_v);
-  else if (warp == SOFTMAX / 32 + 2) score_issuer(c, w, s, more);
-  else output_issuer(c, w, s, more);
+  if (warp < SOFTMAX / 32) softmax_warps<D>(c, w, s, more);
+  else if (warp == SOFTMAX / 32) producer<D, true>(c, w, s, more, &tm_k);
+  else if (warp == SOFTMAX / 32 + 1) producer<D, false>(c, w, s, more, &tm_v);
+  else if (warp == SOFTMAX / 32 + 2) score_issuer<D>(c, w, s, more);
+  else output_issuer<D>(c, w, s, more);
   mv::um::fence_before();
   __syncthreads();
   if (warp == 0) mv::um::tmem_dealloc(meta->tmem, 256);
@@ -734,20 +750,17 @@ struct Maps {
   CUtensorMap k, v;
 };
 
-}  // namespace
-
-namespace mv {
-// Attention kernel of mv_dag_decode_attn_fp8_blk at head_dim 128 (the caller validated the arguments and launches the merge).
-mv_status decode_blk_tc(const blk::Args& a, cudaStream_t st) {
+template <int D>
+mv_status launch(const Args& a, cudaStream_t st) {
   static std::atomic<uint64_t> opted{0};  // per device
-  if (!opt_in_smem(decode_blk_tc_kernel, SMEM, opted)) return MV_ERR_CUDA;
-  static thread_local KeyedCache<Maps, 4> cache;
-  const int64_t rows = a.num_pages * a.Hkv * PS;  // 128-byte rows of a pool
-  const TmapKey key{current_device(), a.k8, a.v8, nullptr, rows, 9};
+  if (!mv::opt_in_smem(decode_blk_tc_kernel<D>, Lay<D>::SMEM, opted)) return MV_ERR_CUDA;
+  static thread_local mv::KeyedCache<Maps, 4> cache;
+  const int64_t rows = a.num_pages * a.Hkv * PS;  // rows of a pool: a token of a KV head
+  const mv::TmapKey key{mv::current_device(), a.k8, a.v8, nullptr, rows, 9};
   Maps* hit = cache.find(key);
   if (!hit) {
     hit = cache.claim(key);
-    if (!make_tmap_u8_2d(&hit->k, a.k8, uint64_t(rows), PS) || !make_tmap_u8_2d(&hit->v, a.v8, uint64_t(rows), PS)) {
+    if (!mv::make_tmap_u8_2d(&hit->k, a.k8, uint64_t(rows), PS, D) || !mv::make_tmap_u8_2d(&hit->v, a.v8, uint64_t(rows), PS, D)) {
       cache.drop();
       return MV_ERR_CUDA;
     }
@@ -755,19 +768,25 @@ mv_status decode_blk_tc(const blk::Args& a, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(SHARES, 1, 1);
   cfg.blockDim = dim3(NT, 1, 1);
-  cfg.dynamicSmemBytes = SMEM;
+  cfg.dynamicSmemBytes = Lay<D>::SMEM;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, decode_blk_tc_kernel, a, hit->k, hit->v);
-  g_launches++;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, decode_blk_tc_kernel<D>, a, hit->k, hit->v);
+  mv::g_launches++;
   if (e != cudaSuccess) {
     (void)cudaGetLastError();
     return MV_ERR_CUDA;
   }
   return MV_OK;
 }
+
+}  // namespace
+
+namespace mv {
+// Attention kernel of mv_dag_decode_attn_fp8_blk (the caller validated the arguments and launches the merge).
+mv_status decode_blk_tc(const blk::Args& a, int head_dim, cudaStream_t st) { return head_dim == 128 ? launch<128>(a, st) : launch<64>(a, st); }
 }  // namespace mv
