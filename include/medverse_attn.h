@@ -347,9 +347,14 @@ mv_status mv_rope_write_kv_fp8_blk(const mv_step_tables* tables, const mv_attn_g
  *   q_rot, out  device [max_rows][n_q_heads][head_dim] bf16;  pools, kv_scale as above
  *   workspace   device, 256-byte aligned, mv_decode_fp8_blk_workspace_bytes(geom) bytes (it does not depend on the step);
  *               scratch, not to be shared by calls that may overlap on the device
- * The same inputs give the same bits on every call.  dtype MV_BF16, head_dim 64 or 128, group size at most
- * 64 and rows_per_group * group size <= 64; all tensors 16-byte aligned.  Errors: MV_ERR_INVALID_ARG, MV_ERR_UNSUPPORTED,
- * MV_ERR_WORKSPACE, MV_ERR_CUDA. */
+ * out must not overlap q_rot.  A scale counts as the power of two that its exponent gives (its sign and mantissa are not looked at).
+ * Arithmetic: q as two 8-bit floats at one power of two per group and KV head (off by at most 2^-17 of the group's largest element),
+ * weights as two 8-bit floats (off by at most 2^-9 of the weight or 2^-19 of the row's largest), sums and softmax statistics
+ * in 32 bits.  The same inputs give the same bits on every call.
+ * dtype MV_BF16, head_dim 64 or 128, group size at most 64 and rows_per_group * group size <= 64; all tensors 16-byte aligned.
+ * Errors: MV_ERR_INVALID_ARG, MV_ERR_UNSUPPORTED (also a pool of 2^31 or more (page, KV head, token) rows, and capacities
+ * of max_entries / 8 + max_groups tiles whose product with n_kv_heads passes 1.7e9), MV_ERR_WORKSPACE, MV_ERR_CUDA.  A wait inside the
+ * kernel that runs out (seconds) ends the call with MV_ERR_TIMEOUT in counts[4]; `out` is then undefined. */
 size_t mv_decode_fp8_blk_workspace_bytes(const mv_attn_geom* geom);
 mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* tables, const mv_attn_geom* geom, const void* q_rot, const void* k_pages8,
                                      const void* v_pages8, const float* kv_scale, void* out, void* workspace,

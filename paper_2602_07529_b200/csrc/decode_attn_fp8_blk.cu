@@ -12,6 +12,7 @@ namespace {
 using bf16 = __nv_bfloat16;
 using mv::blk::Args;
 using mv::blk::MAXQV;
+using mv::blk::PS;
 using mv::blk::SHARES;
 
 // Merge of the cut streams:
@@ -238,6 +239,7 @@ extern "C" mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* t, const m
   if (g->dtype != MV_BF16) return MV_ERR_UNSUPPORTED;
   const int G = g->n_q_heads / g->n_kv_heads;
   if (G > MAXQV || t->rows_per_group < 1 || t->rows_per_group > MAXQV / G) return MV_ERR_UNSUPPORTED;
+  if (g->num_pages > INT32_MAX / PS / g->n_kv_heads) return MV_ERR_UNSUPPORTED;  // the rows of a pool are TMA coordinates
   if (t->max_rows == 0 || t->max_groups == 0) return MV_OK;
   if (!t->group_row_off || !t->group_ent_off || !t->group_tile_off || (t->max_entries > 0 && !t->entries)) return MV_ERR_INVALID_ARG;
   if (!q_rot || !k_pages8 || !v_pages8 || !kv_scale || !out) return MV_ERR_INVALID_ARG;

@@ -32,6 +32,8 @@
 // With head_dim 64 a cache row is 64 bytes: everything is the same but for the swizzle, and the second product takes V's 64 elements
 // twice to fill the 128 lanes.
 // Every wait is bounded; the softmax warps vote once per tile, and the vote carries a failed wait, so that they leave together.
+#include <algorithm>
+
 #include "blk_stream.cuh"
 #include "tmap_cache.h"
 #include "umma.cuh"
@@ -755,7 +757,7 @@ mv_status launch(const Args& a, cudaStream_t st) {
   static std::atomic<uint64_t> opted{0};  // per device
   if (!mv::opt_in_smem(decode_blk_tc_kernel<D>, Lay<D>::SMEM, opted)) return MV_ERR_CUDA;
   static thread_local mv::KeyedCache<Maps, 4> cache;
-  const int64_t rows = a.num_pages * a.Hkv * PS;  // rows of a pool: a token of a KV head
+  const int64_t rows = std::max<int64_t>(1, a.num_pages * a.Hkv * PS);  // rows of a pool: a token of a KV head (no pages: no entry is accepted, nothing is read)
   const mv::TmapKey key{mv::current_device(), a.k8, a.v8, nullptr, rows, 9};
   Maps* hit = cache.find(key);
   if (!hit) {

@@ -9,7 +9,7 @@ Tolerances, fixed before the first run:
            (cos, sin and two products: under 2^-21 of the pair's length).
   q_rot    bf16: 2^-8 of the value, plus the same.
   out      bf16 rounds by at most 2^-8 of the value.  Weights carry at most 2^-8 each (8-bit floats as value plus
-           remainder, or half precision), which moves an output by at most 2^-8 * A in the numerator, A = sum_j p_j |V_j| / sum_j p_j; scores
+           remainder), which moves an output by at most 2^-8 * A in the numerator, A = sum_j p_j |V_j| / sum_j p_j; scores
            are sums of 128 products in 32 bits, off by far less than 2^-12 in the exponent for the magnitudes drawn here, another 2^-12 A.  Small
            weights as 8-bit floats: remainders have a quantum of 2^-9 / 16, the largest weight is kept at 2^5 or more, so a
            weight is off by at most half a quantum, 2^-14 / 2^5 = 2^-19 of the largest: at most N * 2^-19 A's scale for N tokens.
@@ -432,6 +432,35 @@ def test_attention_many_requests(hq, hkv, d):
     rng = np.random.default_rng(3)
     reqs = [[([], int(rng.integers(1, 400)), 0)] + [([0], int(rng.integers(0, 60)), 1) for _ in range(int(rng.integers(1, 9)))] for _ in range(150)]
     _attend(_batch_of(reqs), hq, hkv, d, 23)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,requests,length,branches", [
+    (4, 1, 1, 60000, 1),    # one stream in every share
+    (2, 2, 1, 9000, 1),     # one q-vector per stream
+    (40, 8, 60, 1900, 3),   # more cut q-vectors than warps that join them, an odd number in each stream
+    (8, 8, 90, 700, 1),     # the same with one
+    (7, 1, 3, 20000, 9),    # 63 q-vectors in each of few streams
+])
+def test_attention_joins_cut_streams(hq, hkv, requests, length, branches, d):
+    reqs = [[([], length + 13 * r, 0)] + [([0], 5 * b, 1) for b in range(branches)] for r in range(requests)]
+    _attend(_batch_of(reqs), hq, hkv, d, 25, tokens=length + 13 * requests + 64)
+
+
+def test_attention_over_a_pool_without_pages():
+    """No page id is valid then: every row gets zeros, and the bad entry is reported."""
+    B, _ = _mods()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    t = {"pos_id": i32(0, 0), "slot": torch.full((2,), -1, dtype=torch.int64, device="cuda"), "counts": i32(2, 1, 1, 1, 0, 0, 0, 0),
+         "group_row_off": i32(0, 2), "group_ent_off": i32(0, 1), "group_tile_off": i32(0, 1), "entries": i32(0, 16, 3, 0).view(1, 4)}
+    tables = B.StepTables(**t, rows_per_group=16)
+    geom = B.make_geom(8, 2, 128, 0, "bf16")
+    k8, v8, sc = pools_of(1, 2, 128, 5)
+    q = torch.randn(2, 8, 128, device="cuda").bfloat16()
+    out = torch.full_like(q, 7.0)
+    ws = torch.empty(B.mv_decode_fp8_blk_workspace_bytes(geom), dtype=torch.uint8, device="cuda")
+    B.mv_dag_decode_attn_fp8_blk(tables, geom, q, k8, v8, sc, out, ws)
+    assert B.mv_step_tables_read_status(tables) == 1 and (out == 0).all()
 
 
 @pytest.mark.parametrize("d", [64, 128])

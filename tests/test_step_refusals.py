@@ -102,6 +102,8 @@ def test_attention_refuses():
         assert attend(tables(), g, good[:i] + [P + 8] + good[i + 1:]) == INVALID, i
     for ws, n in ((None, need), (P, need - 1), (P + 64, need)):
         assert attend(tables(), g, good, ws, n) == WORKSPACE
+    assert attend(tables(), B.make_geom(8, 2, 128, 2 ** 31 // 32, "bf16"), good) == UNSUPPORTED  # rows of the pool beyond 31 bits
+    assert attend(tables(max_entries=2 ** 31 - 1), B.make_geom(8, 8, 128, 100, "bf16"), good) == UNSUPPORTED
     assert attend(tables(max_rows=0), g, [None] * 5) == OK
     assert attend(tables(max_groups=0), g, [None] * 5) == OK
     assert B.lib.mv_decode_fp8_blk_workspace_bytes(C.byref(B.make_geom(8, 2, 96, 100, "bf16"))) == 0
