@@ -12,6 +12,11 @@
 //
 // The rows of a page form a run of consecutive rows; the CTA whose chunk holds the run's first row writes the whole block,
 // a warp per (run, KV head, K or V), so no two warps touch a block and no atomics are needed.
+//
+// Bound by memory for a prompt: 17K tokens, 32 query and 8 KV heads of 128, 420 MB in 76 us (5.5 TB/s, 84 % of the measured copy
+// rate).  Measured there: 4, 8, 16 rows per CTA 82.6, 78.0, 82.7 us; with 8 rows, registers for 3, 4, 5 CTAs per SM 78.0, 76.1, 93.2;
+// two pairs of q per thread at a time instead of four 77.9.  Bound by the launch for a decode step: 9.5 us a call from a host program,
+// 4 to 5 us in a graph.
 #include "common.cuh"
 #include "rope.cuh"
 #include "trace.h"
@@ -244,7 +249,7 @@ constexpr int MANY = 8;  // rows per CTA of a prompt
 template <int D>
 void launch(const Args& a, double rope_base, cudaStream_t st) {
   const mv::ThetaTable tt = mv::theta_table(rope_base, D);
-  // few rows (a decode step): one per CTA spreads them over the SMs; many (a prompt): a page's worth per CTA
+  // few rows (a decode step): one per CTA spreads them over the SMs; many (a prompt): MANY per CTA share the angles' staging
   if (a.max_rows < 2048) rope_write_kv_blk_kernel<D, 1><<<a.max_rows, NT, 0, st>>>(a, tt);
   else rope_write_kv_blk_kernel<D, MANY><<<(a.max_rows + MANY - 1) / MANY, NT, 0, st>>>(a, tt);
 }

@@ -6,6 +6,8 @@
 // one launch that does both.  Analysing twice costs a few microseconds of mostly idle SMs and saves storing the per-node results.
 // What bounds it is latency: launches, a few dependent loads, shared-memory sweeps over the request's nodes, and the arrival
 // of the instructions (one piece of code for both launches, loops not unrolled), not the bytes written.
+// Measured: one request 10.2 us (8.2 in a graph), 128 requests of 512 to 16K tokens and 2 to 8 branches 18.4 us, 512 layered ones 26 us (4.8 MB of
+// tables, 0.7 us at the memory's rate); with a kernel of its own for each launch 14, 20 and 30 us.
 //
 // The DAG mask needs no closure matrix.  For one group of at most 64 rows, a node's mask is the set of the group's rows
 // that see it: a sweep over the nodes from last to first hands every node's mask on to its parents (parents have smaller
