@@ -44,7 +44,6 @@
 #include <algorithm>
 
 #include "blk_stream.cuh"
-#include "tmap_cache.h"
 #include "umma.cuh"
 
 namespace {
@@ -757,25 +756,14 @@ __global__ void __launch_bounds__(NT, 2) decode_blk_tc_kernel(const Args a, cons
   if (warp == 0) mv::um::tmem_dealloc(meta->tmem, 256);
 }
 
-struct Maps {
-  CUtensorMap k, v;
-};
-
 template <int D>
 mv_status launch(const Args& a, cudaStream_t st) {
   static std::atomic<uint64_t> opted{0};  // per device
   if (!mv::opt_in_smem(decode_blk_tc_kernel<D>, Lay<D>::SMEM, opted)) return MV_ERR_CUDA;
-  static thread_local mv::KeyedCache<Maps, 4> cache;
-  const int64_t rows = std::max<int64_t>(1, a.num_pages * a.Hkv * PS);  // rows of a pool: a token of a KV head (no pages: no entry is accepted, nothing is read)
-  const mv::TmapKey key{mv::current_device(), a.k8, a.v8, nullptr, rows, 9};
-  Maps* hit = cache.find(key);
-  if (!hit) {
-    hit = cache.claim(key);
-    if (!mv::make_tmap_u8_2d(&hit->k, a.k8, uint64_t(rows), PS, D) || !mv::make_tmap_u8_2d(&hit->v, a.v8, uint64_t(rows), PS, D)) {
-      cache.drop();
-      return MV_ERR_CUDA;
-    }
-  }
+  // a pool's map: a row is a token of a KV head (no pages: no entry is accepted, nothing is read).  Made anew for every call, which does not show in its time.
+  const int64_t rows = std::max<int64_t>(1, a.num_pages * a.Hkv * PS);
+  CUtensorMap tm_k, tm_v;
+  if (!mv::make_tmap_u8_2d(&tm_k, a.k8, uint64_t(rows), PS, D) || !mv::make_tmap_u8_2d(&tm_v, a.v8, uint64_t(rows), PS, D)) return MV_ERR_CUDA;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(SHARES, 1, 1);
   cfg.blockDim = dim3(NT, 1, 1);
@@ -786,7 +774,7 @@ mv_status launch(const Args& a, cudaStream_t st) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, decode_blk_tc_kernel<D>, a, hit->k, hit->v);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, decode_blk_tc_kernel<D>, a, tm_k, tm_v);
   mv::g_launches++;
   if (e != cudaSuccess) {
     (void)cudaGetLastError();

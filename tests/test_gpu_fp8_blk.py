@@ -80,9 +80,9 @@ def check_tables(step, batch):
         keys = [(int(p), int(c)) for p, c in e[:, :2]]
         assert len(set(keys)) == len(keys)
         for i in range(ro[g], ro[g + 1]):
-            mine = {int(p): int(c) for (p, c), m in zip(keys, mask) if (int(m) >> (i - ro[g])) & 1}
+            mine = {int(p): int(c) for (p, c), m in zip(keys, mask) if (int(m) >> int(i - ro[g])) & 1}
             assert mine == seen[i][1]
-            assert sum(1 for m in mask if (int(m) >> (i - ro[g])) & 1) == len(mine)     # each page once per row
+            assert sum(1 for m in mask if (int(m) >> int(i - ro[g])) & 1) == len(mine)     # each page once per row
     return t
 
 
@@ -146,7 +146,7 @@ def _dag(seed, **kw):
 
 @pytest.mark.parametrize("vis", [0, 1])
 @pytest.mark.parametrize("pos", [0, 1])
-@pytest.mark.parametrize("seed,max_new,group", [(0, 1, 4), (1, 1, 1), (2, 7, 8), (3, 40, 16), (4, 100, 64), (5, 256, 4)])
+@pytest.mark.parametrize("seed,max_new,group", [(0, 1, 4), (1, 1, 1), (2, 7, 8), (3, 40, 16), (4, 100, 64), (5, 256, 4), (6, 40, 1), (7, 17, 2)])
 def test_tables_random_dags(vis, pos, seed, max_new, group):
     _, runtime = _mods()
     wl = _dag(seed, n_req=5, max_nodes=12, max_len=90, max_new=max_new, vis_mode=vis, pos_mode=pos)
