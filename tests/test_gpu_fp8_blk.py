@@ -477,6 +477,57 @@ def test_attention_scales_differ_from_page_to_page(d):
     _attend(batch, 8, 2, d, 31, pools=(k8, v8, sc))
 
 
+def bound64(q, k8, v8, scale, t, group):
+    """(row, out, bound) in float64, element by element, where one token may dominate a row and have values near zero itself: the
+    second term of the weights' rounding then belongs to the row's largest weight, not to A.  With w_j = p_j * scale of V:
+      2^-8 |out| (bf16) + (2^-8 + 2^-12) sum_j w_j |v_j|  +  2^-19 max_j w_j * sum_j |v_j|
+      + what q's rounding (2^-17 of the group's largest element) moves the scores: ds_j = 2^-17 max |q| sum |K_j| * sm_scale,
+        sum_j w_j |v_j| ds_j + (sum_j p_j ds_j) sum_j w_j |v_j|, and a tenth of it for the second order."""
+    d, hkv = q.shape[2], k8.shape[1]
+    ro, eo, ent, counts = (t[k].cpu() for k in ("group_row_off", "group_ent_off", "entries", "counts"))
+    kd = k8.view(torch.float8_e4m3fn).double() * scale[:, :, 0].double()[:, :, None, None]
+    vb, se = v8.view(torch.float8_e4m3fn).double(), scale[:, :, 1].double()
+    for g in range(int(counts[1])):
+        e = ent[int(eo[g]):int(eo[g + 1])].long()
+        r0, r1 = int(ro[g]), int(ro[g + 1])
+        qmax = q[r0:r1].double().abs().view(r1 - r0, hkv, group * d).amax((0, 2))
+        for r in range(r0, r1):
+            b = r - r0
+            sel = e[((e[:, 2 + b // 32] >> (b % 32)) & 1) > 0]
+            tok = (torch.arange(16) < sel[:, 1:2]).reshape(-1).nonzero()[:, 0].to(q.device)
+            if tok.numel() == 0:
+                continue
+            page = sel[:, 0].to(q.device)
+            kk, vv = (x[page].transpose(1, 2).reshape(-1, hkv, d)[tok] for x in (kd, vb))
+            sv = se[page][:, None, :].expand(-1, 16, -1).reshape(-1, hkv)[tok]
+            s = torch.einsum("hgd,nhd->hgn", q[r].double().view(hkv, group, d), kk) * d ** -0.5
+            ds = torch.einsum("h,nh->hn", qmax * 2.0 ** -17, kk.abs().sum(2)) * d ** -0.5
+            p = torch.softmax(s, -1)
+            w = p * sv.t()[:, None, :]
+            ref, a = torch.einsum("hgn,nhd->hgd", w, vv), torch.einsum("hgn,nhd->hgd", w, vv.abs())
+            moved = torch.einsum("hgn,hn,nhd->hgd", w, ds, vv.abs()) + a * torch.einsum("hgn,hn->hg", p, ds)[..., None]
+            tol = (2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2.0 ** -12) * a + 1.1 * moved
+                   + 2.0 ** -19 * w.amax(-1)[..., None] * vv.abs().sum(0)[:, None, :] + 1e-30)
+            yield r, ref.reshape(-1, d), tol.reshape(-1, d)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group,hkv", [(1, 4), (4, 2), (11, 5), (33, 2), (64, 3)])
+@pytest.mark.parametrize("spread", ["2^8", "all"])
+def test_attention_peaked_scores_over_spread_scales(d, group, hkv, spread):
+    """Scores of a dozen units, V's scales up to 2^16 apart, or anywhere a scale may be."""
+    seed = group * 2 + d
+    wl = _dag(seed, n_req=5, max_nodes=8, max_len=200, max_new=3, hq=hkv * group, hkv=hkv, d=d)
+    k8, v8, sc = pools_of(wl.batch.num_pages, hkv, d, seed, spread=8)
+    sc[..., 0] = 2.0 ** -4
+    if spread == "all":
+        sc[..., 1] = torch.exp2(torch.randint(-60, 41, sc[..., 1].shape, generator=torch.Generator().manual_seed(seed)).float()).cuda()
+    out, step, _, q, _, _ = _attend(wl.batch, hkv * group, hkv, d, seed, pools=(k8, v8, sc), check=False)
+    for r, ref, tol in bound64(q, k8, v8, sc, step.t, group):
+        over = (out[r].double() - ref).abs() > tol
+        assert not over.any(), (r, over.nonzero()[:4].tolist())
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_attention_large_scores_and_one_heavy_token(d):
     """A token whose weight is far above a long tail that together weighs as much, and scores that grow along the history
