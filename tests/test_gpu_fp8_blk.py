@@ -231,7 +231,7 @@ def test_tables_bad_contents_give_an_empty_step(what, status):
 # ------------------------------------------------------------------------------------------------ cache write
 
 def write64(batch_tabs, k, v, k8, v8, scale, base=10000.0):
-    """The write by its definition: (values of K, values of V, scales, tie) after it, from the pools before it; values in
+    """The write by its definition: (values of K and V, scales, slack, tie, slots that belong to the block's tokens) after it, from the pools before it; values in
     float64, unrounded for the new tokens and for stored tokens that moved."""
     pos, slot = batch_tabs
     pools = [p.cpu().view(torch.float8_e4m3fn).double().numpy() for p in (k8, v8)]
@@ -241,11 +241,13 @@ def write64(batch_tabs, k, v, k8, v8, scale, base=10000.0):
     pair = np.concatenate([pair, pair], -1)
     slack = [np.zeros_like(pools[0]), np.zeros_like(pools[1])]
     tie = np.zeros(sc.shape, bool)
+    held = np.zeros((sc.shape[0], 16), bool)
     order = {}
     for i, s in enumerate(slot):
         order.setdefault(int(s) // 16, []).append(i)
     for page, rows in order.items():
         off = int(slot[rows[0]]) % 16
+        held[page, :off + len(rows)] = True
         for w, (raw, x, top) in enumerate(((k, rot, 316.0), (v, v, 448.0))):
             for h in range(k.shape[1]):
                 amax = np.abs(raw[rows, h]).max()
@@ -267,12 +269,12 @@ def write64(batch_tabs, k, v, k8, v8, scale, base=10000.0):
                     o = int(slot[i]) % 16
                     pools[w][page, h, o] = x[i, h] / new if ok else 0.0
                     slack[w][page, h, o] = pair[i, h] * 2.0 ** -21 / new if w == 0 and ok else 0.0
-    return pools, sc, slack, tie
+    return pools, sc, slack, tie, held
 
 
 def check_write(state, tabs, before, k, v):
     k8, v8, sc = state
-    pools, want_sc, slack, tie = write64(tabs, k.cpu().double().numpy(), v.cpu().double().numpy(), *before)
+    pools, want_sc, slack, tie, held = write64(tabs, k.cpu().double().numpy(), v.cpu().double().numpy(), *before)
     got_sc = sc.cpu().double().numpy()
     same = (got_sc == want_sc) | (np.isnan(got_sc) & np.isnan(want_sc))
     assert (same | (tie & (got_sc == 2 * want_sc))).all()
@@ -281,7 +283,7 @@ def check_write(state, tabs, before, k, v):
         assert np.isfinite(got).all()
         lost = np.isnan(got_sc[..., w])
         factor = np.where(lost, 1.0, got_sc[..., w] / np.where(lost, 1.0, want_sc[..., w]))[..., None, None]   # a tie resolved upwards
-        ref = pools[w] / factor
+        ref = pools[w] / np.where(held[:, None, :, None], factor, 1.0)   # (slots behind the tokens stay as they were)
         tol = np.maximum(np.abs(ref) * 2.0 ** -4, 2.0 ** -10) + slack[w]
         err = np.abs(got - np.clip(ref, -448, 448))
         err[lost] = 0.0
