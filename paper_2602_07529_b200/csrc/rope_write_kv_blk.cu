@@ -13,7 +13,7 @@
 // The rows of a page form a run of consecutive rows; the CTA whose chunk holds the run's first row writes the whole block,
 // a warp per (run, KV head, K or V), so no two warps touch a block and no atomics are needed.
 //
-// Bound by memory for a prompt: 17K tokens, 32 query and 8 KV heads of 128, 420 MB in 76 us (5.5 TB/s, 84 % of the measured copy
+// Bound by memory for a prompt: 17K tokens, 32 query and 8 KV heads of 128, 420 MB in 77 us (5.5 TB/s, 83 % of the measured copy
 // rate).  Measured there: 4, 8, 16 rows per CTA 82.6, 78.0, 82.7 us; with 8 rows, registers for 3, 4, 5 CTAs per SM 78.0, 76.1, 93.2;
 // two pairs of q per thread at a time instead of four 77.9.  Bound by the launch for a decode step: 9.5 us a call from a host program,
 // 4 to 5 us in a graph.
