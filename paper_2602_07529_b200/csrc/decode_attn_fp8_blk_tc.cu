@@ -477,17 +477,19 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
           if (lane < 8) xch[quarter * MAXQV + b * 8 + lane] = __int_as_float(best < 0 ? best ^ 0x7fffffff : best);
         });
         if (!vote_all(ok)) return false;
+        // what O and the sums take: 0 is a factor like any other (a reference that moves by more than 126), and where there was no
+        // reference nothing has to move, they are zero (or NaN) there
         float f = 1.f;
         if (tid < s.n_qv && ((todo >> tid) & 1)) {
           const float m = fmaxf(fmaxf(xch[tid], xch[MAXQV + tid]), fmaxf(xch[2 * MAXQV + tid], xch[3 * MAXQV + tid]));
           const float now = meta->minus_ref[tid], want = HEADROOM - m;  // minus the references, old and new
           if (m > -INFINITY && want < now) {
-            f = mv::fast_exp2(want - now);  // 0 where there was none: O and the sums are zero (or NaN) there
+            if (now < INFINITY) f = mv::fast_exp2(want - now);
             meta->minus_ref[tid] = want;
           }
         }
         if (tid < cols) xch[4 * MAXQV + tid] = f;
-        if (vote_any(f != 1.f && f != 0.f)) {
+        if (vote_any(f != 1.f)) {
           ok = ok && warp_wait(c, bar(&meta->pv_done[(tile - 1) & 1]), ((tile - 1) >> 1) & 1);  // (some reference is older: t > 0)
           mv::um::fence_after();
           mv::um::wait_st();

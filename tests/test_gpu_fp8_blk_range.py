@@ -1,0 +1,160 @@
+"""Decode attention over the block-scaled 8-bit cache where its arithmetic is strained: scores that leap, scales far apart, weights far
+apart, magnitudes that differ inside a group; with many streams of several tiles each, so that a share holds tiles of which the later
+ones move what the first ones set.
+
+Bound of an element, before the first run (64-bit reference; p softmax weights, w_j = p_j * scale of V's block, v_j stored values):
+  2^-8 |out|                                     bf16 rounds by half a step
+  (2^-8 + 2^-12) sum_j w_j |v_j|                 a weight as two 8-bit floats, exp2 and the joins of partial results
+  2^-19 max_j w_j * sum_j |v_j|                  what a weight loses below the smallest 8-bit float
+  1.1 (sum_j w_j |v_j| ds_j + (sum_j p_j ds_j) sum_j w_j |v_j|)   scores off by ds_j, the tenth for the second order:
+      ds_j = sm_scale (2^-17 max |q| sum_d |K_jd| + 2^-20 sum_d |q_d K_jd|) + 2^-22 max_j |s_j|
+      (q as two 8-bit floats; 128 products summed in 32 bits; scores against a reference in 32 bits)
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2602_07529_b200 import synth
+from test_gpu_fp8_blk import _batch_of, _mods, pools_of
+
+pytestmark = pytest.mark.gpu
+
+
+def elementwise(q, k8, v8, scale, t, group, sm_scale, weight=2.0 ** -8 + 2.0 ** -12, floor=2.0 ** -19, own_q=False):
+    """(row, out, bound) of every row of the step.  own_q: q's rounding counts from the row's own largest element, else from its group's."""
+    d, hkv = q.shape[2], k8.shape[1]
+    ro, eo, ent, counts = (t[k].cpu() for k in ("group_row_off", "group_ent_off", "entries", "counts"))
+    kd = k8.view(torch.float8_e4m3fn).double() * scale[:, :, 0].double()[:, :, None, None]
+    vb, se = v8.view(torch.float8_e4m3fn).double(), scale[:, :, 1].double()
+    for g in range(int(counts[1])):
+        e = ent[int(eo[g]):int(eo[g + 1])].long()
+        r0, r1 = int(ro[g]), int(ro[g + 1])
+        qabs = q[r0:r1].double().abs().view(r1 - r0, hkv, group, d)
+        most = qabs.amax((0, 2, 3))[:, None].expand(hkv, group)
+        for r in range(r0, r1):
+            b = r - r0
+            sel = e[((e[:, 2 + b // 32] >> (b % 32)) & 1) > 0]
+            tok = (torch.arange(16) < sel[:, 1:2]).reshape(-1).nonzero()[:, 0].to(q.device)
+            page = sel[:, 0].to(q.device)
+            kk, vv = (x[page].transpose(1, 2).reshape(-1, hkv, d)[tok] for x in (kd, vb))
+            sv = se[page][:, None, :].expand(-1, 16, -1).reshape(-1, hkv)[tok]
+            qq = q[r].double().view(hkv, group, d)
+            s = torch.einsum("hgd,nhd->hgn", qq, kk) * sm_scale
+            qm = qabs[b].amax(-1) if own_q else most
+            ds = (torch.einsum("hg,nh->hgn", qm * 2.0 ** -17, kk.abs().sum(2)) + 2.0 ** -20 * torch.einsum("hgd,nhd->hgn", qq.abs(), kk.abs())) * sm_scale
+            ds = ds + 2.0 ** -22 * s.abs().amax(-1, keepdim=True)
+            p = torch.softmax(s, -1)
+            w = p * sv.t()[:, None, :]
+            va = vv.abs()
+            ref, a = torch.einsum("hgn,nhd->hgd", w, vv), torch.einsum("hgn,nhd->hgd", w, va)
+            moved = torch.einsum("hgn,nhd->hgd", w * ds, va) + a * (p * ds).sum(-1)[..., None]
+            tol = 2.0 ** -8 * ref.abs() + weight * a + 1.1 * moved + floor * w.amax(-1)[..., None] * va.sum(0)[:, None, :] + 1e-30
+            yield r, ref.reshape(-1, d), tol.reshape(-1, d)
+
+
+def attend(batch, hq, hkv, d, q, pools, sm_scale=0.0):
+    B, runtime = _mods()
+    step = runtime.StepOnDevice(batch, hq // hkv)
+    step.build()
+    geom = B.make_geom(hq, hkv, d, batch.num_pages, "bf16", sm_scale=sm_scale)
+    ws = torch.full((B.mv_decode_fp8_blk_workspace_bytes(geom),), 255, dtype=torch.uint8, device="cuda")
+    out = torch.full_like(q, 7.0)
+    B.mv_dag_decode_attn_fp8_blk(step.tables, geom, q, *pools, out, ws)
+    assert step.read_status() == 0
+    return out, step
+
+
+def check(batch, hq, hkv, d, q, pools, sm_scale=0.0, **kw):
+    out, step = attend(batch, hq, hkv, d, q, pools, sm_scale)
+    worst = 0.0
+    for r, ref, tol in elementwise(q, *pools, step.t, hq // hkv, sm_scale or d ** -0.5, **kw):
+        err = (out[r].double() - ref).abs()
+        assert not torch.isnan(err).any(), r
+        worst = max(worst, float((err / tol).max()))
+    assert worst <= 1.0, worst
+    return out, step
+
+
+def streams(n_req=40, prefix=2000, branches=2, seed=5):
+    """Streams that hold enough tiles for segments of many tiles: a prompt, and branches of a few tokens each with one new one."""
+    return _batch_of([[([], prefix + 3 * r, 0)] + [([0], 5 * b, 1) for b in range(branches)] for r in range(n_req)], seed)
+
+
+def of_prompt(batch, values):
+    """Per slot of the pool [pages, 16]: values[request][token] for the prompts' tokens, 0 elsewhere."""
+    x = np.zeros((batch.num_pages, 16), np.float32)
+    for r in range(batch.n_req):
+        v = int(batch.node_off[r])
+        n = int(batch.node_len[v])
+        t = np.arange(n)
+        x[batch.page_idx[batch.page_off[v] + t // 16], t % 16] = values(r, n)
+    return torch.from_numpy(x).cuda()
+
+
+def keyed(batch, hkv, d, col0):
+    """A cache whose keys have one element besides zeros, so that q = (1, 0, 0, ...) makes it the score; random V."""
+    k8, v8, sc = pools_of(batch.num_pages, hkv, d, 3)
+    k = torch.zeros(batch.num_pages, hkv, 16, d, device="cuda")
+    k[..., 0] = col0[:, None, :]
+    sc[..., 0] = 1.0
+    return k.to(torch.float8_e4m3fn).view(torch.uint8).contiguous(), v8, sc
+
+
+def unit_q(batch, hq, d):
+    q = torch.zeros(int(batch.node_new.sum()), hq, d, device="cuda").bfloat16()
+    q[..., 0] = 1.0
+    return q
+
+
+# (query heads, KV heads, branches): 2, 16, 32 and 64 q-vectors in a stream
+SHAPES = [(8, 8, 2), (32, 8, 4), (64, 8, 4), (64, 8, 8)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,branches", SHAPES)
+@pytest.mark.parametrize("leap", [60, 86, 88, 200])
+def test_one_score_leaps(hq, hkv, branches, d, leap):
+    """All scores are 0 but one, deep in the history: the answer is that token's V.  The references move by up to 288 powers of two."""
+    batch = streams(branches=branches)
+    col0 = of_prompt(batch, lambda r, n: np.where(np.arange(n) == 700 + 23 * r, 64.0, 0.0))
+    check(batch, hq, hkv, d, unit_q(batch, hq, d), keyed(batch, hkv, d, col0), sm_scale=leap / 64)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,branches", SHAPES)
+@pytest.mark.parametrize("leap,at", [(10, 900), (60, 900), (48, 330), (52, 330), (60, 330)])
+def test_one_score_leaps_behind_blocks_of_zeros(hq, hkv, branches, d, leap, at):
+    """The history begins with V = 0, whose blocks have the lowest scale: its exponent counts in the references, which move by 54 powers
+    of two where the zeros end (token 320), together with the score's leap or before it."""
+    batch = streams(branches=branches)
+    col0 = of_prompt(batch, lambda r, n: np.where(np.arange(n) == at + r, 64.0, 0.0))
+    k8, v8, sc = keyed(batch, hkv, d, col0)
+    for r in range(batch.n_req):
+        v = int(batch.node_off[r])
+        pages = torch.from_numpy(batch.page_idx[batch.page_off[v]:batch.page_off[v] + 20].astype(np.int64)).cuda()
+        v8[pages] = 0
+        sc[pages, :, 1] = 2.0 ** -60
+    check(batch, hq, hkv, d, unit_q(batch, hq, d), (k8, v8, sc), sm_scale=leap / 64)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,branches", SHAPES)
+@pytest.mark.parametrize("name", ["ramp up", "ramp down", "stairs", "late sink"])
+def test_references_move_along_the_history(hq, hkv, branches, d, name):
+    batch = streams(branches=branches)
+    fn = {"ramp up": lambda r, n: np.linspace(-200, 250, n), "ramp down": lambda r, n: np.linspace(250, -200, n),
+          "stairs": lambda r, n: 16.0 * (np.arange(n) // (128 + r)), "late sink": lambda r, n: np.where(np.arange(n) == n - 2, 30.0, (np.arange(n) * 37 % 64) / 32.0)}[name]
+    q = unit_q(batch, hq, d)
+    q[..., 0] *= torch.linspace(-1.0, 2.0, hq, device="cuda").bfloat16()[None]    # heads that see it rise, fall and stand still
+    check(batch, hq, hkv, d, q, keyed(batch, hkv, d, of_prompt(batch, fn)), sm_scale=0.5)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,branches", SHAPES)
+def test_scores_of_a_wide_spread(hq, hkv, branches, d):
+    """Random scores of about a dozen units, V's scales up to 2^16 apart: every few tiles something moves."""
+    batch = streams(branches=branches)
+    k8, v8, sc = pools_of(batch.num_pages, hkv, d, 11, spread=8)
+    sc[..., 0] = 2.0 ** -6
+    q = torch.randn(int(batch.node_new.sum()), hq, d, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").bfloat16()
+    check(batch, hq, hkv, d, q, (k8, v8, sc), sm_scale=1.0)
