@@ -468,7 +468,8 @@ extern "C" mv_status mv_step_tables_build(const mv_dag_batch* b, const mv_step_s
   a.blocks = blocks ? 1 : 0;
   static std::atomic<uint64_t> opted{0};  // per device
   const size_t smem = smem_bytes(s->max_req_nodes);
-  if (smem > 48 * 1024 && !mv::opt_in_smem(step_tables_kernel, int(smem_bytes(MV_STEP_MAX_REQ_NODES)), opted)) return MV_ERR_CUDA;
+  constexpr size_t kStatic = 1024;  // the kernel's static arrays (under a hundred bytes) count in the 48 KB too
+  if (smem + kStatic > 48 * 1024 && !mv::opt_in_smem(step_tables_kernel, int(smem_bytes(MV_STEP_MAX_REQ_NODES)), opted)) return MV_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(unsigned(b->n_req > 0 ? b->n_req : 1), 1, 1);

@@ -10,6 +10,10 @@ Bound of an element, before the first run (64-bit reference; p softmax weights, 
       ds_j = sm_scale (2^-17 max |q| sum_d |K_jd| + 2^-20 sum_d |q_d K_jd|) + 2^-22 max_j |s_j|
       (q as two 8-bit floats; 128 products summed in 32 bits; scores against a reference in 32 bits)
 """
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -18,6 +22,7 @@ from paper_2602_07529_b200 import synth
 from test_gpu_fp8_blk import _batch_of, _mods, pools_of
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def elementwise(q, k8, v8, scale, t, group, sm_scale, weight=2.0 ** -8 + 2.0 ** -12, floor=2.0 ** -19, own_q=False):
@@ -158,3 +163,19 @@ def test_scores_of_a_wide_spread(hq, hkv, branches, d):
     sc[..., 0] = 2.0 ** -6
     q = torch.randn(int(batch.node_new.sum()), hq, d, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").bfloat16()
     check(batch, hq, hkv, d, q, (k8, v8, sc), sm_scale=1.0)
+
+
+def test_tables_of_every_size_around_the_plain_shared_memory_limit():
+    """The first build of a process, for request sizes at which the kernel's shared memory passes what a launch gets without asking."""
+    code = """
+import sys
+sys.path[:0] = ["tests", "."]
+from test_gpu_fp8_blk import _batch_of, _mods, check_tables
+for n in (800, 815, 816, 817, 818):
+    batch = _batch_of([[([], 1, 0)] + [([v], 0, int(v == n - 2)) for v in range(n - 1)]])
+    step = _mods()[1].StepOnDevice(batch, 4)
+    step.build()
+    check_tables(step, batch)
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
