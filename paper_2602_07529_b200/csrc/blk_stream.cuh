@@ -42,6 +42,7 @@ struct Args {
   Tables t;
   int64_t num_pages;
   int Hq, Hkv, G;
+  int group_rows;      // MAXQV / G: the most rows of a group
   float scale_log2;    // softmax scale * log2 e
   int cost_shift;      // see tile_cost
 };
@@ -75,16 +76,23 @@ struct Walk {
   uint32_t per, per_tile, per_stream;     // costs of one of its streams (per: all of it), of a tile, of the set-up
   uint32_t base, x_end;                   // cost position of group g's first stream; end of the share
 
-  __device__ __forceinline__ void take_group(const Args& a, int row0, int row1, int ent0, int ent1, int n_tiles) {
+  // Group with these offsets.  False where they are not a group's: rows or entries outside the arrays, more q-vectors than a stream
+  // holds, or a number of tiles that does not follow from the entries.  Such a group counts as empty: everything behind this
+  // check stays inside the arrays whatever the tables hold.
+  __device__ __forceinline__ bool take_group(const Args& a, int row0, int row1, int ent0, int ent1, int n_tiles) {
+    const bool ents = ent0 >= 0 && ent1 >= ent0 && ent1 <= a.t.max_entries && n_tiles == int((uint32_t(ent1 - ent0) + TILE_ENTRIES - 1) / TILE_ENTRIES);
+    const bool rows = row0 >= 0 && row1 > row0 && row1 <= a.t.max_rows && row1 - row0 <= a.group_rows;
+    const bool sound = ents && (rows || n_tiles == 0);
     r0 = row0;
-    n_qv = (row1 - row0) * a.G;
+    n_qv = sound ? (row1 - row0) * a.G : 0;
     e0 = ent0;
     e1 = ent1;
-    tiles = n_tiles;
+    tiles = sound ? n_tiles : 0;
     const int blocks = max(1, min(MAXQV / 16, (n_qv + 15) / 16));
     per_tile = tile_cost(blocks, a.cost_shift);
     per_stream = stream_cost(blocks, a.cost_shift);
     per = tiles > 0 ? per_stream + per_tile * uint32_t(tiles) : 0;
+    return sound;
   }
   // Two passes over the groups, 32 at a time: the total cost, then the group that holds the share's first tile.  The loads of
   // a pass do not wait for anything (the arrays are as long as the capacities say), so a step of up to 32 groups costs one
@@ -94,6 +102,7 @@ struct Walk {
     share = c;
     const int counted = __ldcg(a.t.counts + 1);
     int row[2], ent[2], til[2];
+    bool sound = true;
     auto load = [&](int i) {
       const bool there = i < a.t.max_groups;
 #pragma unroll
@@ -104,7 +113,8 @@ struct Walk {
       }
     };
     auto cost_of = [&](int i) {
-      take_group(a, row[0], row[1], ent[0], ent[1], til[1] - til[0]);
+      const bool fine = take_group(a, row[0], row[1], ent[0], ent[1], int(uint32_t(til[1]) - uint32_t(til[0])));
+      sound = sound && (fine || i >= n_groups);
       return i < n_groups ? uint32_t(a.Hkv) * per : 0u;
     };
     load(lane);
@@ -117,6 +127,7 @@ struct Walk {
       if (i - lane >= n_groups) break;
       load(i);
     }
+    if (c == 0 && !sound) atomicExch(a.t.counts + 4, int(MV_ERR_INVALID_ARG));  // (its groups are skipped)
     const uint32_t total = __reduce_add_sync(0xffffffffu, sum);
     const uint32_t each = total / SHARES, more = total % SHARES;  // the first `more` shares hold one unit more
     const uint32_t x = each * c + min(uint32_t(c), more);
@@ -161,8 +172,8 @@ struct Walk {
     const uint32_t at = x - base;                 // the share starts at the first tile whose point is not before x
     tile = at > per_stream ? int((at - per_stream + per_tile - 1) / per_tile) : 0;
   }
-  // The next sound segment; false at the end of the share.
-  __device__ __forceinline__ bool next(const Args& a, Segment& s, bool report) {
+  // The next segment; false at the end of the share.
+  __device__ __forceinline__ bool next(const Args& a, Segment& s) {
     while (g < n_groups) {
       if (tile >= tiles) {
         tile = 0;
@@ -170,8 +181,8 @@ struct Walk {
         if (++head >= a.Hkv || tiles <= 0) {
           head = 0;
           if (++g < n_groups)
-            take_group(a, __ldcg(a.t.row_off + g), __ldcg(a.t.row_off + g + 1), __ldcg(a.t.ent_off + g), __ldcg(a.t.ent_off + g + 1),
-                       __ldcg(a.t.tile_off + g + 1) - __ldcg(a.t.tile_off + g));
+            (void)take_group(a, __ldcg(a.t.row_off + g), __ldcg(a.t.row_off + g + 1), __ldcg(a.t.ent_off + g), __ldcg(a.t.ent_off + g + 1),
+                             int(uint32_t(__ldcg(a.t.tile_off + g + 1)) - uint32_t(__ldcg(a.t.tile_off + g))));
         }
         continue;
       }
@@ -189,10 +200,7 @@ struct Walk {
       s.ends = end == tiles;
       s.slot = tile == 0 && s.ends ? -1 : 2 * share + (tile > 0 ? 0 : 1);
       tile = end;
-      if (r0 >= 0 && n_qv > 0 && n_qv <= MAXQV && r0 + n_qv / a.G <= a.t.max_rows && e0 >= 0 && e1 <= a.t.max_entries &&
-          s.n_ent > (s.n_tiles - 1) * TILE_ENTRIES)
-        return true;
-      if (report) atomicExch(a.t.counts + 4, int(MV_ERR_INVALID_ARG));  // rows or entries out of range: the segment is skipped
+      return true;
     }
     return false;
   }

@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) decode_blk_merge_kernel(cons
   // groups that have rows but no entries see nothing: zeros
   const int n_groups = max(0, min(counted, a.t.max_groups));
   for (int g = blockIdx.x; g < n_groups; g += gridDim.x)
-    if (a.t.tile_off[g + 1] <= a.t.tile_off[g]) {
+    if (a.t.tile_off[g + 1] == a.t.tile_off[g] && a.t.ent_off[g + 1] == a.t.ent_off[g]) {
       const int r0 = max(0, a.t.row_off[g]), r1 = min(a.t.max_rows, a.t.row_off[g + 1]);
       for (int64_t i = int64_t(r0) * a.Hq * D / 8 + tid; i < int64_t(r1) * a.Hq * D / 8; i += blockDim.x) reinterpret_cast<uint4*>(a.out)[i] = make_uint4(0, 0, 0, 0);
     }
@@ -263,6 +263,7 @@ extern "C" mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* t, const m
   a.Hq = g->n_q_heads;
   a.Hkv = g->n_kv_heads;
   a.G = G;
+  a.group_rows = MAXQV / G;
   a.scale_log2 = mv::softmax_scale(g) * 1.4426950408889634f;
   a.cost_shift = 0;
   const int64_t tiles = (int64_t(t->max_entries) / mv::blk::TILE_ENTRIES + t->max_groups) * g->n_kv_heads;  // the most there may be

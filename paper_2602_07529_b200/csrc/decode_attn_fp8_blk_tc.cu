@@ -184,7 +184,7 @@ __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk
   auto scale_at = [&](const int4& e) {
     return e.x >= 0 ? __ldcg(reinterpret_cast<const float2*>(a.scale) + int64_t(e.x) * a.Hkv + s.head) : make_float2(0.f, 1.f);
   };
-  for (; ok && more; more = ok && w.next(a, s, IS_K && lane == 0)) {
+  for (; ok && more; more = ok && w.next(a, s)) {
     // what the softmax threads need of an entry
     auto describe = [&](const int4& e, const float2& sc) {
       Entry d{0, 0, 0.f, 127u << 23};
@@ -614,7 +614,7 @@ __device__ __forceinline__ void softmax_warps(const Cta& c, mv::blk::Walk& w, mv
     (void)vote_all(true);  // the factors are there for all
     if ((threadIdx.x & 31) == 0) mv::mbar_arrive(bar(&c.meta->q_full));
     ok = run_segment<D>(c, s, tile);
-    more = ok && w.next(*c.a, s, false);
+    more = ok && w.next(*c.a, s);
   }
   if (threadIdx.x == 0) cuts.store(*c.a, blockIdx.x);
 }
@@ -635,7 +635,7 @@ __device__ __forceinline__ void score_issuer(const Cta& c, mv::blk::Walk& w, mv:
   const uint64_t q_desc = Lay<D>::desc(c.base + Lay<D>::Q);
   int tile = 0, segment = 0;
   bool ok = true;
-  for (; more; more = ok && w.next(*c.a, s, false)) {
+  for (; more; more = ok && w.next(*c.a, s)) {
     const int cols = (s.n_qv + 15) / 16 * 16;
     const Columns at(cols);
     const uint32_t idesc = mv::um::idesc_e4m3(128, cols, 0, 0);
@@ -674,7 +674,7 @@ __device__ __forceinline__ void output_issuer(const Cta& c, mv::blk::Walk& w, mv
   const bool lead = mv::um::elect_one();
   int tile = 0;
   bool ok = true;
-  for (; more; more = ok && w.next(*c.a, s, false)) {
+  for (; more; more = ok && w.next(*c.a, s)) {
     const int cols = (s.n_qv + 15) / 16 * 16;
     const uint32_t o_t = meta->tmem + Columns(cols).o;
     const uint32_t idesc = mv::um::idesc_e4m3(128, 2 * cols, 1, 1);
@@ -747,7 +747,7 @@ __global__ void __launch_bounds__(NT, 2) decode_blk_tc_kernel(const Args a, cons
   mv::blk::Walk w;
   mv::blk::Segment s;
   w.begin(a, blockIdx.x);
-  const bool more = w.next(a, s, tid == 0);
+  const bool more = w.next(a, s);
   if (warp < SOFTMAX / 32) softmax_warps<D>(c, w, s, more);
   else if (warp == SOFTMAX / 32) producer<D, true>(c, w, s, more, &tm_k);
   else if (warp == SOFTMAX / 32 + 1) producer<D, false>(c, w, s, more, &tm_v);

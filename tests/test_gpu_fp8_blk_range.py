@@ -179,3 +179,32 @@ for n in (800, 815, 816, 817, 818):
 """
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("what,at,value", [("group_tile_off", 2, 2 ** 29 + 5), ("group_tile_off", 2, -(2 ** 31)), ("group_tile_off", 2, 2), ("group_ent_off", 2, 5000), ("group_ent_off", 2, -7),
+                                           ("group_ent_off", 2, 2 ** 31 - 1), ("group_row_off", 2, 2 ** 31 - 1), ("group_row_off", 2, -(2 ** 31)), ("group_row_off", 2, 400)])
+def test_tables_of_the_callers_own_with_offsets_that_do_not_fit(what, at, value):
+    """Groups whose rows or entries leave the arrays, or whose tiles do not follow from their entries, are reported and skipped;
+    the groups around them keep their results."""
+    B, _ = _mods()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    t = {"pos_id": i32(*[0] * 9), "slot": torch.full((9,), -1, dtype=torch.int64, device="cuda"), "counts": i32(8, 4, 40, 7, 0, 0, 0, 0),
+         "group_row_off": i32(0, 2, 4, 6, 8, 8), "group_ent_off": i32(0, 9, 18, 30, 40, 40), "group_tile_off": i32(0, 2, 4, 6, 8, 8),
+         "entries": torch.stack([torch.arange(44) % 23, torch.full((44,), 16), torch.full((44,), 3), torch.zeros(44)], 1).int().cuda()}
+    d, geom = 128, B.make_geom(8, 2, 128, 23, "bf16")
+    pools = pools_of(23, 2, d, 3)
+    q = torch.randn(9, 8, d, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    ws = torch.zeros(B.mv_decode_fp8_blk_workspace_bytes(geom), dtype=torch.uint8, device="cuda")
+    outs = []
+    for spoilt in (False, True):
+        if spoilt:
+            t[what][at] = value
+        tables = B.StepTables(**t, rows_per_group=16)
+        out = torch.full_like(q, 7.0)
+        B.mv_dag_decode_attn_fp8_blk(tables, geom, q, *pools, out, ws)
+        assert B.mv_step_tables_read_status(tables) == (1 if spoilt else 0)
+        outs.append(out)
+    good, out = outs
+    assert not (good[:8] == 7.0).all(-1).any() and (good[8] == 7.0).all()
+    assert torch.equal(out[:2], good[:2]) and torch.equal(out[6:], good[6:])
+    assert (out[2:6] == 7.0).all()     # both groups that share the offset
