@@ -347,7 +347,8 @@ mv_status mv_rope_write_kv_fp8_blk(const mv_step_tables* tables, const mv_attn_g
  *   q_rot, out  device [max_rows][n_q_heads][head_dim] bf16;  pools, kv_scale as above
  *   workspace   device, 256-byte aligned, mv_decode_fp8_blk_workspace_bytes(geom) bytes (it does not depend on the step);
  *               scratch, not to be shared by calls that may overlap on the device
- * out must not overlap q_rot.  A scale counts as the power of two that its exponent gives (its sign and mantissa are not looked at).
+ * out must not overlap q_rot.  A scale counts as the power of two that its exponent gives (its sign and mantissa are not looked at);
+ * V's has to be at most 2^40, and below 2^-80 (a scale of zero too) counts as 2^-80.
  * Arithmetic: q as two 8-bit floats at one power of two per group and KV head (off by at most 2^-17 of the group's largest element),
  * weights as two 8-bit floats (off by at most 2^-9 of the weight or 2^-19 of the row's largest), sums and softmax statistics
  * in 32 bits.  The same inputs give the same bits on every call.

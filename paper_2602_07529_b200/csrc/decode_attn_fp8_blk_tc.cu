@@ -64,6 +64,10 @@ constexpr int NT = SOFTMAX + 128;         // and four warps: K, V, first product
 constexpr float TOP = 448.f;              // largest 8-bit float
 constexpr float HEADROOM = 5.f;           // a reference that moves puts the largest weight at 2^5
 constexpr float LO_SCALE = 16.f;
+constexpr float CAP = 0x1p20f;            // what a weight past TOP counts as until the references have moved
+// Least exponent of a scale of V, below what the cache write gives (2^-60): a scale of zero (a block nobody has quantised, or zeros) counts
+// as 2^-80.  Sums hold weight * 2^80 at most, below 2^124 for 2^23 tokens, and weights go down to 2^-126, which leaves 2^46 for the other end.
+constexpr int V_MIN = -80;
 
 struct alignas(16) Entry {  // one page of a tile, as the softmax threads need it
   uint32_t see_lo, see_hi;  // q-vectors that see it
@@ -205,7 +209,7 @@ __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk
         d.see_lo = uint32_t(see);
         d.see_hi = uint32_t(see >> 32);
         d.ks = ek == 255 || ev == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float(ek << 23);
-        d.vs = (ev == 255 ? 127u : ev) << 23 | (mask == all_rows && e.y == PS ? 256u : 0u) | uint32_t(e.y);
+        d.vs = (ev == 255 ? 127u : max(ev, uint32_t(127 + V_MIN))) << 23 | (mask == all_rows && e.y == PS ? 256u : 0u) | uint32_t(e.y);
       }
       return d;
     };
@@ -430,9 +434,9 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
         *reinterpret_cast<uint4*>(p_row + (((u + nb) ^ sw) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         // A weight past the format's range only says that the references have to move; what it adds here is taken back then, so it must
         // not overflow (capped, it still exceeds what the move leaves of it, and the sum loses nothing but a rounding).
-        if (most > 0x1p60f)
+        if (most > CAP)
 #pragma unroll
-          for (int j = 0; j < W; ++j) p[j] = p[j] > 0x1p60f ? 0x1p60f : p[j];
+          for (int j = 0; j < W; ++j) p[j] = p[j] > CAP ? CAP : p[j];
         uint32_t l[W];
         mv::um::ld16(lanes + at.sums + col, l);
         mv::um::wait_ld();

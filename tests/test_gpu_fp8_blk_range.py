@@ -208,3 +208,20 @@ def test_tables_of_the_callers_own_with_offsets_that_do_not_fit(what, at, value)
     assert not (good[:8] == 7.0).all(-1).any() and (good[8] == 7.0).all()
     assert torch.equal(out[:2], good[:2]) and torch.equal(out[6:], good[6:])
     assert (out[2:6] == 7.0).all()     # both groups that share the offset
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,branches", SHAPES)
+@pytest.mark.parametrize("pages", [3, 20, 1000])
+def test_scales_of_zero(hq, hkv, branches, d, pages):
+    """The first blocks of the history, or all of them, have scales of zero: they weigh like any other and their values are zero."""
+    batch = streams(branches=branches)
+    k8, v8, sc = pools_of(batch.num_pages, hkv, d, 17)
+    first = np.concatenate([batch.page_idx[batch.page_off[v]:min(batch.page_off[v] + pages, batch.page_off[v + 1])]
+                            for r in range(batch.n_req) for v in range(batch.node_off[r], batch.node_off[r + 1])])
+    first = torch.from_numpy(first.astype(np.int64)).cuda()
+    v8[first] = 0
+    sc[first] = 0.0
+    q = torch.randn(int(batch.node_new.sum()), hq, d, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").bfloat16()
+    out, _ = check(batch, hq, hkv, d, q, (k8, v8, sc))
+    assert pages < 1000 or (out == 0).all()
