@@ -17,18 +17,21 @@
 //   - Q is two K-major tiles of 8-bit floats, the rounded element and its rounded remainder at one power-of-two scale per
 //     q-vector: a bf16 element has eight significant bits, value plus remainder hold nine, so the split is exact
 //     for elements within 2^-9 of the largest (and off by at most 2^-17 of the largest below).
-//   - The weights are two tiles as well, value and 16 times the remainder, accumulated in columns of their own
-//     and joined at the end (O = O_hi + O_lo / 16): at least eight significant bits where a weight is within 2^-6 of the
-//     largest, down to a quantum of 2^-18 of the largest.  The factor 16 keeps long tails of small weights.
-//   - The reference exponent of a q-vector moves only when a weight would pass the format's largest value (448): every
+//   - The weights are three tiles of 8-bit floats with five exponent bits (the upper byte of a half-precision number): the weight in
+//     half precision cut to its upper byte, what is left of it rounded to one, and what is left then.  All have the same scale.  A
+//     weight is off by at most 1.5 * 2^-10 of itself (2^-11 in half precision, 2^-10 behind the third byte) or 2^-17, where the largest
+//     one stands at 2^12 or more: 2^-29 of it.  That far down because history is long: a sink that takes 97 % of a row leaves each of
+//     64K other tokens 2^-21 of its weight, and together they may be all of the result.
+//     Three and not two: a value with three mantissa bits and 16 times its remainder end at 2^-19 of the largest weight.
+//   - The reference exponent of a q-vector moves only when a weight would pass the format's largest value (57344): every
 //     thread looks at its own weights and one barrier votes, so the maximum over the tokens (a reduction across lanes) is taken only
 //     on a stream's first tile and in the rare tile that lifts it.
-// The softmax warps keep the sums of a token (one per q-vector) in tensor memory as well, and walk the columns eight at a time
-// in a loop that is not unrolled: with the columns unrolled (per-thread arrays, a code path per number of columns) misses of
+// The softmax warps keep the sums of a token (one per q-vector) in tensor memory as well, and walk the columns sixteen at a time (the
+// references and the results eight at a time) in a loop that is not unrolled: with the columns unrolled (per-thread arrays, a code path per number of columns) misses of
 // the SM's instruction cache cost three cycles per instruction.
 // A CTA is four softmax warps (a thread per token), a producer warp each for K and V and an issuer warp for either product; two
-// CTAs per SM hide each other's hand-overs.  K and V tiles have two slots apiece, scores and weights two buffers (one score buffer
-// at 64 columns), so that the products of one tile overlap the weights of the next.
+// CTAs per SM hide each other's hand-overs.  K and V tiles have two slots apiece (V one where the weights need the other), scores and
+// weights two buffers, so that the products of one tile overlap the weights of the next.
 // With head_dim 64 a cache row is 64 bytes: everything is the same but for the swizzle, and the second product takes V's 64 elements
 // twice to fill the 128 lanes.
 // Measured (cache not in the L2, a call with its merge): 64 requests of mixed length, 64 query over 8 KV heads, 2.1 GB of cache, 481 us
@@ -56,14 +59,19 @@ using mv::blk::SHARES;
 using mv::blk::TILE_ENTRIES;
 
 constexpr int TILE = 128;                 // tokens per tile
-constexpr int RING = 4;                   // K in slots 0 and 2, V in slots 1 and 3
+constexpr int RING = 4;                   // K in slots 0 and 2, V in slots 1 and 3 (see Slots)
 constexpr int METAS = 4;                  // descriptions that may be live: K of tile j waits for the scores of tile j - 2, which wait for the weights of tile j - 4
-constexpr int P_TILE = TILE * 128;        // weights of a tile: [128 tokens][128 bytes], 128-byte swizzle
+// Weights of a tile.  Up to 32 columns: [128 tokens][128 bytes], the three bytes of a weight `cols` apart, 128-byte swizzle, and one
+// product over 3 * cols columns whose thirds are joined at the end.  From 48 columns on: three tiles [128 tokens][64 bytes], 64-byte
+// swizzle, and three products that add up in the same columns.  Two tiles of weights either way; at head_dim 128 the wide ones take
+// V's second slot as well (with one tile of weights 64 columns wait for the product before: 128 mixed requests 483 instead of 440 us).
+// Narrow or wide: an instruction of the second product costs some 47 cycles however few its columns, so three times as many do not pay
+// up to 32 columns: 48 requests of 8 q-vectors 104 us against 144, 32 layered ones of up to 24 92 against 96, 128 mixed ones 440 against 468.
+constexpr int P_NARROW = TILE * 128, P_THIRD = TILE * 64, P_WIDE = 3 * P_THIRD;
 constexpr int SOFTMAX = 128;
 constexpr int NT = SOFTMAX + 128;         // and four warps: K, V, first products, second products
-constexpr float TOP = 448.f;              // largest 8-bit float
-constexpr float HEADROOM = 5.f;           // a reference that moves puts the largest weight at 2^5
-constexpr float LO_SCALE = 16.f;
+constexpr float TOP = 57344.f;            // largest 8-bit float with five exponent bits
+constexpr float HEADROOM = 12.f;          // a reference that moves puts the largest weight at 2^12
 constexpr float CAP = 0x1p20f;            // what a weight past TOP counts as until the references have moved
 // Least exponent of a scale of V, below what the cache write gives (2^-60): a scale of zero (a block nobody has quantised, or zeros) counts
 // as 2^-80.  Sums hold weight * 2^80 at most, below 2^124 for 2^23 tokens, and weights go down to 2^-126, which leaves 2^46 for the other end.
@@ -92,9 +100,12 @@ static_assert(offsetof(Meta, minus_ref) % 16 == 0, "vector loads");
 template <int D>
 struct Lay {
   static constexpr int PIECE = TILE * D;           // K or V of a tile
-  static constexpr int P = RING * PIECE;           // weights of two tiles
-  static constexpr int Q = P + 2 * P_TILE;         // Q values [64][D], then Q remainders
+  static constexpr int P = RING * PIECE;           // weights
+  static constexpr bool BORROWS = D == 128;        // V's second slot holds weights in segments of 48 and 64 columns
+  static constexpr int PW = BORROWS ? P - PIECE : P;
+  static constexpr int Q = PW + 2 * P_WIDE;        // Q values [64][D], then Q remainders
   static constexpr int Q_BYTES = MAXQV * D;
+  static_assert(P + 2 * P_NARROW <= Q && Q % 1024 == 0, "room for both kinds");
   static constexpr int META = Q + 2 * Q_BYTES;
   static constexpr int SMEM = META + 1024;
   static_assert(2 * (SMEM + 1024) <= 228 * 1024, "two CTAs per SM");
@@ -106,6 +117,24 @@ struct Lay {
 };
 
 __device__ __forceinline__ uint32_t bar(const void* p) { return mv::smem_u32(p); }
+__device__ __forceinline__ int columns_of(int n_qv) { return (n_qv + 15) / 16 * 16; }
+__device__ __forceinline__ bool in_thirds(int cols) { return cols <= 32; }
+
+// Slots of K (0 and 2) or V (1 and 3) in the order in which tiles take them: in turn, or the first one alone while the second holds
+// weights.  The tile after such a segment takes the first slot again, and with it waits for the segment's last product: the second is free then.
+struct Slots {
+  int first;
+  uint32_t second = 0, phase = 0;  // phase: bit per slot, parity of its next fill
+  __device__ __forceinline__ void begin(bool both) { second = both ? second : 0; }
+  __device__ __forceinline__ int slot() const { return first + 2 * int(second); }
+  __device__ __forceinline__ uint32_t parity() const { return (phase >> second) & 1; }
+  __device__ __forceinline__ void advance(bool both) {
+    phase ^= 1u << second;
+    second = both ? second ^ 1 : 0;
+  }
+};
+template <int D>
+__device__ __forceinline__ bool both_slots_of_v(int cols) { return in_thirds(cols) || !Lay<D>::BORROWS; }
 
 struct Cta {
   const Args* a;
@@ -144,22 +173,26 @@ __device__ __forceinline__ bool vote_all(bool p) {
   return r != 0;
 }
 
-// four floats -> four 8-bit floats each: values, and 16 times the remainders.  The values are unpacked from the packed word: with
-// the 16-bit halves unpacked first and packed afterwards, the code that ptxas 12.9 makes unpacks zeros.
-__device__ __forceinline__ void split_e4m3x4(float x0, float x1, float x2, float x3, uint32_t& hi, uint32_t& lo) {
-  asm("{\n\t.reg .b16 a, b, c, d, e, f;\n\t.reg .b32 h0, h1, r0, r1, k;\n\t"
-      "cvt.rn.f16x2.f32 h0, %3, %2;\n\tcvt.rn.f16x2.f32 h1, %5, %4;\n\t"
-      "cvt.rn.satfinite.e4m3x2.f16x2 a, h0;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, h1;\n\t"
-      "mov.b32 %0, {a, b};\n\tmov.b32 {e, f}, %0;\n\t"
-      "cvt.rn.f16x2.e4m3x2 r0, e;\n\tcvt.rn.f16x2.e4m3x2 r1, f;\n\t"
-      "mov.b32 k, 0x4c004c00;\n\t"
-      "sub.f16x2 r0, h0, r0;\n\tsub.f16x2 r1, h1, r1;\n\tmul.f16x2 r0, r0, k;\n\tmul.f16x2 r1, r1, k;\n\t"
-      "cvt.rn.satfinite.e4m3x2.f16x2 c, r0;\n\tcvt.rn.satfinite.e4m3x2.f16x2 d, r1;\n\t"
-      "mov.b32 %1, {c, d};\n\t}"
-      : "=&r"(hi), "=r"(lo)
-      : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
+// Four weights (not negative) -> the three bytes of each: upper byte of the half-precision number, the remainder rounded to its upper
+// byte, the second remainder likewise (half a step is added to the magnitude, whose bits count up across exponents).  The differences are
+// exact.  A NaN stays one in the first byte.
+__device__ __forceinline__ void split_weights(float x0, float x1, float x2, float x3, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  constexpr uint32_t UPPER = 0xff00ff00u, HALF_STEP = 0x00800080u;
+  uint32_t h[2], m[2], l[2];
+  asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(h[0]) : "f"(x1), "f"(x0));
+  asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(h[1]) : "f"(x3), "f"(x2));
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(h[i]), "r"(h[i] & UPPER));
+    m[i] = r + HALF_STEP;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(l[i]) : "r"(r), "r"(m[i] & UPPER));
+    l[i] += HALF_STEP;
+  }
+  hi = __byte_perm(h[0], h[1], 0x7531);
+  mid = __byte_perm(m[0], m[1], 0x7531);
+  lo = __byte_perm(l[0], l[1], 0x7531);
 }
-static_assert(LO_SCALE == 16.f, "0x4c00 is 16 in half precision");
 
 // ---- producer warps: one for K and the tiles' descriptions, one for V ---------------------------------------
 // Eight boxes, a page each, make a piece; one lane sends them all, with the rows in uniform registers.  Sending a box occupies its
@@ -172,6 +205,7 @@ __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk
   const bool lead = mv::um::elect_one();
   const uint64_t policy = mv::l2_policy_evict_first();  // the cache is read once per call
   int tile = 0;
+  Slots ring{IS_K ? 0 : 1};
   bool ok = true;
   // a window of 32 entries, one per lane
   auto entry_at = [&](int i0) {
@@ -213,6 +247,8 @@ __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk
       }
       return d;
     };
+    const bool both = IS_K || both_slots_of_v<D>(columns_of(s.n_qv));
+    ring.begin(both);
     int4 e0 = entry_at(0), e1 = entry_at(32);
     float2 s0 = make_float2(0.f, 1.f);
     if (IS_K) s0 = scale_at(e0);
@@ -226,9 +262,10 @@ __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk
       }
       const unsigned present = (__ballot_sync(0xffffffffu, e0.x >= 0) >> at) & 0xffu;
       const int my_row = (e0.x * a.Hkv + s.head) * PS;
-      const int piece = 2 * tile + (IS_K ? 0 : 1), slot = piece % RING;
-      ok = warp_wait(c, bar(&meta->empty[slot]), ((piece / RING) & 1) ^ 1);
+      const int slot = ring.slot();
+      ok = warp_wait(c, bar(&meta->empty[slot]), ring.parity() ^ 1);
       if (!ok) break;
+      ring.advance(both);
       const uint32_t fb = bar(&meta->full[slot]), dst = c.base + slot * Lay<D>::PIECE;
       if (lead) mv::mbar_arrive_expect_tx(fb, uint32_t(__popc(present)) * (PS * D));
 #pragma unroll
@@ -250,12 +287,9 @@ __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk
     }
   }
   if (!ok) {
-    // what is in flight must land before the CTA may leave: this warp's last two fills
+    // what is in flight must land before the CTA may leave: the last fills of this warp's slots
     if (lane == 0)
-      for (int k = max(0, tile - 2); k < tile; ++k) {
-        const int piece = 2 * k + (IS_K ? 0 : 1);
-        (void)mv::mbar_wait_bounded(bar(&meta->full[piece % RING]), (piece / RING) & 1, 20000000ull);
-      }
+      for (int k = 0; k < 2; ++k) (void)mv::mbar_wait_bounded(bar(&meta->full[ring.first + 2 * k]), ((ring.phase >> k) & 1) ^ 1, 20000000ull);
     __syncwarp();
   }
 }
@@ -345,16 +379,15 @@ __device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s,
   }
 }
 
-// Tensor-memory columns of a segment with `cols` columns of q-vectors: score buffers, O (values, then remainders), sums.  With 64
-// columns there is room for one score buffer only.
+// Tensor-memory columns of a segment with `cols` columns of q-vectors: two score buffers, O (in three parts up to 32 columns), sums.
 struct Columns {
-  int s1, o, sums;
-  __device__ __forceinline__ explicit Columns(int cols) : s1(cols < 64 ? cols : 0), o(s1 + cols), sums(s1 + 3 * cols) {}
+  int parts, s1, o, sums;
+  __device__ __forceinline__ explicit Columns(int cols) : parts(in_thirds(cols) ? 3 : 1), s1(cols), o(2 * cols), sums((2 + parts) * cols) {}
 };
 
 // The tiles of one segment and its result.  False: a wait ran out.
 template <int D>
-__device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment& s, int& tile) {
+__device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment& s, int& tile, Slots& v_ring) {
   const Args& a = *c.a;
   Meta* const meta = c.meta;
   const int tid = threadIdx.x, token = tid, quarter = tid >> 5, lane = tid & 31;
@@ -365,8 +398,11 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
   };
   const Columns at(cols);
   const uint32_t lanes = meta->tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
-  const int sw = token & 7;
+  const bool thirds = in_thirds(cols);
+  const int sw = thirds ? token & 7 : (token >> 1) & 3;                           // swizzle of the token's row of weights
+  const int p_next = thirds ? nb : 0, p_plane = thirds ? 0 : P_THIRD;             // from one byte of a weight to the next: pieces of the row, or bytes
   bool ok = true;
+  v_ring.begin(both_slots_of_v<D>(cols));
   uint64_t referenced = 0;  // q-vectors that have a reference (or saw scores that were not numbers)
 #pragma unroll 1
   for (int t = 0; t < s.n_tiles; ++t, ++tile) {
@@ -383,8 +419,8 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
     const float fk = meta->factor * en.ks;
     const uint64_t fk2 = mv::pack_f32x2(fk, fk), ev2 = mv::pack_f32x2(evf, evf);
     const uint32_t s_t = lanes + ((tile & 1) ? at.s1 : 0);
-    unsigned char* const p_tile = c.smem + Lay<D>::P + (tile & 1) * P_TILE;
-    unsigned char* const p_row = p_tile + token * 128;
+    unsigned char* const p_tile = c.smem + (thirds ? Lay<D>::P + (tile & 1) * P_NARROW : Lay<D>::PW + (tile & 1) * P_WIDE);
+    unsigned char* const p_row = p_tile + token * (thirds ? 128 : 64);
     float* const xch = reinterpret_cast<float*>(p_tile);  // exchange area until the weights stand
     bool valid = true;
     uint64_t see = ~0ull;
@@ -392,8 +428,7 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
       valid = (token & 15) < int(en.vs & 255u);
       see = valid ? (uint64_t(en.see_hi) << 32) | en.see_lo : 0;
     }
-    // Weights of the thread's token against the references as they stand, into the weight tile (row = token; values, then
-    // remainders) and, times `sign` 2^(-e), into the token's sums.  Returns the largest weight.
+    // Weights of the thread's token against the references as they stand, into the weight tile (row = token) and, times `sign` 2^(-e), into the token's sums.  Returns the largest weight.
     auto pass = [&](float sign, bool first) {
       float top = 0.f;
       const uint64_t vinv2 = mv::pack_f32x2(sign * vinv, sign * vinv);
@@ -425,13 +460,12 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
 #pragma unroll
         for (int j = 0; j < W; j += 2) most = mv::max3(most, p[j], p[j + 1]);
         top = fmaxf(top, most);
-        uint32_t hi[W / 4], lo[W / 4];
+        uint32_t hi[W / 4], mid[W / 4], lo[W / 4];
 #pragma unroll
-        for (int k = 0; k < W / 4; ++k) {
-          split_e4m3x4(p[k * 4], p[k * 4 + 1], p[k * 4 + 2], p[k * 4 + 3], hi[k], lo[k]);
-        }
+        for (int k = 0; k < W / 4; ++k) split_weights(p[k * 4], p[k * 4 + 1], p[k * 4 + 2], p[k * 4 + 3], hi[k], mid[k], lo[k]);
         *reinterpret_cast<uint4*>(p_row + ((u ^ sw) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(p_row + (((u + nb) ^ sw) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        *reinterpret_cast<uint4*>(p_row + p_plane + (((u + p_next) ^ sw) << 4)) = make_uint4(mid[0], mid[1], mid[2], mid[3]);
+        *reinterpret_cast<uint4*>(p_row + 2 * p_plane + (((u + 2 * p_next) ^ sw) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         // A weight past the format's range only says that the references have to move; what it adds here is taken back then, so it must
         // not overflow (capped, it still exceeds what the move leaves of it, and the sum loses nothing but a rounding).
         if (most > CAP)
@@ -500,7 +534,7 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
           each_eight([&](int b) {
             const float* const f = xch + 4 * MAXQV + b * 8;
 #pragma unroll 1
-            for (int k = 0; k < 3; ++k) {  // O (values, remainders) and the sums, which lie side by side
+            for (int k = 0; k <= at.parts; ++k) {  // O and the sums, which lie side by side
               uint32_t o[8];
               mv::um::ld8(lanes + at.o + k * cols + b * 8, o);
               mv::um::wait_ld();
@@ -530,8 +564,8 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
     }
     if (!plain && !__all_sync(0xffffffffu, valid)) {
       // no token here: whatever the slot holds meets a weight of zero, so it must be finite
-      const int vp = 2 * tile + 1, vslot = vp % RING;
-      ok = ok && warp_wait(c, bar(&meta->full[vslot]), (vp / RING) & 1);
+      const int vslot = v_ring.slot();
+      ok = ok && warp_wait(c, bar(&meta->full[vslot]), v_ring.parity());
       if (!valid) {
         uint4* const row = reinterpret_cast<uint4*>(c.smem + vslot * Lay<D>::PIECE + token * D);
 #pragma unroll
@@ -542,6 +576,7 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
     mv::um::fence_before();
     __syncwarp();
     if (lane == 0 && ok) mv::mbar_arrive(bar(&meta->p_full[tile & 1]));
+    v_ring.advance(both_slots_of_v<D>(cols));
   }
   // ---- the segment's result: sums over the tokens, then the head vectors (thread = element; at 64 elements the upper half of the lanes holds them once more)
   ok = ok && warp_wait(c, bar(&meta->pv_done[(tile - 1) & 1]), ((tile - 1) >> 1) & 1);  // (products complete in order)
@@ -578,9 +613,12 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
   }
   (void)vote_all(true);
   each_eight([&](int b) {
-    uint32_t o0[8], o1[8];
+    uint32_t o0[8], o1[8] = {}, o2[8] = {};
     mv::um::ld8(lanes + at.o + b * 8, o0);
-    mv::um::ld8(lanes + at.o + (n8 + b) * 8, o1);
+    if (thirds) {
+      mv::um::ld8(lanes + at.o + cols + b * 8, o1);
+      mv::um::ld8(lanes + at.o + 2 * cols + b * 8, o2);
+    }
     const int left = s.n_qv - b * 8;
     int h = (b * 8) % a.G;  // head of the q-vector inside the group
     bf16* out = a.out + (int64_t(s.row0 + b * 8 / a.G) * a.Hq + s.head * a.G + h) * D + token;
@@ -589,7 +627,7 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
     mv::um::wait_ld();
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float y = fmaf(__uint_as_float(o1[j]), 1.f / LO_SCALE, __uint_as_float(o0[j]));
+      const float y = __uint_as_float(o0[j]) + (__uint_as_float(o1[j]) + __uint_as_float(o2[j]));
       if (j < left && (D == 128 || token < D)) {
         if (s.slot >= 0) part[j * D] = y;
         else *out = __float2bfloat16_rn(y * xch[4 * MAXQV + b * 8 + j]);
@@ -609,15 +647,16 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
 template <int D>
 __device__ __forceinline__ void softmax_warps(const Cta& c, mv::blk::Walk& w, mv::blk::Segment& s, bool more) {
   mv::blk::CutLog cuts;
-  int tile = 0;  // tiles of the share so far: ring position, score buffer and phases follow from it
+  int tile = 0;  // tiles of the share so far: score and weight buffers and their phases follow from it
+  Slots v_ring{1};
   bool ok = true;
   for (int turn = 0; more; turn ^= 1) {
     cuts.add(*c.a, s);
-    stage_q<D>(c, s, (s.n_qv + 15) / 16 * 16, turn);
+    stage_q<D>(c, s, columns_of(s.n_qv), turn);
     mv::fence_proxy_async();
     (void)vote_all(true);  // the factors are there for all
     if ((threadIdx.x & 31) == 0) mv::mbar_arrive(bar(&c.meta->q_full));
-    ok = run_segment<D>(c, s, tile);
+    ok = run_segment<D>(c, s, tile, v_ring);
     more = ok && w.next(*c.a, s);
   }
   if (threadIdx.x == 0) cuts.store(*c.a, blockIdx.x);
@@ -640,15 +679,15 @@ __device__ __forceinline__ void score_issuer(const Cta& c, mv::blk::Walk& w, mv:
   int tile = 0, segment = 0;
   bool ok = true;
   for (; more; more = ok && w.next(*c.a, s)) {
-    const int cols = (s.n_qv + 15) / 16 * 16;
+    const int cols = columns_of(s.n_qv);
     const Columns at(cols);
     const uint32_t idesc = mv::um::idesc_e4m3(128, cols, 0, 0);
     ok = warp_wait(c, bar(&meta->q_full), segment & 1);
     ++segment;
 #pragma unroll 1
     for (int t = 0; t < s.n_tiles && ok; ++t, ++tile) {
-      // the buffer was read before the weights of the tile that last used it were handed over: two tiles ago, or one where there is room for one
-      const int last = tile - (cols < 64 ? 2 : 1), slot = (2 * tile) % RING;
+      // the buffer was read before the weights of the tile that last used it, two tiles ago, were handed over
+      const int last = tile - 2, slot = (2 * tile) % RING;
       if (t > 0 && last >= 0) ok = warp_wait(c, bar(&meta->p_full[last & 1]), (last >> 1) & 1);
       ok = ok && warp_wait(c, bar(&meta->full[slot]), ((2 * tile) / RING) & 1);
       if (!ok) break;
@@ -677,27 +716,43 @@ __device__ __forceinline__ void output_issuer(const Cta& c, mv::blk::Walk& w, mv
   Meta* const meta = c.meta;
   const bool lead = mv::um::elect_one();
   int tile = 0;
+  Slots v_ring{1};
   bool ok = true;
   for (; more; more = ok && w.next(*c.a, s)) {
-    const int cols = (s.n_qv + 15) / 16 * 16;
+    const int cols = columns_of(s.n_qv);
+    const bool both = both_slots_of_v<D>(cols);
+    v_ring.begin(both);
     const uint32_t o_t = meta->tmem + Columns(cols).o;
-    const uint32_t idesc = mv::um::idesc_e4m3(128, 2 * cols, 1, 1);
+    const bool thirds = in_thirds(cols);
+    const uint32_t idesc = mv::um::idesc_e4m3_e5m2(128, thirds ? 3 * cols : cols, 1, 1);
 #pragma unroll 1
     for (int t = 0; t < s.n_tiles; ++t, ++tile) {
-      const int vp = 2 * tile + 1, vslot = vp % RING;
-      ok = warp_wait(c, bar(&meta->full[vslot]), (vp / RING) & 1) && warp_wait(c, bar(&meta->p_full[tile & 1]), (tile >> 1) & 1);
+      const int vslot = v_ring.slot();
+      ok = warp_wait(c, bar(&meta->full[vslot]), v_ring.parity()) && warp_wait(c, bar(&meta->p_full[tile & 1]), (tile >> 1) & 1);
       if (!ok) break;
       mv::um::fence_after();
       if (lead) {
         const uint64_t v_desc = Lay<D>::desc(c.base + vslot * Lay<D>::PIECE);
-        const uint64_t p_desc = mv::um::smem_desc(c.base + Lay<D>::P + (tile & 1) * P_TILE, 16, 1024);
-        if (t == 0) mv::um::mma8_ss<false>(o_t, v_desc, p_desc, idesc);
-        else mv::um::mma8_ss<true>(o_t, v_desc, p_desc, idesc);
+        if (thirds) {
+          const uint64_t p_desc = mv::um::smem_desc(c.base + Lay<D>::P + (tile & 1) * P_NARROW, 16, 1024);
+          if (t == 0) mv::um::mma8_ss<false>(o_t, v_desc, p_desc, idesc);
+          else mv::um::mma8_ss<true>(o_t, v_desc, p_desc, idesc);
 #pragma unroll
-        for (int k = 1; k < TILE / 32; ++k) mv::um::mma8_ss<true>(o_t, v_desc + uint32_t((k * 32 * D) >> 4), p_desc + uint32_t((k * 4096) >> 4), idesc);
+          for (int k = 1; k < TILE / 32; ++k) mv::um::mma8_ss<true>(o_t, v_desc + uint32_t((k * 32 * D) >> 4), p_desc + uint32_t((k * 32 * 128) >> 4), idesc);
+        } else {
+#pragma unroll 1
+          for (int third = 0; third < 3; ++third) {
+            const uint64_t p_desc = mv::um::smem_desc_64b(c.base + Lay<D>::PW + (tile & 1) * P_WIDE + third * P_THIRD, 16, 512);
+            if (t == 0 && third == 0) mv::um::mma8_ss<false>(o_t, v_desc, p_desc, idesc);
+            else mv::um::mma8_ss<true>(o_t, v_desc, p_desc, idesc);
+#pragma unroll
+            for (int k = 1; k < TILE / 32; ++k) mv::um::mma8_ss<true>(o_t, v_desc + uint32_t((k * 32 * D) >> 4), p_desc + uint32_t((k * 32 * 64) >> 4), idesc);
+          }
+        }
         mv::um::commit(bar(&meta->pv_done[tile & 1]));
         mv::um::commit(bar(&meta->empty[vslot]));
       }
+      v_ring.advance(both);
       __syncwarp();
     }
   }

@@ -115,6 +115,10 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int a_mn_major, 
 __host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N, int a_mn_major, int b_mn_major) {
   return (1u << 4) | (uint32_t(a_mn_major) << 15) | (uint32_t(b_mn_major) << 16) | (uint32_t(N >> 3) << 17) | (uint32_t(M >> 4) << 24);
 }
+// the same with five exponent and two mantissa bits in B
+__host__ __device__ constexpr uint32_t idesc_e4m3_e5m2(int M, int N, int a_mn_major, int b_mn_major) {
+  return idesc_e4m3(M, N, a_mn_major, b_mn_major) | (1u << 10);
+}
 // D[tmem] (+)= A * B, 8-bit float operands (32 elements of the contraction per instruction)
 template <bool Acc>
 __device__ __forceinline__ void mma8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc) {

@@ -225,3 +225,57 @@ def test_scales_of_zero(hq, hkv, branches, d, pages):
     q = torch.randn(int(batch.node_new.sum()), hq, d, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").bfloat16()
     out, _ = check(batch, hq, hkv, d, q, (k8, v8, sc))
     assert pages < 1000 or (out == 0).all()
+
+
+# Weights in three 8-bit floats: off by at most 1.5 * 2^-10 of themselves (2^-11 for exp2, joins and sums on top makes less than 2^-9), or 2^-29
+# of the row's largest (2^-28 with the half-precision number's own last step).
+FINE = {"weight": 2.0 ** -9, "floor": 2.0 ** -28}
+
+
+def with_sink(batch, hq, hkv, d, mass, sink_value):
+    """q and a cache whose first token takes ``mass`` of every row, before a tail of scores of spread one and V of mean 1/2."""
+    rng = np.random.default_rng(1)
+    n = int(max(batch.node_len))
+    tail = torch.from_numpy((8 * rng.standard_normal(n)).astype(np.float32)).to(torch.float8_e4m3fn).float().numpy()
+    k8, v8, sc = keyed(batch, hkv, d, of_prompt(batch, lambda r, m: np.concatenate([[0.0], tail[1:m]])))
+    score = float(np.log(np.exp(tail[1:] / 8.0).sum() * mass / (1.0 - mass)))
+    k, v = k8.view(torch.float8_e4m3fn).float(), v8.view(torch.float8_e4m3fn).float() + 32.0
+    first = torch.from_numpy(batch.page_idx[batch.page_off[batch.node_off[:-1]]].astype(np.int64)).cuda()
+    k[first, :, 0, 1] = 32.0
+    v[first, :, 0] = sink_value
+    q = torch.zeros(int(batch.node_new.sum()), hq, d, device="cuda")
+    q[..., 0], q[..., 1] = 0.125, score / 32.0
+    f8 = lambda x: x.to(torch.float8_e4m3fn).view(torch.uint8).contiguous()
+    return q.bfloat16(), (f8(k), f8(v), sc)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,branches", SHAPES)
+@pytest.mark.parametrize("mass", [0.9, 0.97, 0.999])
+@pytest.mark.parametrize("sink_value", [0.0, 64.0])
+def test_a_sink_leaves_the_tail_its_share(hq, hkv, branches, d, mass, sink_value):
+    """A first token that takes nearly all of a row, its own V zero or not, and 16K others that share the rest."""
+    batch = streams(10, 16000, branches)
+    q, pools = with_sink(batch, hq, hkv, d, mass, sink_value)
+    check(batch, hq, hkv, d, q, pools, 1.0, **FINE)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("sink_value", [0.0, 64.0])
+def test_a_sink_before_64k_tokens(d, sink_value):
+    batch = streams(6, 65000, 4)
+    q, pools = with_sink(batch, 16, 4, d, 0.97, sink_value)
+    check(batch, 16, 4, d, q, pools, 1.0, **FINE)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,requests,length,branches", [
+    (8, 2, 1, 40000, 2), (4, 1, 1, 60000, 1), (2, 2, 1, 9000, 1), (40, 8, 60, 1900, 3), (8, 8, 90, 700, 1), (7, 1, 3, 20000, 9), (64, 8, 8, 5000, 8)])
+def test_long_and_cut_streams_element_by_element(hq, hkv, requests, length, branches, d):
+    """Flat random scores over long histories: every weight is small, so that a part lost on the way, or counted twice, shows."""
+    batch = _batch_of([[([], length + 13 * r, 0)] + [([0], 5 * b, 1) for b in range(branches)] for r in range(requests)])
+    q = torch.randn(int(batch.node_new.sum()), hq, d, generator=torch.Generator(device="cuda").manual_seed(26), device="cuda").bfloat16()
+    out, step = check(batch, hq, hkv, d, q, pools_of(batch.num_pages, hkv, d, 25), **FINE)
+    # and the bound tells: zeros fail it everywhere, a result without a 64th of the history somewhere
+    r, ref, tol = next(elementwise(q, *pools_of(batch.num_pages, hkv, d, 25), step.t, hq // hkv, d ** -0.5, **FINE))
+    assert (ref.abs() > tol).float().mean() > 0.5
