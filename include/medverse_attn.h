@@ -349,7 +349,7 @@ mv_status mv_rope_write_kv_fp8_blk(const mv_step_tables* tables, const mv_attn_g
  *               scratch, not to be shared by calls that may overlap on the device
  * out must not overlap q_rot.  A scale counts as the power of two that its exponent gives (its sign and mantissa are not looked at);
  * V's has to be at most 2^40, and below 2^-80 (a scale of zero too) counts as 2^-80.
- * Arithmetic: q as two 8-bit floats at one power of two per group and KV head (off by at most 2^-17 of the group's largest element),
+ * Arithmetic: q as two 8-bit floats at one power of two per row and query head (off by at most 2^-17 of its largest element),
  * weights as three 8-bit floats (off by at most 1.5 * 2^-10 of the weight or 2^-29 of the row's largest), sums and softmax statistics
  * in 32 bits.  The same inputs give the same bits on every call.
  * dtype MV_BF16, head_dim 64 or 128, group size at most 64 and rows_per_group * group size <= 64; all tensors 16-byte aligned.

@@ -16,7 +16,9 @@
 // and one pair of scales.
 //   - Q is two K-major tiles of 8-bit floats, the rounded element and its rounded remainder at one power-of-two scale per
 //     q-vector: a bf16 element has eight significant bits, value plus remainder hold nine, so the split is exact
-//     for elements within 2^-9 of the largest (and off by at most 2^-17 of the largest below).
+//     for elements within 2^-9 of the vector's largest (and off by at most 2^-17 of the largest below).  A power of its own for every
+//     vector costs a multiplication per pair of scores (128 mixed requests 441 -> 460 us); with one for the whole stream a head 2^12 below
+//     another lost 2 % of its result, one 2^16 below 28 %.
 //   - The weights are three tiles of 8-bit floats with five exponent bits (the upper byte of a half-precision number): the weight in
 //     half precision cut to its upper byte, what is left of it rounded to one, and what is left then.  All have the same scale.  A
 //     weight is off by at most 1.5 * 2^-10 of itself (2^-11 in half precision, 2^-10 behind the third byte) or 2^-17, where the largest
@@ -77,23 +79,21 @@ constexpr float CAP = 0x1p20f;            // what a weight past TOP counts as un
 // as 2^-80.  Sums hold weight * 2^80 at most, below 2^124 for 2^23 tokens, and weights go down to 2^-126, which leaves 2^46 for the other end.
 constexpr int V_MIN = -80;
 
-struct alignas(16) Entry {  // one page of a tile, as the softmax threads need it
-  uint32_t see_lo, see_hi;  // q-vectors that see it
-  float ks;                 // K's scale; NaN if either scale is
-  uint32_t vs;              // V's scale, a power of two, with the tokens in the mantissa's low byte; bit 8: sixteen tokens that every q-vector sees
-};
+// One page of a tile, as the softmax threads need it: K's exponent (biased) in bits 23 to 30, V's in bits 15 to 22, the tokens in the low
+// byte, and two marks.
+constexpr uint32_t ALL_SEE = 256, LOST = 512;  // sixteen tokens that every q-vector sees; either scale is NaN
 struct Meta {
-  alignas(16) float minus_ref[MAXQV];  // minus the reference of a q-vector (+infinity: none yet; -infinity: no such q-vector); read four at a time
-  float factor;                        // of a score
-  uint32_t largest[2];                 // magnitude among a segment's finite q-vectors (bf16 bits), segments in turn
-  Entry entry[METAS][TILE_ENTRIES];
-  uint2 seen[METAS];                   // q-vectors that see some page of the tile
+  alignas(16) float minus_ref[MAXQV];    // minus the reference of a q-vector (+infinity: none yet; -infinity: no such q-vector); read four at a time
+  alignas(16) uint16_t unit[MAXQV];      // power of two of a q-vector's 8-bit floats, upper half of the float; read eight at a time
+  uint2 see[METAS][TILE_ENTRIES];        // q-vectors that see a page
+  uint32_t page[METAS][TILE_ENTRIES];
+  uint2 seen[METAS];                     // q-vectors that see some page of the tile
   uint64_t full[RING], empty[RING], described[METAS], s_full[2], q_full, p_full[2], pv_done[2], drained[2];
   int abort;
   uint32_t tmem;
 };
 static_assert(sizeof(Meta) <= 1024, "meta area");
-static_assert(offsetof(Meta, minus_ref) % 16 == 0, "vector loads");
+static_assert(offsetof(Meta, minus_ref) % 16 == 0 && offsetof(Meta, unit) % 16 == 0, "vector loads");
 
 // Shared memory.  A row of the cache is a token's D bytes, and so is a row of the tiles: 128 bytes with the 128-byte swizzle, or 64
 // bytes with the 64-byte swizzle.
@@ -224,13 +224,13 @@ __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk
   };
   for (; ok && more; more = ok && w.next(a, s)) {
     // what the softmax threads need of an entry
-    auto describe = [&](const int4& e, const float2& sc) {
-      Entry d{0, 0, 0.f, 127u << 23};
+    auto describe = [&](const int4& e, const float2& sc, uint64_t& see) {
+      uint32_t page = 127u << 23 | 127u << 15;
+      see = 0;
       if (e.x >= 0) {
         const int rows = s.n_qv / a.G;
         const uint64_t all_rows = rows >= 64 ? ~0ull : (1ull << rows) - 1;
         const uint64_t mask = ((uint64_t(uint32_t(e.w)) << 32) | uint32_t(e.z)) & all_rows;
-        uint64_t see = 0;
         if (mask == all_rows) {
           see = s.n_qv >= 64 ? ~0ull : (1ull << s.n_qv) - 1;
         } else {
@@ -240,19 +240,17 @@ __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk
             if ((mask >> r) & 1) see |= one_row << (r * a.G);
         }
         const uint32_t ek = uint32_t(mv::blk::scale_exponent(sc.x) + 127), ev = uint32_t(mv::blk::scale_exponent(sc.y) + 127);
-        d.see_lo = uint32_t(see);
-        d.see_hi = uint32_t(see >> 32);
-        d.ks = ek == 255 || ev == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float(ek << 23);
-        d.vs = (ev == 255 ? 127u : max(ev, uint32_t(127 + V_MIN))) << 23 | (mask == all_rows && e.y == PS ? 256u : 0u) | uint32_t(e.y);
+        page = ek << 23 | (ev == 255 ? 127u : max(ev, uint32_t(127 + V_MIN))) << 15 | (ek == 255 || ev == 255 ? LOST : 0u) | (mask == all_rows && e.y == PS ? ALL_SEE : 0u) | uint32_t(e.y);
       }
-      return d;
+      return page;
     };
     const bool both = IS_K || both_slots_of_v<D>(columns_of(s.n_qv));
     ring.begin(both);
     int4 e0 = entry_at(0), e1 = entry_at(32);
     float2 s0 = make_float2(0.f, 1.f);
     if (IS_K) s0 = scale_at(e0);
-    Entry d0;
+    uint32_t page0 = 0;
+    uint64_t see0 = 0;
 #pragma unroll 1
     for (int t = 0; t < s.n_tiles; ++t, ++tile) {
       const int at = (t * TILE_ENTRIES) & 31;
@@ -275,10 +273,13 @@ __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk
       }
       __syncwarp();
       if (IS_K) {
-        if (at == 0) d0 = describe(e0, s0);
+        if (at == 0) page0 = describe(e0, s0, see0);
         const bool mine = lane >= at && lane < at + TILE_ENTRIES;
-        const uint32_t any_lo = __reduce_or_sync(0xffffffffu, mine ? d0.see_lo : 0), any_hi = __reduce_or_sync(0xffffffffu, mine ? d0.see_hi : 0);
-        if (mine) meta->entry[tile % METAS][lane - at] = d0;
+        const uint32_t any_lo = __reduce_or_sync(0xffffffffu, mine ? uint32_t(see0) : 0), any_hi = __reduce_or_sync(0xffffffffu, mine ? uint32_t(see0 >> 32) : 0);
+        if (mine) {
+          meta->see[tile % METAS][lane - at] = make_uint2(uint32_t(see0), uint32_t(see0 >> 32));
+          meta->page[tile % METAS][lane - at] = page0;
+        }
         if (lane == 0) meta->seen[tile % METAS] = make_uint2(any_lo, any_hi);
         __syncwarp();
         if (lane == 0) mv::mbar_arrive(bar(&meta->described[tile % METAS]));
@@ -296,16 +297,14 @@ __device__ __forceinline__ void producer(const Cta& c, mv::blk::Walk& w, mv::blk
 
 // ---- softmax warps ---------------------------------------------------------------------------------------
 // q-vectors of the segment to the two K-major tiles (16-byte pieces XOR-swizzled as TMA does it for the cache), eight threads per
-// q-vector; factor and references of the segment.  One power of two scales them all: what it costs a small q-vector in
-// relative precision is, in its scores, no more than the largest one's rounding.
+// q-vector, each vector at its own power of two: what a row gets does not depend on the rows and heads that share its stream.
 template <int D>
-__device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s, int cols, int turn) {
+__device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s, int cols) {
   const Args& a = *c.a;
   constexpr int ROWS = SOFTMAX / 8, STEPS = MAXQV / ROWS;  // q-vectors at a time
   constexpr int LOADS = D / 64;                            // 16-byte loads of a thread
   const int tid = threadIdx.x, x0 = tid >> 3, ch = tid & 7;
   uint4* const raw = reinterpret_cast<uint4*>(c.smem + Lay<D>::P);  // the q-vectors as they are, in the weight tiles
-  uint32_t most = 0;
   uint4 in[STEPS][LOADS];
 #pragma unroll
   for (int i = 0; i < STEPS; ++i) {
@@ -323,35 +322,26 @@ __device__ __forceinline__ void stage_q(const Cta& c, const mv::blk::Segment& s,
   for (int i = 0; i < STEPS; ++i) {
     const int x = i * ROWS + x0;
     if (x < cols) {
-      uint32_t m = 0;
 #pragma unroll
-      for (int k = 0; k < LOADS; ++k) {
-        const uint4 u = in[i][k];
-        raw[(x * 8 + ch) * LOADS + k] = u;
-        m = __vmaxu2(m, __vmaxu2(__vmaxu2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), __vmaxu2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu)));
-      }
-      m = max(m & 0xffffu, m >> 16);
-      if (m < 0x7f80u) most = max(most, m);  // (of a q-vector that is not finite, any part that is may count)
+      for (int k = 0; k < LOADS; ++k) raw[(x * 8 + ch) * LOADS + k] = in[i][k];  // (each thread reads back its own)
     }
-  }
-  most = __reduce_max_sync(0xffffffffu, most);
-  if ((tid & 31) == 0) atomicMax(&c.meta->largest[turn], most);
-  (void)vote_all(true);
-  // largest element into [128, 256)
-  const int e = max(-120, max(int(c.meta->largest[turn] >> 7), 1) - 127 - 7);
-  const float inv = mv::blk::exp2_int(-e);
-  if (tid == 0) {
-    c.meta->factor = mv::blk::exp2_int(e) * a.scale_log2;
-    c.meta->largest[turn ^ 1] = 0;  // for the next segment
   }
 #pragma unroll 1
   for (int x = x0; x < cols; x += ROWS) {
-    uint32_t w[4 * LOADS], hi[2 * LOADS], lo[2 * LOADS];
+    uint32_t w[4 * LOADS], hi[2 * LOADS], lo[2 * LOADS], m = 0;
 #pragma unroll
     for (int k = 0; k < LOADS; ++k) {
       const uint4 u = raw[(x * 8 + ch) * LOADS + k];
       w[4 * k] = u.x; w[4 * k + 1] = u.y; w[4 * k + 2] = u.z; w[4 * k + 3] = u.w;
+      m = __vmaxu2(m, __vmaxu2(__vmaxu2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), __vmaxu2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu)));
     }
+    // largest element into [128, 256) (a vector that is not finite gives NaN at any power)
+    m = max(m & 0xffffu, m >> 16);
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const int e = max(-120, max(min(int(m >> 7), 254), 1) - 127 - 7);
+    const float inv = mv::blk::exp2_int(-e);
+    if (ch == 0) c.meta->unit[x] = uint16_t(__float_as_uint(mv::blk::exp2_int(e)) >> 16);
 #pragma unroll
     for (int k = 0; k < 2 * LOADS; ++k) {
       uint32_t h2[2], l2[2];
@@ -403,6 +393,7 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
   const int p_next = thirds ? nb : 0, p_plane = thirds ? 0 : P_THIRD;             // from one byte of a weight to the next: pieces of the row, or bytes
   bool ok = true;
   v_ring.begin(both_slots_of_v<D>(cols));
+  const float scale = a.scale_log2;
   uint64_t referenced = 0;  // q-vectors that have a reference (or saw scores that were not numbers)
 #pragma unroll 1
   for (int t = 0; t < s.n_tiles; ++t, ++tile) {
@@ -412,11 +403,12 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
                          (tile < 2 || wait_or_flag(c, bar(&meta->pv_done[tile & 1]), ((tile - 2) >> 1) & 1));
     ok = __all_sync(0xffffffffu, arrived);
     mv::um::fence_after();
-    const Entry en = meta->entry[tile % METAS][token >> 4];
-    const bool plain = __all_sync(0xffffffffu, en.vs & 256u);
-    const uint32_t vs_bits = en.vs & 0x7f800000u;
+    const uint32_t page = meta->page[tile % METAS][token >> 4];
+    const uint2 by = meta->see[tile % METAS][token >> 4];
+    const bool plain = __all_sync(0xffffffffu, page & ALL_SEE);
+    const uint32_t vs_bits = (page << 8) & 0x7f800000u;
     const float evf = float(int(vs_bits >> 23) - 127), vinv = __uint_as_float((254u << 23) - vs_bits);  // exponent; 2^-exponent
-    const float fk = meta->factor * en.ks;
+    const float fk = (page & LOST ? __uint_as_float(0x7fc00000u) : __uint_as_float(page & 0x7f800000u)) * scale;
     const uint64_t fk2 = mv::pack_f32x2(fk, fk), ev2 = mv::pack_f32x2(evf, evf);
     const uint32_t s_t = lanes + ((tile & 1) ? at.s1 : 0);
     unsigned char* const p_tile = c.smem + (thirds ? Lay<D>::P + (tile & 1) * P_NARROW : Lay<D>::PW + (tile & 1) * P_WIDE);
@@ -425,8 +417,8 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
     bool valid = true;
     uint64_t see = ~0ull;
     if (!plain) {
-      valid = (token & 15) < int(en.vs & 255u);
-      see = valid ? (uint64_t(en.see_hi) << 32) | en.see_lo : 0;
+      valid = (token & 15) < int(page & 255u);
+      see = valid ? (uint64_t(by.y) << 32) | by.x : 0;
     }
     // Weights of the thread's token against the references as they stand, into the weight tile (row = token) and, times `sign` 2^(-e), into the token's sums.  Returns the largest weight.
     auto pass = [&](float sign, bool first) {
@@ -440,13 +432,16 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
         uint32_t sc[W];
         mv::um::ld16(s_t + col, sc);
         const float4* const mr = reinterpret_cast<const float4*>(meta->minus_ref + col);
+        const uint4* const un = reinterpret_cast<const uint4*>(meta->unit + col);
         float p[W];
         mv::um::wait_ld();
 #pragma unroll
         for (int j = 0; j < W; j += 4) {
           const float4 y = mr[j / 4];
-          mv::unpack_f32x2(mv::fma_f32x2(mv::pack_u32x2(sc[j], sc[j + 1]), fk2, mv::add_f32x2(mv::pack_f32x2(y.x, y.y), ev2)), p[j], p[j + 1]);
-          mv::unpack_f32x2(mv::fma_f32x2(mv::pack_u32x2(sc[j + 2], sc[j + 3]), fk2, mv::add_f32x2(mv::pack_f32x2(y.z, y.w), ev2)), p[j + 2], p[j + 3]);
+          const uint32_t u0 = j % 8 ? un[j / 8].z : un[j / 8].x, u1 = j % 8 ? un[j / 8].w : un[j / 8].y;
+          const uint64_t f01 = mv::mul_f32x2(mv::pack_u32x2(u0 << 16, u0 & 0xffff0000u), fk2), f23 = mv::mul_f32x2(mv::pack_u32x2(u1 << 16, u1 & 0xffff0000u), fk2);
+          mv::unpack_f32x2(mv::fma_f32x2(mv::pack_u32x2(sc[j], sc[j + 1]), f01, mv::add_f32x2(mv::pack_f32x2(y.x, y.y), ev2)), p[j], p[j + 1]);
+          mv::unpack_f32x2(mv::fma_f32x2(mv::pack_u32x2(sc[j + 2], sc[j + 3]), f23, mv::add_f32x2(mv::pack_f32x2(y.z, y.w), ev2)), p[j + 2], p[j + 3]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) p[j + i] = mv::fast_exp2(p[j + i]);
         }
@@ -506,7 +501,7 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int q = b * 8 + j;
-            float y = fmaf(__uint_as_float(sc[j]), fk, evf);
+            float y = fmaf(__uint_as_float(sc[j]), __uint_as_float(uint32_t(meta->unit[q]) << 16) * fk, evf);
             if (!((see >> q) & 1) || y != y) y = -INFINITY;
             const int k = __float_as_int(y);
             const int m = __reduce_max_sync(0xffffffffu, k < 0 ? k ^ 0x7fffffff : k);  // ordered as the floats are
@@ -650,11 +645,11 @@ __device__ __forceinline__ void softmax_warps(const Cta& c, mv::blk::Walk& w, mv
   int tile = 0;  // tiles of the share so far: score and weight buffers and their phases follow from it
   Slots v_ring{1};
   bool ok = true;
-  for (int turn = 0; more; turn ^= 1) {
+  while (more) {
     cuts.add(*c.a, s);
-    stage_q<D>(c, s, columns_of(s.n_qv), turn);
+    stage_q<D>(c, s, columns_of(s.n_qv));
     mv::fence_proxy_async();
-    (void)vote_all(true);  // the factors are there for all
+    (void)vote_all(true);  // references and units are there for all
     if ((threadIdx.x & 31) == 0) mv::mbar_arrive(bar(&c.meta->q_full));
     ok = run_segment<D>(c, s, tile, v_ring);
     more = ok && w.next(*c.a, s);
@@ -775,7 +770,6 @@ __global__ void __launch_bounds__(NT, 2) decode_blk_tc_kernel(const Args a, cons
   }
   if (tid == 0) {
     meta->abort = 0;
-    meta->largest[0] = meta->largest[1] = 0;
     for (int i = 0; i < RING; ++i) {
       mv::mbar_init(bar(&meta->full[i]), 1);   // the producer's arrive (+ the bytes TMA reports)
       mv::mbar_init(bar(&meta->empty[i]), 1);  // one tcgen05.commit after the product that read the piece

@@ -279,3 +279,36 @@ def test_long_and_cut_streams_element_by_element(hq, hkv, requests, length, bran
     # and the bound tells: zeros fail it everywhere, a result without a 64th of the history somewhere
     r, ref, tol = next(elementwise(q, *pools_of(batch.num_pages, hkv, d, 25), step.t, hq // hkv, d ** -0.5, **FINE))
     assert (ref.abs() > tol).float().mean() > 0.5
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,branches", SHAPES[1:])
+@pytest.mark.parametrize("power", [6, 12, 16, 60])
+@pytest.mark.parametrize("large", ["heads", "rows"])
+def test_rows_and_heads_of_one_stream_differ_in_magnitude(hq, hkv, branches, d, power, large):
+    """Some heads, or some rows, have one element of 2^power, in a channel where every key is zero; the others of their group and
+    KV head are of ordinary size and keep the accuracy that their own elements give."""
+    batch = streams(12, 700, branches)
+    k8, v8, sc = pools_of(batch.num_pages, hkv, d, 13)
+    k8[..., 0] = 0
+    n = int(batch.node_new.sum())
+    q = torch.randn(n, hq, d, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    spike = torch.zeros(n, hq, d, device="cuda")
+    spike[..., 0] = 2.0 ** power
+    which = (torch.arange(hq, device="cuda") % 4 == 1)[None, :, None] if large == "heads" else (torch.arange(n, device="cuda") % branches == 2)[:, None, None]
+    check(batch, hq, hkv, d, torch.where(which, spike, q).bfloat16(), (k8, v8, sc), own_q=True, **FINE)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_q_of_every_magnitude(d):
+    """q-vectors from 2^-100 to 2^20 in one stream, zeros among them: tiny ones average, large ones pick."""
+    batch = streams(6, 700, 8)
+    k8, v8, sc = pools_of(batch.num_pages, 4, d, 14)
+    n = int(batch.node_new.sum())
+    q = torch.zeros(n, 32, d, device="cuda")
+    power = (torch.arange(n * 32, device="cuda") * 29 % 121 - 100).view(n, 32).double()
+    # one element each, so that a score is one product: exact in 8-bit floats
+    at = torch.arange(n * 32, device="cuda").view(n, 32) % d
+    q.scatter_(2, at[..., None], torch.exp2(power).float()[..., None])
+    q[3] = 0
+    check(batch, 32, 4, d, q.bfloat16(), (k8, v8, sc), own_q=True, **FINE)
