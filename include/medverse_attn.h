@@ -353,7 +353,7 @@ mv_status mv_rope_write_kv_fp8_blk(const mv_step_tables* tables, const mv_attn_g
  * weights as three 8-bit floats (off by at most 1.5 * 2^-10 of the weight or 2^-29 of the row's largest), sums and softmax statistics
  * in 32 bits.  The same inputs give the same bits on every call.
  * dtype MV_BF16, head_dim 64 or 128, group size at most 64 and rows_per_group * group size <= 64; all tensors 16-byte aligned.
- * Errors: MV_ERR_INVALID_ARG, MV_ERR_UNSUPPORTED (also a pool of 2^31 or more (page, KV head, token) rows, and capacities
+ * Errors: MV_ERR_INVALID_ARG (also q_rot or out with tables of positions and slots only, max_groups = 0), MV_ERR_UNSUPPORTED (also a pool of 2^31 or more (page, KV head, token) rows, and capacities
  * of max_entries / 8 + max_groups tiles whose product with n_kv_heads passes 1.7e9), MV_ERR_WORKSPACE, MV_ERR_CUDA.  A wait inside the
  * kernel that runs out (seconds) ends the call with MV_ERR_TIMEOUT in counts[4]; `out` is then undefined. */
 size_t mv_decode_fp8_blk_workspace_bytes(const mv_attn_geom* geom);

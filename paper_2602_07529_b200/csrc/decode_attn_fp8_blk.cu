@@ -240,7 +240,9 @@ extern "C" mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* t, const m
   const int G = g->n_q_heads / g->n_kv_heads;
   if (G > MAXQV || t->rows_per_group < 1 || t->rows_per_group > MAXQV / G) return MV_ERR_UNSUPPORTED;
   if (g->num_pages > INT32_MAX / PS / g->n_kv_heads) return MV_ERR_UNSUPPORTED;  // the rows of a pool are TMA coordinates
-  if (t->max_rows == 0 || t->max_groups == 0) return MV_OK;
+  if (t->max_rows == 0) return MV_OK;
+  // Tables of positions and slots only: no row has a group, so nothing could be written for those that there may be.
+  if (t->max_groups == 0) return q_rot || out ? MV_ERR_INVALID_ARG : MV_OK;
   if (!t->group_row_off || !t->group_ent_off || !t->group_tile_off || (t->max_entries > 0 && !t->entries)) return MV_ERR_INVALID_ARG;
   if (!q_rot || !k_pages8 || !v_pages8 || !kv_scale || !out) return MV_ERR_INVALID_ARG;
   for (const void* p : {q_rot, k_pages8, v_pages8, static_cast<const void*>(kv_scale), static_cast<const void*>(out),
