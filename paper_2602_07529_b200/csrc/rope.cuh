@@ -9,12 +9,13 @@ struct ThetaTable {
   double theta[64];
 };
 
-// cos and sin of pos * theta.  The angle and its reduction to [-pi/4, pi/4] (two-term Cody-Waite with a 53-bit and a
-// residual piece of pi/2; pos * theta stays below 2^25, so k * PIO2_HI is exact to well under 1e-12) are double
-// precision; the reduced angle is rounded to float and its cosine and sine come from the accurate float routine
-// (no fast-math intrinsics), so both agree with the double-precision values to within two units in the last place
-// of a float.  Six double-precision instructions per (token, i) instead of a double-precision sincos: with the
-// latter the arithmetic, not HBM, bounded the kernel at prefill sizes.
+// cos and sin of pos * theta, for |pos * theta| below 2^31 (the quadrant is counted in an int; positions of tables go up to
+// 2^30 and theta is at most 1 for a base of at least 1).  The angle and its reduction to [-pi/4, pi/4] (two-term Cody-Waite with a
+// 53-bit and a residual piece of pi/2, by fused multiply-adds) are double precision; the reduced angle is rounded to float and
+// its cosine and sine come from the accurate float routine (no fast-math intrinsics).  Up to an angle of 2^25 both agree with the
+// double-precision values to within two units in the last place of a float; beyond, what theta and the product lost as doubles shows
+// as well: 2^-22 at 2^30 (against 80-bit arithmetic: 2^-23).  Six double-precision instructions per (token, i) instead of a
+// double-precision sincos: with the latter the arithmetic, not HBM, bounded the kernel at prefill sizes.
 __device__ __forceinline__ void rope_cos_sin(int pos, double theta, float& c, float& s) {
   constexpr double TWO_OVER_PI = 0.63661977236758134308;
   constexpr double PIO2_HI = 1.57079632679489655800e+00;  // pi/2 rounded to double
