@@ -312,3 +312,30 @@ def test_q_of_every_magnitude(d):
     q.scatter_(2, at[..., None], torch.exp2(power).float()[..., None])
     q[3] = 0
     check(batch, 32, 4, d, q.bfloat16(), (k8, v8, sc), own_q=True, **FINE)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv", [(32, 4), (16, 8), (15, 3), (64, 1)])
+@pytest.mark.parametrize("spread", [0, 8])
+def test_streams_of_all_widths_follow_one_another(hq, hkv, d, spread):
+    """Groups of few and of many q-vectors in turn, short and long, so that a share goes from one width to another; what lies behind
+    the tokens of a page is NaN, and some rows see a part of their group's pages only."""
+    group = hq // hkv
+    most = max(1, 64 // group)
+    rng = np.random.default_rng(hq + d)
+    rows = [1 + (5 * r) % most for r in range(120)]
+    batch = _batch_of([[([], int(rng.integers(1, 1800)), 0)] + [([0], int(rng.integers(0, 200)), 1) for _ in range(n)] for n in rows])
+    k8, v8, sc = pools_of(batch.num_pages, hkv, d, 33, spread=spread)
+    if spread:
+        sc[..., 0] = 2.0 ** -5
+    used = torch.zeros(batch.num_pages, 16, dtype=torch.bool)
+    for node in range(batch.n_nodes):
+        n = int(batch.node_len[node] + batch.node_new[node])
+        for p in range((n + 15) // 16):
+            used[int(batch.page_idx[batch.page_off[node] + p]), :min(16, n - 16 * p)] = True
+    q = torch.randn(int(batch.node_new.sum()), hq, d, generator=torch.Generator(device="cuda").manual_seed(8), device="cuda").bfloat16()
+    clean, _ = check(batch, hq, hkv, d, q, (k8, v8, sc), own_q=True, **FINE)
+    hole = (~used).cuda()[:, None, :, None].expand_as(k8)
+    k8[hole], v8[hole] = 0x7F, 0xFF
+    dirty, _ = attend(batch, hq, hkv, d, q, (k8, v8, sc))
+    assert torch.equal(clean, dirty)
