@@ -333,6 +333,7 @@ mv_status mv_step_tables_read_status(const mv_step_tables* tables, void* cuda_st
  * A page whose first slot is written by this call starts afresh: its old scale and bytes count for nothing.
  * Rows with slot -1 are skipped and their outputs left as they were.  Rows of one page must be consecutive and ascending
  * (they are, in tables built above), and one page must not be written by two overlapping calls.
+ * The kernel for prompts takes tables with max_rows >= 2048 (whatever their rows are): give decode steps tables of their own.
  *   q, k, v  device [max_rows][heads][head_dim] bf16, q may be NULL;  q_rot  out (may alias q), NULL exactly when q is;
  *   k_rot    out, optional (NULL to skip; may alias k): rotated keys in bf16, what mv_dag_prefill_attn reads
  * dtype MV_BF16, head_dim 64 or 128; all tensors 16-byte aligned.  Errors: MV_ERR_INVALID_ARG, MV_ERR_UNSUPPORTED, MV_ERR_CUDA. */

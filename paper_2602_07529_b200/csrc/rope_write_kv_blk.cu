@@ -249,7 +249,11 @@ constexpr int MANY = 8;  // rows per CTA of a prompt
 template <int D>
 void launch(const Args& a, double rope_base, cudaStream_t st) {
   const mv::ThetaTable tt = mv::theta_table(rope_base, D);
-  // few rows (a decode step): one per CTA spreads them over the SMs; many (a prompt): MANY per CTA share the angles' staging
+  // Few rows (a decode step): one per CTA spreads them over the SMs; many (a prompt): MANY per CTA share the angles' staging.  The host knows the
+  // tables' capacity, not the step's rows.  One / MANY rows per CTA, us in a graph, 32 query and 8 KV heads of 128: runs of 16 rows (a prompt)
+  // 1024 rows 14.3 / 13.5, 2047 19.6 / 16.1, 4096 31.6 / 24.6, 8192 56 / 39; single rows (a decode step) 256 rows 5.8 / 21.9, 2047 26.4 / 34.4,
+  // 4096 49.7 / 51.3; 64 rows in tables of 2048 5.7 / 27.1, of 8192 15.5 / 31.3.  8 and 2 heads of 64, single rows: 1024 6.4 / 6.1, 2047 11.1 / 7.2.
+  // So a decode step should not come in tables made for 2048 rows and more.
   if (a.max_rows < 2048) rope_write_kv_blk_kernel<D, 1><<<a.max_rows, NT, 0, st>>>(a, tt);
   else rope_write_kv_blk_kernel<D, MANY><<<(a.max_rows + MANY - 1) / MANY, NT, 0, st>>>(a, tt);
 }
