@@ -23,7 +23,7 @@ using mv::blk::SHARES;
 // Bound by latency: the records, the references and parts, and the instructions' own arrival; the CTAs start as those of the
 // attention kernel leave their registers, so there are no more of them than fit at once.  Against CTAs that belong to
 // a share each, calls of one request of 8K tokens and 4 KV heads 34 -> 18 us, of 64K tokens and 2 KV heads 39 -> 22.5; against one
-// job at a time, 64 mixed requests 439 -> 432.  With 148 CTAs a short request 15.0 instead of 15.2 us, mixed ones 113 to 116.
+// job at a time, 128 mixed requests 439 -> 432.  With 148 CTAs a short request 15.0 instead of 15.2 us, mixed ones 113 to 116.
 constexpr int MERGE_WARPS = 8, ACCS = 4, ACC_LOADS = 2, PAIR = 2, MERGE_CTAS = SHARES;
 static_assert(SHARES % 2 == 0 && SHARES <= MERGE_WARPS * 64, "a thread takes two shares");
 template <int D>

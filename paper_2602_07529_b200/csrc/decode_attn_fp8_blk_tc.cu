@@ -36,13 +36,12 @@
 // weights two buffers, so that the products of one tile overlap the weights of the next.
 // With head_dim 64 a cache row is 64 bytes: everything is the same but for the swizzle, and the second product takes V's 64 elements
 // twice to fill the 128 lanes.
-// Measured (cache not in the L2, a call with its merge): 64 requests of mixed length, 64 query over 8 KV heads, 2.1 GB of cache, 481 us
-// (4.4 TB/s); 32 layered requests, 446 MB, 95 us (4.7 TB/s); 16 requests, 107 MB, 34 us; 64K tokens alone, 136 MB, 34 us; a short
-// request 15.4 us; 176 MB of 64-byte rows, partly in the L2, 64 us.
-// What bounds it: with 16 q-vectors the bytes (a tile and CTA takes 1900 cycles, 2 x 32 KB per SM: 4.9 TB/s); with 64 the weights
-// (about 4000 cycles, of which 2300 to 2700 are the loop over the columns, 1000 the wait for the one score buffer and 300 the
-// vote and the hand-over; the SM issues 42 % of its slots, more warps do not fit its registers); in small calls the chain of
-// launch, tables, first bytes, epilogue and merge, about 13 us.
+// Measured (cache not in the L2, a call with its merge): 128 requests of mixed length, 64 query over 8 KV heads, 2.1 GB of cache, 511 us
+// (4.1 TB/s; one set of inputs again and again 459); 32 layered requests, 446 MB, 101 us (4.4 TB/s); 16 requests, 107 MB, 36 us; 64K
+// tokens alone, 136 MB, 34 us; a short request 15.7 us; 37 requests of 64-element heads 29 us.
+// What bounds it: with 16 q-vectors the bytes (5.6 TB/s of DRAM reads inside the kernel); with 64 the loop over the weights (2.2 TB/s, the tensor
+// pipe 17 % busy, 47 % of the issue slots; more warps do not fit the registers); in small calls the chain of launch, tables, first
+// bytes, epilogue and merge, about 13 us.
 // Slower: eight softmax warps per CTA (register limit of 80), the column loop unrolled by two (instruction fetches), scores or sums
 // loaded ahead of their use (registers), the second product held back until the next scores are out.
 // Every wait is bounded; the softmax warps vote once per tile, and the vote carries a failed wait, so that they leave together.
