@@ -5,7 +5,7 @@
 // The scale of V is a power of two, 2^e, so it goes into the exponent: weights p_xj = 2^(s_xj + e_j - m_x) multiply the
 // stored bytes, and the denominator takes p_xj 2^(-e_j).  The reference m_x follows the largest s + e, which
 // keeps the weights of whatever dominates the NUMERATOR near one however much the pages' scales differ; with
-// exponents in [-60, 40] a token that matters to the denominator alone still gets a weight above 2^-126.
+// exponents in [-80, 40] a token that matters to the denominator alone still gets a weight above 2^-126.
 // Block scale NaN: the scores of the rows that see the page become NaN; a row that does not see it multiplies
 // finite bytes by zero.
 //
@@ -419,7 +419,8 @@ __device__ __forceinline__ bool run_segment(const Cta& c, const mv::blk::Segment
       valid = (token & 15) < int(page & 255u);
       see = valid ? (uint64_t(by.y) << 32) | by.x : 0;
     }
-    // Weights of the thread's token against the references as they stand, into the weight tile (row = token) and, times `sign` 2^(-e), into the token's sums.  Returns the largest weight.
+    // Weights of the thread's token against the references as they stand, into the weight tile (row = token) and, times
+    // `sign` 2^(-e), into the token's sums.  Returns the largest weight.
     auto pass = [&](float sign, bool first) {
       float top = 0.f;
       const uint64_t vinv2 = mv::pack_f32x2(sign * vinv, sign * vinv);
