@@ -216,6 +216,61 @@ mv_status mv_rope_write_kv(const mv_plan* plan, const mv_attn_geom* geom, const 
                            const void* v, void* q_rot, void* k_rot, void* k_pages, void* v_pages,
                            void* cuda_stream);
 
+/* ---- Rotary forms ----------------------------------------------------------------------------------------------------
+ * mv_rope_write_kv and its relatives rotate whole heads in two halves with angles pos * rope_base^(-2i/head_dim).  Backbones
+ * differ in that: which elements are paired, how much of the head turns, and how the angles are stretched for contexts longer
+ * than those trained on.  A form says so; the calls with _form take it in place of geom->rope_base (which they do not read).
+ * With rotary_dim = R, pair i < R / 2 is (first + i, first + R/2 + i) as halves, (first + 2i, first + 2i + 1) as pairs, and
+ *   a' = A (a cos x - b sin x),  b' = A (b cos x + a sin x),  x = pos * theta[i],  A = amplitude;
+ * elements outside [first, first + R) are passed on as they are.  Angles and arithmetic as in mv_rope_write_kv (the products with
+ * A are rounded once more, to float). */
+typedef enum { MV_ROPE_HALVES = 0, MV_ROPE_PAIRS = 1 } mv_rope_layout;
+typedef struct {
+  int32_t layout;      /* mv_rope_layout                                                                     */
+  int32_t first;       /* first rotated element of a head, a multiple of 16                                  */
+  int32_t rotary_dim;  /* elements rotated, a multiple of 16, 16 .. head_dim - first                         */
+  float amplitude;     /* A above, greater than 0 and at most 1024                                           */
+  double theta[64];    /* angle per position of every pair, -1 .. 1; the first rotary_dim / 2 are read        */
+} mv_rope_form;
+
+/* How mv_rope_form_init stretches the angles theta_i = base^(-2i/R): */
+typedef enum {
+  MV_ROPE_PLAIN = 0,   /* not at all                                                                          */
+  MV_ROPE_LINEAR = 1,  /* theta_i / factor                                                                    */
+  MV_ROPE_BASE = 2,    /* with base * factor^(R / (R - 2)) for base: the slowest pair is stretched by factor, the fastest not */
+  MV_ROPE_RAMP = 3     /* by the turns n = length * theta_i / (2 pi) a pair makes over the length it was trained on: with
+                          w = (n - slow) / (fast - slow), held in [0, 1], w theta_i + (1 - w) theta_i / factor            */
+} mv_rope_scaling;
+
+/* Fills a form (host only).  factor is read unless the scaling is MV_ROPE_PLAIN; length, slow and fast with MV_ROPE_RAMP only.
+ * The struct may as well be filled, or changed, by the caller's own code.
+ * Errors: MV_ERR_INVALID_ARG (enums, base < 1, factor < 1, length <= 0, slow < 0, fast <= slow, amplitude),
+ * MV_ERR_UNSUPPORTED (first or rotary_dim not a multiple of 16, rotary_dim outside 16 .. 128, first < 0 or > 112). */
+mv_status mv_rope_form_init(mv_rope_form* form, int32_t layout, int32_t first, int32_t rotary_dim, double base, int32_t scaling,
+                            double factor, double length, double slow, double fast, float amplitude);
+
+/* The rotation by itself, and its backward pass: with backward = 0 q_out[t] = R(pos_id[t]) q[t] and k_out[t] = R(pos_id[t]) k[t],
+ * with backward = 1 the transposed map (the sine changes its sign), which turns the gradients of q_rot and k_rot, as
+ * mv_dag_prefill_attn_bwd gives them, into those of q and k.
+ *   pos_id   device int32 [n_tokens], positions -2^30 .. 2^30: mv_step_tables.pos_id, mv_plan_positions, or the caller's own
+ *   q, k     device, token t's heads at q + t * q_stride elements ([n_q_heads][head_dim], contiguous), k likewise: q and k may lie side by side
+ *            in the rows of one projection.  Either may be NULL with its output
+ *   q_out, k_out  device, with strides of their own; may be q and k with the same strides.  Otherwise no output may overlap an input
+ * geom: n_q_heads, n_kv_heads, head_dim and dtype are read.  Strides are multiples of 16 bytes and at least a token's heads;
+ * all tensors are 16-byte aligned.
+ * Errors: MV_ERR_INVALID_ARG, MV_ERR_UNSUPPORTED, MV_ERR_CUDA. */
+mv_status mv_rope_rotate(const mv_rope_form* form, const mv_attn_geom* geom, const int32_t* pos_id, int64_t n_tokens, int32_t backward,
+                         const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out, int64_t q_out_stride,
+                         void* k_out, int64_t k_out_stride, void* cuda_stream);
+
+/* Positions of the plan's new tokens on the device (int32 [n_new_tokens], part of the uploaded tables; valid as long as they are).
+ * Errors: MV_ERR_INVALID_ARG, MV_ERR_WORKSPACE (not uploaded). */
+mv_status mv_plan_positions(const mv_plan* plan, const int32_t** device_ptr);
+
+/* mv_rope_write_kv with a form.  Errors: its own, and MV_ERR_INVALID_ARG for a form that does not fit head_dim. */
+mv_status mv_rope_write_kv_form(const mv_plan* plan, const mv_attn_geom* geom, const mv_rope_form* form, const void* q, const void* k,
+                                const void* v, void* q_rot, void* k_rot, void* k_pages, void* v_pages, void* cuda_stream);
+
 /* Multi-branch decode attention (Eq. 2 with the DAG mask of Eq. 3 over a shared paged cache, Sec. 4.3
  * Fork / Join): for every row r (the single new token of a frontier node v) and query head h,
  *   out[r][h] = sum_j softmax_j(sm_scale * <q_rot[r][h], K_j>) V_j
@@ -339,6 +394,12 @@ mv_status mv_step_tables_read_status(const mv_step_tables* tables, void* cuda_st
  * dtype MV_BF16, head_dim 64 or 128; all tensors 16-byte aligned.  Errors: MV_ERR_INVALID_ARG, MV_ERR_UNSUPPORTED, MV_ERR_CUDA. */
 mv_status mv_rope_write_kv_fp8_blk(const mv_step_tables* tables, const mv_attn_geom* geom, const void* q, const void* k, const void* v,
                                    void* q_rot, void* k_rot, void* k_pages8, void* v_pages8, float* kv_scale, void* cuda_stream);
+
+/* mv_rope_write_kv_fp8_blk with a rotary form.  The rule of the K scale takes |k| times the form's amplitude (rounded to float) where that
+ * is above 1, so that a rotated element still fits.  Errors: its own, and MV_ERR_INVALID_ARG for a form that does not fit head_dim. */
+mv_status mv_rope_write_kv_fp8_blk_form(const mv_step_tables* tables, const mv_attn_geom* geom, const mv_rope_form* form, const void* q,
+                                        const void* k, const void* v, void* q_rot, void* k_rot, void* k_pages8, void* v_pages8,
+                                        float* kv_scale, void* cuda_stream);
 
 /* Decode attention over that cache: for every row r of the tables and query head h
  *   out[r][h] = sum_j softmax_j(sm_scale * <q_rot[r][h], K_j>) V_j

@@ -32,7 +32,8 @@ EXPORTS = ["mv_plan_dag", "mv_plan_bind_geometry", "mv_plan_table", "mv_plan_get
            "mv_launch_count", "mv_plan_read_status", "mv_dag_decode_attn_static",
            "mv_static_workspace_bytes", "mv_rope_write_kv_fp8", "mv_dag_decode_attn_fp8", "mv_step_tables_workspace_bytes",
            "mv_step_tables_build", "mv_step_tables_read_status", "mv_rope_write_kv_fp8_blk", "mv_decode_fp8_blk_workspace_bytes",
-           "mv_dag_decode_attn_fp8_blk", "mv_selftest_bounded_wait", "mv_selftest_tmap_cache",
+           "mv_dag_decode_attn_fp8_blk", "mv_rope_form_init", "mv_rope_rotate", "mv_plan_positions", "mv_rope_write_kv_form",
+           "mv_rope_write_kv_fp8_blk_form", "mv_selftest_bounded_wait", "mv_selftest_tmap_cache",
            "mv_sched_create", "mv_sched_destroy", "mv_sched_add_request", "mv_sched_step", "mv_sched_rows",
            "mv_sched_commit", "mv_sched_page_refs", "mv_sched_get_stats"]
 
@@ -77,6 +78,10 @@ class _StepTables(C.Structure):
         (n, C.c_void_p) for n in ("pos_id", "slot", "group_row_off", "group_ent_off", "group_tile_off", "entries", "counts")]
 
 
+class _RopeForm(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("first", C.c_int32), ("rotary_dim", C.c_int32), ("amplitude", C.c_float), ("theta", C.c_double * 64)]
+
+
 class _StepShape(C.Structure):
     _fields_ = [("n_nodes", C.c_int32), ("n_parents", C.c_int32), ("n_pages", C.c_int32), ("max_req_nodes", C.c_int32),
                 ("num_pages", C.c_int64)]
@@ -114,6 +119,12 @@ def _load():
     lib.mv_decode_fp8_blk_workspace_bytes.argtypes = [C.POINTER(_Geom)]
     lib.mv_decode_fp8_blk_workspace_bytes.restype = sz
     lib.mv_dag_decode_attn_fp8_blk.argtypes = [vp] * 8 + [sz, vp]
+    f64 = C.c_double
+    lib.mv_rope_form_init.argtypes = [C.POINTER(_RopeForm), i32, i32, i32, f64, i32, f64, f64, f64, f64, C.c_float]
+    lib.mv_rope_rotate.argtypes = [vp, vp, vp, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.mv_plan_positions.argtypes = [vp, C.POINTER(vp)]
+    lib.mv_rope_write_kv_form.argtypes = [vp, C.POINTER(_Geom)] + [vp] * 9
+    lib.mv_rope_write_kv_fp8_blk_form.argtypes = [vp] * 12
     lib.mv_static_workspace_bytes.argtypes = []
     lib.mv_static_workspace_bytes.restype = sz
     lib.mv_decode_step_staging_bytes.argtypes = [vp, C.POINTER(_Geom)]
@@ -418,16 +429,93 @@ def mv_step_tables_read_status(tables: StepTables, stream=None) -> int:
     return int(out.value)
 
 
-def mv_rope_write_kv_fp8_blk(tables: StepTables, geom: _Geom, q, k, v, q_rot, k_rot, k_pages8, v_pages8, kv_scale, stream=None):
+def _write_blk_args(tables: StepTables, geom: _Geom, q, k, v, q_rot, k_rot, k_pages8, v_pages8, kv_scale, stream):
     i, T = tables.index, _Torch
     s = _launch_stream(i, stream)
     hkv, d, blocks = geom.n_kv_heads, geom.head_dim, geom.num_pages * geom.n_kv_heads
     nq, nk, pool = tables.max_rows * geom.n_q_heads * d, tables.max_rows * hkv * d, blocks * 16 * d
-    _check(lib.mv_rope_write_kv_fp8_blk(
-        tables._ref, C.byref(geom), None if q is None else _arr(q, "q", T.bfloat16, nq, i), _arr(k, "k", T.bfloat16, nk, i),
-        _arr(v, "v", T.bfloat16, nk, i), None if q_rot is None else _arr(q_rot, "q_rot", T.bfloat16, nq, i),
-        None if k_rot is None else _arr(k_rot, "k_rot", T.bfloat16, nk, i), _arr(k_pages8, "k_pages8", T.uint8, pool, i),
-        _arr(v_pages8, "v_pages8", T.uint8, pool, i), _arr(kv_scale, "kv_scale", T.float32, blocks * 2, i), s), "mv_rope_write_kv_fp8_blk")
+    return (None if q is None else _arr(q, "q", T.bfloat16, nq, i), _arr(k, "k", T.bfloat16, nk, i),
+            _arr(v, "v", T.bfloat16, nk, i), None if q_rot is None else _arr(q_rot, "q_rot", T.bfloat16, nq, i),
+            None if k_rot is None else _arr(k_rot, "k_rot", T.bfloat16, nk, i), _arr(k_pages8, "k_pages8", T.uint8, pool, i),
+            _arr(v_pages8, "v_pages8", T.uint8, pool, i), _arr(kv_scale, "kv_scale", T.float32, blocks * 2, i), s)
+
+
+def mv_rope_write_kv_fp8_blk(tables: StepTables, geom: _Geom, q, k, v, q_rot, k_rot, k_pages8, v_pages8, kv_scale, stream=None):
+    a = _write_blk_args(tables, geom, q, k, v, q_rot, k_rot, k_pages8, v_pages8, kv_scale, stream)
+    _check(lib.mv_rope_write_kv_fp8_blk(tables._ref, C.byref(geom), *a), "mv_rope_write_kv_fp8_blk")
+
+
+def mv_rope_write_kv_fp8_blk_form(tables: StepTables, geom: _Geom, form: RopeForm, q, k, v, q_rot, k_rot, k_pages8, v_pages8, kv_scale, stream=None):
+    a = _write_blk_args(tables, geom, q, k, v, q_rot, k_rot, k_pages8, v_pages8, kv_scale, stream)
+    _check(lib.mv_rope_write_kv_fp8_blk_form(tables._ref, C.byref(geom), form._ref, *a), "mv_rope_write_kv_fp8_blk_form")
+
+
+# ---- rotary forms
+
+ROPE_HALVES, ROPE_PAIRS = 0, 1
+ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
+
+
+class RopeForm:
+    """How a backbone rotates (see ``mv_rope_form`` in the header): ``layout`` ROPE_HALVES or ROPE_PAIRS, ``rotary_dim`` elements from
+    ``first`` on, angles from ``base`` stretched by ``scaling``, or given as they are by ``theta``."""
+
+    def __init__(self, layout, rotary_dim, first=0, base=10000.0, scaling="plain", factor=1.0, length=0.0, slow=1.0, fast=32.0, amplitude=1.0,
+                 theta=None):
+        self.c_form = _RopeForm()
+        _check(lib.mv_rope_form_init(C.byref(self.c_form), int(layout), int(first), int(rotary_dim), float(base), ROPE_SCALING[scaling], float(factor),
+                                     float(length), float(slow), float(fast), float(amplitude)), "mv_rope_form_init")
+        if theta is not None:
+            if len(theta) != rotary_dim // 2:
+                raise ValueError(f"theta: {rotary_dim // 2} angles are needed, got {len(theta)}")
+            self.c_form.theta[:len(theta)] = [float(x) for x in theta]
+        self._ref = C.byref(self.c_form)
+
+    @property
+    def theta(self) -> np.ndarray:
+        return np.asarray(self.c_form.theta[:self.c_form.rotary_dim // 2])
+
+
+def _heads_at(t, name: str, n_tokens: int, heads: int, d: int, dtype, index: int):
+    """Pointer and token stride of a tensor [tokens][heads][head_dim] whose heads are contiguous; the tokens may be further apart."""
+    if (t is None or t.dim() != 3 or t.dtype is not dtype or t.get_device() != index or t.shape[0] < n_tokens or t.shape[1] != heads or t.shape[2] != d
+            or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d)):
+        raise ValueError(f"{name}: a tensor [{n_tokens}][{heads}][{d}] of {dtype} on cuda:{index} with contiguous heads is needed, got "
+                         + ("None" if t is None else f"{tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}"))
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * d)
+
+
+def mv_rope_rotate(form: RopeForm, geom: _Geom, positions, q, k, q_out, k_out, backward: bool = False, stream=None):
+    """Rotates q and k (either may be None) by ``positions``: an int32 CUDA tensor, StepTables, or an uploaded Plan whose tokens they are.
+    ``backward``: the transposed map, from the gradients of the rotated tensors to those of the raw ones."""
+    T = _torch()
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("q and k are both None")
+    i = some.get_device()
+    s = _launch_stream(i, stream)
+    n, keep = some.shape[0], None
+    if isinstance(positions, Plan):
+        ptr = C.c_void_p()
+        _check(lib.mv_plan_positions(positions.handle, C.byref(ptr)), "mv_plan_positions")
+        if positions.stats()["n_new_tokens"] != n:
+            raise ValueError(f"the plan has {positions.stats()['n_new_tokens']} new tokens, the tensors {n}")
+        pos = ptr.value
+    else:
+        keep = positions._keep[0] if isinstance(positions, StepTables) else positions
+        pos = _arr(keep, "positions", T.int32, n, i)
+    dt = T.bfloat16 if geom.dtype == MV_BF16 else T.float32
+    a = [(None, 0)] * 4
+    if q is not None:
+        a[0], a[2] = (_heads_at(t, m, n, geom.n_q_heads, geom.head_dim, dt, i) for t, m in ((q, "q"), (q_out, "q_out")))
+    if k is not None:
+        a[1], a[3] = (_heads_at(t, m, n, geom.n_kv_heads, geom.head_dim, dt, i) for t, m in ((k, "k"), (k_out, "k_out")))
+    _check(lib.mv_rope_rotate(form._ref, C.byref(geom), pos, n, 1 if backward else 0, *a[0], *a[1], *a[2], *a[3], s), "mv_rope_rotate")
+
+
+def mv_rope_write_kv_form(plan: Plan, geom: _Geom, form: RopeForm, q, k, v, q_rot, k_rot, k_pages, v_pages, stream=None):
+    _check(lib.mv_rope_write_kv_form(plan.handle, C.byref(geom), form._ref, _ptr(q), _ptr(k), _ptr(v), _ptr(q_rot), _ptr(k_rot),
+                                     _ptr(k_pages), _ptr(v_pages), _stream_ptr(stream)), "mv_rope_write_kv_form")
 
 
 def mv_decode_fp8_blk_workspace_bytes(geom: _Geom) -> int:

@@ -68,6 +68,13 @@ extern "C" mv_status mv_plan_upload(mv_plan* P, void* device_buf, size_t device_
   return MV_OK;
 }
 
+extern "C" mv_status mv_plan_positions(const mv_plan* P, const int32_t** device_ptr) {
+  if (!P || !P->valid || !device_ptr) return MV_ERR_INVALID_ARG;
+  if (!P->device_buf) return MV_ERR_WORKSPACE;
+  *device_ptr = mv::table<int32_t>(P, P->layout.pos_id);
+  return MV_OK;
+}
+
 extern "C" void mv_plan_destroy(mv_plan* P) {
   if (!P) return;
   if (P->pinned) {

@@ -32,6 +32,67 @@ __device__ __forceinline__ void rope_cos_sin(int pos, double theta, float& c, fl
   c = ((k + 1) & 2) ? -cc : cc;
 }
 
+// ---- rotary forms (mv_rope_form): which elements of a head make up a pair, and what is left alone
+//
+// A head is worked on in pieces: two vectors of W elements at lo and hi.  Pieces c = 0, W, 2 W, .. below half (the number of
+// pairs) hold the pairs c .. c + W - 1: as halves, element first + i goes with first + half + i; as pairs, first + 2 i goes with its
+// neighbour.  The pieces behind hold the elements outside the rotated part.  first and 2 half are multiples of 16, so no piece
+// straddles a border for W up to 8.
+struct FormTable {
+  ThetaTable t;
+  float amplitude;
+  int first, half, pairs;  // pairs: 1 = neighbours, 0 = halves
+};
+
+inline bool form_ok(const mv_rope_form* f, int head_dim) {
+  if (!f || (f->layout != MV_ROPE_HALVES && f->layout != MV_ROPE_PAIRS)) return false;
+  if (f->first < 0 || f->rotary_dim < 16 || (f->first & 15) || (f->rotary_dim & 15) || f->rotary_dim > head_dim - f->first) return false;
+  if (!(f->amplitude > 0.f) || !(f->amplitude <= 1024.f)) return false;
+  for (int i = 0; i < f->rotary_dim / 2; ++i)
+    if (!(f->theta[i] >= -1.0 && f->theta[i] <= 1.0)) return false;
+  return true;
+}
+inline FormTable form_table(const mv_rope_form& f) {
+  FormTable r{};
+  for (int i = 0; i < f.rotary_dim / 2; ++i) r.t.theta[i] = f.theta[i];
+  r.amplitude = f.amplitude;
+  r.first = f.first;
+  r.half = f.rotary_dim / 2;
+  r.pairs = f.layout == MV_ROPE_PAIRS ? 1 : 0;
+  return r;
+}
+
+struct Piece {
+  int lo, hi;
+  bool turns;
+};
+template <int W>
+__device__ __forceinline__ Piece piece_at(const FormTable& f, int c) {
+  if (c < f.half) return f.pairs ? Piece{f.first + 2 * c, f.first + 2 * c + W, true} : Piece{f.first + c, f.first + f.half + c, true};
+  const int u = 2 * (c - f.half), e = u < f.first ? u : u + 2 * f.half;
+  return Piece{e, e + W, false};
+}
+// One pair turned.  The roundings are spelt out, so that every kernel that turns the same pair gets the same bits.
+__device__ __forceinline__ void turn_pair(float& a, float& b, float c, float s) {
+  const float x = a;
+  a = __fmaf_rn(x, c, -__fmul_rn(b, s));
+  b = __fmaf_rn(b, c, __fmul_rn(x, s));
+}
+// the pairs of a piece turned; cs, sn: cosines and sines of pair c and those behind it (amplitude included)
+template <int W>
+__device__ __forceinline__ void turn_piece(bool pairs, float (&lo)[W], float (&hi)[W], const float* cs, const float* sn) {
+  if (pairs) {
+#pragma unroll
+    for (int n = 0; n < W; n += 2) {
+      turn_pair(lo[n], lo[n + 1], cs[n / 2], sn[n / 2]);
+      turn_pair(hi[n], hi[n + 1], cs[W / 2 + n / 2], sn[W / 2 + n / 2]);
+    }
+  } else {
+#pragma unroll
+    for (int n = 0; n < W; ++n) turn_pair(lo[n], hi[n], cs[n], sn[n]);
+  }
+}
+
 // the table for head_dim d
 inline ThetaTable theta_table(double rope_base, int d) {
   ThetaTable tt{};

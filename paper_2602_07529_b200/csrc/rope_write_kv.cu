@@ -9,6 +9,8 @@
 //
 // HBM-bound elementwise kernel: one or four tokens per CTA, 16-byte vector loads and stores, the cos/sin
 // rows of the CTA's tokens are computed once into shared memory and reused by all heads.
+#include <type_traits>
+
 #include "common.cuh"
 #include "rope.cuh"
 #include "trace.h"
@@ -17,6 +19,9 @@ namespace {
 
 using mv::rope_cos_sin;
 using mv::ThetaTable;
+
+template <bool FORM>
+using TableOf = std::conditional_t<FORM, mv::FormTable, ThetaTable>;
 
 template <typename T>
 struct Vec16;  // 16 bytes of T
@@ -68,13 +73,14 @@ __device__ __forceinline__ void store_e4m3(unsigned char* dst, const float (&x)[
 // loads of phase 2 are already in flight; phase 2: 16-byte units of q, k (rotated) and v (copied) stream through.
 // FP8: the pools hold 8-bit floats (4 exponent, 3 mantissa bits), [pages][KV heads][16 tokens][head_dim bytes]; a value is
 // stored as round(x / scale[head]), saturating (kv_scale = the K scales of all heads, then the V scales).
-template <typename T, int D, int TPC, bool FP8 = false>
+// FORM: pairs, rotated part and angles as the form says (rope.cuh); without it whole heads in halves.
+template <typename T, int D, int TPC, bool FP8 = false, bool FORM = false>
 // q_rot may be q and k_rot may be k (rotation in place), so those four carry no __restrict__.
 __global__ void __launch_bounds__(256) rope_write_kv_kernel(const T* q, const T* k, const T* __restrict__ v, T* q_rot, T* k_rot,
                                                             T* __restrict__ k_pages,
                                                             T* __restrict__ v_pages, const int32_t* __restrict__ pos_id,
                                                             const int64_t* __restrict__ slot, int n_tok, int Hq, int Hkv,
-                                                            const __grid_constant__ ThetaTable tt, const float* __restrict__ kv_scale = nullptr,
+                                                            const __grid_constant__ TableOf<FORM> tt, const float* __restrict__ kv_scale = nullptr,
                                                             int64_t num_pages_dbg = 0, int32_t* status_dbg = nullptr) {
   constexpr int HALF = D / 2;
   constexpr int N = Vec16<T>::N;
@@ -91,7 +97,13 @@ __global__ void __launch_bounds__(256) rope_write_kv_kernel(const T* q, const T*
   for (int x = threadIdx.x; x < n_here * HALF; x += blockDim.x) {
     const int tl = x / HALF, i = x % HALF;
     float c, s;
-    rope_cos_sin(__ldg(pos_id + t0 + tl), tt.theta[i], c, s);
+    if constexpr (FORM) {
+      rope_cos_sin(__ldg(pos_id + t0 + tl), tt.t.theta[i], c, s);
+      c *= tt.amplitude;
+      s *= tt.amplitude;
+    } else {
+      rope_cos_sin(__ldg(pos_id + t0 + tl), tt.theta[i], c, s);
+    }
     cs[tl][i] = c;
     sn[tl][i] = s;
     if (i == 0) {
@@ -143,58 +155,71 @@ __global__ void __launch_bounds__(256) rope_write_kv_kernel(const T* q, const T*
     const int h = uu / CH, c = uu % CH;
     const T* src = is_q ? q + (t * Hq + h) * D : k + (t * Hkv + h) * D;
     float lo[N], hi[N], olo[N], ohi[N];
-    Vec16<T>::load(src + c * N, lo);
-    Vec16<T>::load(src + HALF + c * N, hi);
+    int e0 = c * N, e1 = HALF + c * N;
+    bool turns = true;
+    if constexpr (FORM) {
+      const mv::Piece p = mv::piece_at<N>(tt, c * N);
+      e0 = p.lo;
+      e1 = p.hi;
+      turns = p.turns;
+    }
+    Vec16<T>::load(src + e0, lo);
+    Vec16<T>::load(src + e1, hi);
+    if constexpr (FORM) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float cc = cs[tl][c * N + i], ss = sn[tl][c * N + i];
-      olo[i] = lo[i] * cc - hi[i] * ss;
-      ohi[i] = hi[i] * cc + lo[i] * ss;
+      for (int i = 0; i < N; ++i) {
+        olo[i] = lo[i];
+        ohi[i] = hi[i];
+      }
+      if (turns) mv::turn_piece<N>(tt.pairs != 0, olo, ohi, &cs[tl][c * N], &sn[tl][c * N]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float cc = cs[tl][c * N + i], ss = sn[tl][c * N + i];
+        olo[i] = lo[i] * cc - hi[i] * ss;
+        ohi[i] = hi[i] * cc + lo[i] * ss;
+      }
     }
     if (is_q) {
       T* dst = q_rot + (t * Hq + h) * D;
-      Vec16<T>::store(dst + c * N, olo);
-      Vec16<T>::store(dst + HALF + c * N, ohi);
+      Vec16<T>::store(dst + e0, olo);
+      Vec16<T>::store(dst + e1, ohi);
       continue;
     }
     if (FP8 && pool_ok) {
       const float inv = 1.f / __ldg(kv_scale + h);
       unsigned char* dst = reinterpret_cast<unsigned char*>(k_pages) + (page * Hkv + h) * (16 * D) + off * D;
-      store_e4m3<N>(dst + c * N, olo, inv);
-      store_e4m3<N>(dst + HALF + c * N, ohi, inv);
+      store_e4m3<N>(dst + e0, olo, inv);
+      store_e4m3<N>(dst + e1, ohi, inv);
     } else if (!FP8 && k_pages != nullptr && pool_ok) {
       // pool element (page, head, token, e) lives in 64-element column block e / 64 of the (page, head) block
       T* dst = k_pages + (page * Hkv + h) * (16 * D) + off * 64;
-      const int e0 = c * N, e1 = HALF + c * N;
       Vec16<T>::store(dst + (e0 >> 6) * 1024 + (e0 & 63), olo);
       Vec16<T>::store(dst + (e1 >> 6) * 1024 + (e1 & 63), ohi);
     }
     if (k_rot != nullptr) {
       T* dst2 = k_rot + (t * Hkv + h) * D;
-      Vec16<T>::store(dst2 + c * N, olo);
-      Vec16<T>::store(dst2 + HALF + c * N, ohi);
+      Vec16<T>::store(dst2 + e0, olo);
+      Vec16<T>::store(dst2 + e1, ohi);
     }
   }
 }
 
 inline int32_t* dbg_status(const mv_plan* P) { return const_cast<int32_t*>(mv::table<int32_t>(P, P->layout.sched)) + 2; }
 
-template <typename T, int D>
-mv_status launch_d(const mv_plan* P, const mv_attn_geom* g, const void* q, const void* k, const void* v, void* q_rot,
+template <typename T, int D, bool FORM>
+mv_status launch_d(const mv_plan* P, const mv_attn_geom* g, const TableOf<FORM>& tt, const void* q, const void* k, const void* v, void* q_rot,
                    void* k_rot, void* k_pages, void* v_pages, cudaStream_t st) {
   const int n = int(P->stats.n_new_tokens);
   const int32_t* pos = mv::table<int32_t>(P, P->layout.pos_id);
   const int64_t* slot = mv::table<int64_t>(P, P->layout.slot);
-  ThetaTable tt{};
-  const double c = -2.0 * log2(g->rope_base) / double(D);
-  for (int i = 0; i < D / 2; ++i) tt.theta[i] = exp2(double(i) * c);  // base^(-2i/d)
   // few tokens (a decode step): one token per CTA spreads them over the SMs; many (prefill, history): four per CTA
   // amortise the set-up and keep more 16-byte units in flight per thread
   if (n < 2048)
-    rope_write_kv_kernel<T, D, 1><<<n, 256, 0, st>>>((const T*)q, (const T*)k, (const T*)v, (T*)q_rot, (T*)k_rot, (T*)k_pages,
+    rope_write_kv_kernel<T, D, 1, false, FORM><<<n, 256, 0, st>>>((const T*)q, (const T*)k, (const T*)v, (T*)q_rot, (T*)k_rot, (T*)k_pages,
                                                      (T*)v_pages, pos, slot, n, g->n_q_heads, g->n_kv_heads, tt, nullptr, g->num_pages, dbg_status(P));
   else
-    rope_write_kv_kernel<T, D, 4><<<(n + 3) / 4, 256, 0, st>>>((const T*)q, (const T*)k, (const T*)v, (T*)q_rot, (T*)k_rot,
+    rope_write_kv_kernel<T, D, 4, false, FORM><<<(n + 3) / 4, 256, 0, st>>>((const T*)q, (const T*)k, (const T*)v, (T*)q_rot, (T*)k_rot,
                                                                (T*)k_pages, (T*)v_pages, pos, slot, n, g->n_q_heads,
                                                                g->n_kv_heads, tt, nullptr, g->num_pages, dbg_status(P));
   mv::g_launches++;
@@ -203,10 +228,16 @@ mv_status launch_d(const mv_plan* P, const mv_attn_geom* g, const void* q, const
 }
 
 template <typename T>
-mv_status launch(const mv_plan* P, const mv_attn_geom* g, const void* q, const void* k, const void* v, void* q_rot,
+mv_status launch(const mv_plan* P, const mv_attn_geom* g, const mv_rope_form* form, const void* q, const void* k, const void* v, void* q_rot,
                  void* k_rot, void* k_pages, void* v_pages, cudaStream_t st) {
-  return g->head_dim == 128 ? launch_d<T, 128>(P, g, q, k, v, q_rot, k_rot, k_pages, v_pages, st)
-                            : launch_d<T, 64>(P, g, q, k, v, q_rot, k_rot, k_pages, v_pages, st);
+  if (form) {
+    const mv::FormTable ft = mv::form_table(*form);
+    return g->head_dim == 128 ? launch_d<T, 128, true>(P, g, ft, q, k, v, q_rot, k_rot, k_pages, v_pages, st)
+                              : launch_d<T, 64, true>(P, g, ft, q, k, v, q_rot, k_rot, k_pages, v_pages, st);
+  }
+  const ThetaTable tt = mv::theta_table(g->rope_base, g->head_dim);
+  return g->head_dim == 128 ? launch_d<T, 128, false>(P, g, tt, q, k, v, q_rot, k_rot, k_pages, v_pages, st)
+                            : launch_d<T, 64, false>(P, g, tt, q, k, v, q_rot, k_rot, k_pages, v_pages, st);
 }
 
 template <int TPC>
@@ -243,10 +274,11 @@ extern "C" mv_status mv_rope_write_kv_fp8(const mv_plan* P, const mv_attn_geom* 
   return cudaGetLastError() == cudaSuccess ? MV_OK : MV_ERR_CUDA;
 }
 
-extern "C" mv_status mv_rope_write_kv(const mv_plan* P, const mv_attn_geom* g, const void* q, const void* k,
-                                      const void* v, void* q_rot, void* k_rot, void* k_pages, void* v_pages,
-                                      void* cuda_stream) {
-  mv::NvtxRange nvtx_range("mv_rope_write_kv");
+namespace {
+
+// mv_rope_write_kv, with a form in place of geom->rope_base where there is one
+mv_status write_kv(const mv_plan* P, const mv_attn_geom* g, const mv_rope_form* form, const void* q, const void* k, const void* v,
+                   void* q_rot, void* k_rot, void* k_pages, void* v_pages, void* cuda_stream) {
   if (!P || !P->valid) return MV_ERR_INVALID_ARG;
   mv_status st = mv::check_geom(g);
   if (st != MV_OK) return st;
@@ -257,8 +289,28 @@ extern "C" mv_status mv_rope_write_kv(const mv_plan* P, const mv_attn_geom* g, c
   if (!k_pages && !k_rot) return MV_ERR_INVALID_ARG;
   if ((q == nullptr) != (q_rot == nullptr)) return MV_ERR_INVALID_ARG;
   if (k_pages && P->stats.max_page_id >= g->num_pages) return MV_ERR_INVALID_ARG;
-  if (g->rope_base <= 0.0) return MV_ERR_INVALID_ARG;
+  if (!form && g->rope_base <= 0.0) return MV_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  return g->dtype == MV_BF16 ? launch<__nv_bfloat16>(P, g, q, k, v, q_rot, k_rot, k_pages, v_pages, s)
-                             : launch<float>(P, g, q, k, v, q_rot, k_rot, k_pages, v_pages, s);
+  return g->dtype == MV_BF16 ? launch<__nv_bfloat16>(P, g, form, q, k, v, q_rot, k_rot, k_pages, v_pages, s)
+                             : launch<float>(P, g, form, q, k, v, q_rot, k_rot, k_pages, v_pages, s);
+}
+
+}  // namespace
+
+extern "C" mv_status mv_rope_write_kv(const mv_plan* P, const mv_attn_geom* g, const void* q, const void* k,
+                                      const void* v, void* q_rot, void* k_rot, void* k_pages, void* v_pages,
+                                      void* cuda_stream) {
+  mv::NvtxRange nvtx_range("mv_rope_write_kv");
+  return write_kv(P, g, nullptr, q, k, v, q_rot, k_rot, k_pages, v_pages, cuda_stream);
+}
+
+extern "C" mv_status mv_rope_write_kv_form(const mv_plan* P, const mv_attn_geom* g, const mv_rope_form* form, const void* q, const void* k,
+                                           const void* v, void* q_rot, void* k_rot, void* k_pages, void* v_pages, void* cuda_stream) {
+  mv::NvtxRange nvtx_range("mv_rope_write_kv_form");
+  const mv_status st = mv::check_geom(g);
+  if (st != MV_OK) return st;
+  if (!mv::form_ok(form, g->head_dim)) return MV_ERR_INVALID_ARG;
+  for (const void* p : {q, k, v, static_cast<const void*>(q_rot), static_cast<const void*>(k_rot), static_cast<const void*>(k_pages), static_cast<const void*>(v_pages)})
+    if ((reinterpret_cast<uintptr_t>(p) & 15) != 0) return MV_ERR_INVALID_ARG;
+  return write_kv(P, g, form, q, k, v, q_rot, k_rot, k_pages, v_pages, cuda_stream);
 }
