@@ -423,6 +423,24 @@ mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* tables, const mv_attn
                                      const void* v_pages8, const float* kv_scale, void* out, void* workspace,
                                      size_t workspace_bytes, void* cuda_stream);
 
+/* Copies pages inside pools: page dst[i] of every pool becomes page src[i], for i < n (a fork that goes on writing gets a copy of
+ * the partly filled last page; a compacted pool moves its upper pages down: mv_sched_clone_request and mv_sched_compact make
+ * such lists).  One launch for all pools, K and V and scales of any number of layers.
+ *   pools    host, read during the call: base address (device) and bytes of a page of each, both multiples of 4 (of 16: faster);
+ *            a page of the 16-bit pools has n_kv_heads * head_dim * 32 bytes, of the 8-bit pools half as many, of kv_scale n_kv_heads * 8
+ *   src, dst device int32 [n]; pages outside [0, num_pages) are skipped, and *status becomes MV_ERR_INVALID_ARG.
+ *            No page may be a destination twice, nor a destination and the source of another pair (its content is then undefined)
+ *   count    device int32 [1], or NULL: only the first min(n, *count) pairs are copied, so a captured call can do any number up to n
+ *   status   device int32 [1], or NULL (counts + 4 of tables will do); not touched unless something is wrong
+ * Errors: MV_ERR_INVALID_ARG, MV_ERR_UNSUPPORTED (n_pools > MV_PAGES_MAX_POOLS, pages above 2 GB, more than 2^31 blocks of work), MV_ERR_CUDA. */
+#define MV_PAGES_MAX_POOLS 256
+typedef struct {
+  void* base;
+  int64_t page_bytes;
+} mv_page_pool;
+mv_status mv_pages_copy(const mv_page_pool* pools, int32_t n_pools, int64_t num_pages, const int32_t* src, const int32_t* dst, int32_t n,
+                        const int32_t* count, int32_t* status, void* cuda_stream);
+
 /* Decode attention for callers that cannot allocate device memory.  (The paper has no counterpart: this is
  * a packaging variant of mv_dag_decode_attn, same arithmetic, same kernels.)
  *

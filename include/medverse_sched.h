@@ -10,8 +10,8 @@
  *     token per step each; the marking advances only when all of them are complete (Sec. 3.3, execution loop).
  *   - Fork: siblings read the same pages; only a reference count changes.  Join: the step reads the union of its
  *     predecessors' page lists; nothing is copied (Sec. 4.3, Phase II).
- *   - Pages are handed out lowest free id first.  A page's count is one for the node that owns it plus one per running
- *     transition that reads it; a request's pages return to the pool when nothing of it is running or enabled.
+ *   - Pages are handed out lowest free id first.  A page's count is one for every node that owns it (one, or one per clone) plus one
+ *     per running transition that reads it; a request's pages return to the pool when nothing of it is running or enabled.
  *
  * All pointers are HOST pointers.  The arrays behind an emitted batch, and behind mv_sched_rows, belong to the
  * scheduler and stay valid until the next mv_sched_step after a commit, or mv_sched_destroy.  Not thread safe.
@@ -72,6 +72,22 @@ mv_status mv_sched_rows(const mv_sched* sched, const int32_t** request_ids, cons
  * next frontier, or, with nothing enabled, returns all its pages.
  * Errors: MV_ERR_INVALID_ARG (no batch emitted since the last commit). */
 mv_status mv_sched_commit(mv_sched* sched, const uint8_t* finished);
+
+/* A second request that goes on from where request_id stands (several continuations sampled from one state): same net, marking
+ * and lengths.  Complete steps and full pages are shared by reference; of every running transition whose last page is partly
+ * filled the clone gets a page of its own, and the pair (src, dst) is listed: copy those pages (mv_pages_copy, every pool) before
+ * the next step writes.  src, dst: [capacity], *n pairs (at most one per running transition).
+ * Not allowed between mv_sched_step and its mv_sched_commit.
+ * Errors: MV_ERR_INVALID_ARG (also a request that is done), MV_ERR_PAGE_CAPACITY, MV_ERR_WORKSPACE (capacity; *n says what is needed).
+ * On an error nothing changes. */
+mv_status mv_sched_clone_request(mv_sched* sched, int32_t request_id, int32_t* new_request_id, int32_t capacity, int32_t* src, int32_t* dst,
+                                 int32_t* n);
+
+/* Moves pages in use to lower free ones, the highest first, until every page in use lies below every free one or max_moves pages
+ * have moved.  The scheduler's own lists change at once; copy page src[i] to dst[i] (i < *n <= max_moves) in every pool before the
+ * next step (no page is in both lists).  *top (may be null): one more than the highest page then in use, so what lies
+ * from there on may be given back.  Not allowed between mv_sched_step and its mv_sched_commit.  Errors: MV_ERR_INVALID_ARG. */
+mv_status mv_sched_compact(mv_sched* sched, int32_t max_moves, int32_t* src, int32_t* dst, int32_t* n, int32_t* top);
 
 /* Reference counts of the given pages (0 = free).  Errors: MV_ERR_INVALID_ARG (a page id out of range). */
 mv_status mv_sched_page_refs(const mv_sched* sched, const int32_t* page_ids, int32_t n, int32_t* refs);

@@ -33,7 +33,7 @@ EXPORTS = ["mv_plan_dag", "mv_plan_bind_geometry", "mv_plan_table", "mv_plan_get
            "mv_static_workspace_bytes", "mv_rope_write_kv_fp8", "mv_dag_decode_attn_fp8", "mv_step_tables_workspace_bytes",
            "mv_step_tables_build", "mv_step_tables_read_status", "mv_rope_write_kv_fp8_blk", "mv_decode_fp8_blk_workspace_bytes",
            "mv_dag_decode_attn_fp8_blk", "mv_rope_form_init", "mv_rope_rotate", "mv_plan_positions", "mv_rope_write_kv_form",
-           "mv_rope_write_kv_fp8_blk_form", "mv_selftest_bounded_wait", "mv_selftest_tmap_cache",
+           "mv_rope_write_kv_fp8_blk_form", "mv_pages_copy", "mv_sched_clone_request", "mv_sched_compact", "mv_selftest_bounded_wait", "mv_selftest_tmap_cache",
            "mv_sched_create", "mv_sched_destroy", "mv_sched_add_request", "mv_sched_step", "mv_sched_rows",
            "mv_sched_commit", "mv_sched_page_refs", "mv_sched_get_stats"]
 
@@ -82,6 +82,10 @@ class _RopeForm(C.Structure):
     _fields_ = [("layout", C.c_int32), ("first", C.c_int32), ("rotary_dim", C.c_int32), ("amplitude", C.c_float), ("theta", C.c_double * 64)]
 
 
+class _PagePool(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("page_bytes", C.c_int64)]
+
+
 class _StepShape(C.Structure):
     _fields_ = [("n_nodes", C.c_int32), ("n_parents", C.c_int32), ("n_pages", C.c_int32), ("max_req_nodes", C.c_int32),
                 ("num_pages", C.c_int64)]
@@ -125,6 +129,9 @@ def _load():
     lib.mv_plan_positions.argtypes = [vp, C.POINTER(vp)]
     lib.mv_rope_write_kv_form.argtypes = [vp, C.POINTER(_Geom)] + [vp] * 9
     lib.mv_rope_write_kv_fp8_blk_form.argtypes = [vp] * 12
+    lib.mv_pages_copy.argtypes = [vp, i32, i64, vp, vp, i32, vp, vp, vp]
+    lib.mv_sched_clone_request.argtypes = [vp, i32, C.POINTER(i32), i32, vp, vp, C.POINTER(i32)]
+    lib.mv_sched_compact.argtypes = [vp, i32, vp, vp, C.POINTER(i32), C.POINTER(i32)]
     lib.mv_static_workspace_bytes.argtypes = []
     lib.mv_static_workspace_bytes.restype = sz
     lib.mv_decode_step_staging_bytes.argtypes = [vp, C.POINTER(_Geom)]
@@ -533,6 +540,37 @@ def mv_dag_decode_attn_fp8_blk(tables: StepTables, geom: _Geom, q_rot, k_pages8,
         _arr(out, "out", T.bfloat16, nq, i), _arr(workspace, "workspace", T.uint8, 0, i), workspace.numel(), s), "mv_dag_decode_attn_fp8_blk")
 
 
+# ---- pages
+
+class PagePools:
+    """Pools whose pages ``mv_pages_copy`` copies: contiguous CUDA tensors with the pages as their first dimension, as many in each (K, V
+    and scales of any number of layers).  They are kept alive here."""
+
+    def __init__(self, pools):
+        self._keep = list(pools)
+        if not self._keep:
+            raise ValueError("no pools")
+        self.index, self.num_pages = self._keep[0].get_device(), self._keep[0].shape[0]
+        for j, t in enumerate(self._keep):
+            if t.get_device() != self.index or self.index < 0 or t.shape[0] != self.num_pages or not t.is_contiguous():
+                raise ValueError(f"pools[{j}]: a contiguous tensor of {self.num_pages} pages on cuda:{max(0, self.index)} is needed, got "
+                                 f"{tuple(t.shape)} on {t.device}, strides {t.stride()}")
+        self.c_pools = (_PagePool * len(self._keep))(*[_PagePool(t.data_ptr(), t.numel() // max(1, self.num_pages) * t.element_size()) for t in self._keep])
+
+
+def mv_pages_copy(pools: PagePools, src, dst, count=None, status=None, stream=None):
+    """Page ``dst[i]`` of every pool becomes page ``src[i]`` (int32 CUDA tensors of one length).  ``count``, ``status``: int32 CUDA tensors
+    of one element or None (see the header)."""
+    i, T = pools.index, _torch()
+    s = _launch_stream(i, stream)
+    n = src.numel()
+    if dst.numel() != n:
+        raise ValueError(f"src has {n} pages, dst {dst.numel()}")
+    _check(lib.mv_pages_copy(pools.c_pools, len(pools.c_pools), pools.num_pages, _arr(src, "src", T.int32, n, i), _arr(dst, "dst", T.int32, n, i), n,
+                             None if count is None else _arr(count, "count", T.int32, 1, i),
+                             None if status is None else _arr(status, "status", T.int32, 1, i), s), "mv_pages_copy")
+
+
 def mv_static_workspace_bytes() -> int:
     return int(lib.mv_static_workspace_bytes())
 
@@ -673,6 +711,24 @@ class Scheduler:
         if finished is not None:
             f = np.ascontiguousarray(np.asarray(finished, dtype=np.uint8))
         _check(lib.mv_sched_commit(self._h, f.ctypes.data if f is not None else None), "mv_sched_commit")
+
+    def clone_request(self, request_id: int):
+        """(id of the clone, pages to copy from, pages to copy to)."""
+        rid, n = C.c_int32(-1), C.c_int32(0)
+        st = lib.mv_sched_clone_request(self._h, int(request_id), C.byref(rid), 0, None, None, C.byref(n))
+        src, dst = np.zeros(n.value, np.int32), np.zeros(n.value, np.int32)
+        if STATUS_NAMES.get(st) == "MV_ERR_WORKSPACE":
+            st = lib.mv_sched_clone_request(self._h, int(request_id), C.byref(rid), n.value, src.ctypes.data, dst.ctypes.data, C.byref(n))
+        _check(st, "mv_sched_clone_request")
+        return int(rid.value), src, dst
+
+    def compact(self, max_moves: int):
+        """(pages to copy from, pages to copy to, one more than the highest page in use)."""
+        src, dst = np.zeros(max(0, max_moves), np.int32), np.zeros(max(0, max_moves), np.int32)
+        n, top = C.c_int32(0), C.c_int32(0)
+        _check(lib.mv_sched_compact(self._h, int(max_moves), src.ctypes.data if src.size else None, dst.ctypes.data if dst.size else None, C.byref(n),
+                                    C.byref(top)), "mv_sched_compact")
+        return src[:n.value].copy(), dst[:n.value].copy(), int(top.value)
 
     def page_refs(self, pages) -> np.ndarray:
         p = _i32(pages)

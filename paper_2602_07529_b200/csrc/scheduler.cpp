@@ -282,6 +282,69 @@ extern "C" mv_status mv_sched_commit(mv_sched* s, const uint8_t* finished) {
   return MV_OK;
 }
 
+extern "C" mv_status mv_sched_clone_request(mv_sched* s, int32_t request_id, int32_t* new_request_id, int32_t capacity, int32_t* src,
+                                            int32_t* dst, int32_t* n) {
+  if (!s || !new_request_id || !n || capacity < 0 || (capacity > 0 && (!src || !dst)) || s->pending) return MV_ERR_INVALID_ARG;
+  if (request_id < 0 || size_t(request_id) >= s->requests.size() || s->requests[size_t(request_id)].done) return MV_ERR_INVALID_ARG;
+  Request rq = s->requests[size_t(request_id)];
+  int32_t need = 0;
+  for (int32_t t : rq.running) need += (rq.written[size_t(t)] % s->page_size) != 0;
+  if (need > capacity) {
+    *n = need;
+    return MV_ERR_WORKSPACE;
+  }
+  if (size_t(need) > s->free_pages.size()) return MV_ERR_PAGE_CAPACITY;
+  int32_t k = 0;
+  for (int v = 0; v < rq.n; ++v) {
+    std::vector<int32_t>& pages = rq.pages[size_t(v)];
+    const int32_t w = rq.written[size_t(v)];
+    const bool split = w > 0 && w % s->page_size != 0;  // running, its last page goes on being written
+    for (size_t i = 0; i < pages.size(); ++i) {
+      if (split && i + 1 == pages.size()) {
+        src[k] = pages[i];
+        dst[k] = pages[i] = s->alloc();
+        ++k;
+      } else {
+        s->refs[size_t(pages[i])]++;
+      }
+    }
+  }
+  for (int32_t t : rq.running) s->hold_view(rq, t, +1);
+  s->requests.push_back(std::move(rq));
+  s->stats.requests_live++;
+  *new_request_id = int32_t(s->requests.size()) - 1;
+  *n = k;
+  return MV_OK;
+}
+
+extern "C" mv_status mv_sched_compact(mv_sched* s, int32_t max_moves, int32_t* src, int32_t* dst, int32_t* n, int32_t* top) {
+  if (!s || max_moves < 0 || (max_moves > 0 && (!src || !dst)) || !n || s->pending) return MV_ERR_INVALID_ARG;
+  std::vector<int32_t> to(size_t(s->num_pages), -1);  // where a page goes
+  int32_t lo = 0, hi = s->num_pages - 1, k = 0;
+  for (;;) {
+    while (lo < s->num_pages && s->refs[size_t(lo)] != 0) ++lo;
+    while (hi >= 0 && s->refs[size_t(hi)] == 0) --hi;
+    if (lo >= hi || k == max_moves) break;
+    src[k] = hi;
+    dst[k++] = lo;
+    to[size_t(hi)] = lo;
+    s->refs[size_t(lo)] = s->refs[size_t(hi)];
+    s->refs[size_t(hi)] = 0;
+  }
+  if (k > 0) {
+    for (Request& rq : s->requests)
+      for (auto& pages : rq.pages)
+        for (int32_t& p : pages)
+          if (to[size_t(p)] >= 0) p = to[size_t(p)];
+    s->free_pages = {};
+    for (int32_t p = 0; p < s->num_pages; ++p)
+      if (s->refs[size_t(p)] == 0) s->free_pages.push(p);
+  }
+  *n = k;
+  if (top) *top = hi + 1;
+  return MV_OK;
+}
+
 extern "C" mv_status mv_sched_page_refs(const mv_sched* s, const int32_t* page_ids, int32_t n, int32_t* refs) {
   if (!s || n < 0 || (n > 0 && (!page_ids || !refs))) return MV_ERR_INVALID_ARG;
   for (int32_t i = 0; i < n; ++i) {

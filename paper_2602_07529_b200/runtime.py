@@ -30,6 +30,13 @@ def pool_tokens(pool, slot):
     return x.reshape(x.shape[0], x.shape[1], -1)
 
 
+def copy_pages(pools, src, dst, stream=None):
+    """Copies pages in every pool, from lists on the host (what ``Scheduler.clone_request`` and ``Scheduler.compact`` return)."""
+    dev = pools[0].device
+    up = lambda x: torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(dev)
+    B.mv_pages_copy(B.PagePools(pools), up(src), up(dst), stream=stream)
+
+
 def _dev_bytes(n: int, device):
     """256-byte aligned uint8 scratch of at least n bytes (torch's caching allocator aligns to 512)."""
     return torch.empty(max(int(n), 256), dtype=torch.uint8, device=device)
