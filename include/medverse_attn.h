@@ -423,6 +423,61 @@ mv_status mv_dag_decode_attn_fp8_blk(const mv_step_tables* tables, const mv_attn
                                      const void* v_pages8, const float* kv_scale, void* out, void* workspace,
                                      size_t workspace_bytes, void* cuda_stream);
 
+/* ---- Chunks of new tokens over that cache ------------------------------------------------------------------------------
+ * A node may receive any number of tokens in one step (a prompt or the next piece of it, text put in at a join, accepted drafts), in
+ * batches described on the device as above.  Positions and slots come from mv_step_tables_build with max_groups = 0, K and V from
+ * mv_rope_write_kv_fp8_blk (or _form); then these two calls.  New token j of a node sees its node's tokens 0 .. node_len + j and every
+ * other visible node in full, what that node receives in the same step included.
+ *
+ * The tables: device arrays of the caller.  Rows are the step's new tokens, ordered (request, node, token).  A receiving node has
+ * a list of ENTRIES of two int32 words {page, tokens}: the pages of the other nodes it sees, ordered by (node, page), then its own;
+ * `tokens` (1 .. 16) of a page's slots are held.  Its rows are cut into TILES of rows_per_tile consecutive rows (the last may have fewer),
+ * eight int32 words each: {first row, rows, first entry of the node's list, entries of other nodes in it, index of the first row's token in
+ * its node, key tiles before this tile, key tiles, 0}; a key tile is eight entries, and a query tile walks those up to its last row's own page.
+ * What lies beyond the step's counts is left as it was.  The arrays may also be filled by the caller's own code; a record that does not
+ * fit the arrays is skipped. */
+typedef struct {
+  int32_t max_rows, max_tiles, max_entries;  /* capacities                                                                */
+  int32_t rows_per_tile;                     /* 1 .. 256; for the attention call at most 2 * (128 / group_size): that many is best */
+  int32_t* tiles;          /* device [max_tiles][8], 16-byte aligned                                                      */
+  int32_t* entries;        /* device [max_entries][2], 16-byte aligned                                                    */
+  int32_t* counts;         /* device [8]: rows, tiles, entries, key tiles, status (an mv_status), three zeros             */
+} mv_chunk_tables;
+
+/* Builds them (batch, shape and errors as for mv_step_tables_build; pos_mode is not read).
+ *   workspace  device, 256-byte aligned, mv_chunk_tables_workspace_bytes(n_req) bytes, scratch.  Two calls that may overlap on the device
+ *              must not share it, nor the tables.
+ * Errors found on the host: MV_ERR_INVALID_ARG, MV_ERR_WORKSPACE, MV_ERR_UNSUPPORTED (max_req_nodes, rows_per_tile), MV_ERR_CUDA.
+ * On the device counts[4] then holds the status and the tables describe an empty step: MV_ERR_NOT_TOPOLOGICAL, MV_ERR_PAGE_CAPACITY,
+ * MV_ERR_INVALID_ARG, MV_ERR_WORKSPACE (more rows, tiles or entries than the capacities), MV_ERR_UNSUPPORTED (a request with more than
+ * max_req_nodes nodes, a node of more than 2^30 tokens, 2^31 key tiles). */
+size_t mv_chunk_tables_workspace_bytes(int32_t n_req);
+mv_status mv_chunk_tables_build(const mv_dag_batch* batch, const mv_step_shape* shape, const mv_chunk_tables* tables, void* workspace,
+                                size_t workspace_bytes, void* cuda_stream);
+/* Status word of the tables (counts[4]), as mv_step_tables_read_status.  Synchronises the stream. */
+mv_status mv_chunk_tables_read_status(const mv_chunk_tables* tables, void* cuda_stream, int32_t* status);
+
+/* Attention of every row of the tables over what it sees: for row r and query head h
+ *   out[r][h] = sum_j softmax_j(sm_scale * <q_rot[r][h], K_j>) V_j.
+ * The step's new tokens must be in the cache first.  Rows that no tile names are left as they were.  Single tokens are served as well
+ * (mv_dag_decode_attn_fp8_blk is the faster call where no node receives more than a few, since there the rows of different nodes share
+ * what they read).
+ *   q_rot, out  device [max_rows][n_q_heads][head_dim] bf16, not overlapping;  pools, kv_scale as above
+ *   workspace   device, 256-byte aligned, mv_chunk_attn_workspace_bytes(geom) bytes (it does not depend on the step); scratch, not to be
+ *               shared by calls that may overlap on the device
+ * A scale counts as the power of two that its exponent gives, at least 2^-80, and has to be at most 2^40; NaN in either scale of a block
+ * gives NaN to the rows that see the block and leaves the others untouched.
+ * Arithmetic: keys and values are bf16 exactly; scores, sums and softmax statistics in 32 bits; weights rounded to bf16.  The same
+ * inputs give the same bits on every call.
+ * dtype MV_BF16, head_dim 64 or 128, group size at most 128, sm_scale not negative; all tensors 16-byte aligned.  Errors: MV_ERR_INVALID_ARG,
+ * MV_ERR_UNSUPPORTED (also a pool of 2^31 or more (page, KV head, token) rows, max_tiles * n_kv_heads past 2^31), MV_ERR_WORKSPACE, MV_ERR_CUDA.
+ * In counts[4]: MV_ERR_INVALID_ARG (records, lists of more than 2^26 pages, pages outside the pool, which are skipped); a wait inside
+ * the kernel that runs out (seconds) ends the call with MV_ERR_TIMEOUT there, `out` is then undefined. */
+size_t mv_chunk_attn_workspace_bytes(const mv_attn_geom* geom);
+mv_status mv_dag_chunk_attn_fp8_blk(const mv_chunk_tables* tables, const mv_attn_geom* geom, const void* q_rot, const void* k_pages8,
+                                    const void* v_pages8, const float* kv_scale, void* out, void* workspace, size_t workspace_bytes,
+                                    void* cuda_stream);
+
 /* Copies pages inside pools: page dst[i] of every pool becomes page src[i], for i < n (a fork that goes on writing gets a copy of
  * the partly filled last page; a compacted pool moves its upper pages down: mv_sched_clone_request and mv_sched_compact make
  * such lists).  One launch for all pools, K and V and scales of any number of layers.

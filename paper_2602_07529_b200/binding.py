@@ -33,7 +33,8 @@ EXPORTS = ["mv_plan_dag", "mv_plan_bind_geometry", "mv_plan_table", "mv_plan_get
            "mv_static_workspace_bytes", "mv_rope_write_kv_fp8", "mv_dag_decode_attn_fp8", "mv_step_tables_workspace_bytes",
            "mv_step_tables_build", "mv_step_tables_read_status", "mv_rope_write_kv_fp8_blk", "mv_decode_fp8_blk_workspace_bytes",
            "mv_dag_decode_attn_fp8_blk", "mv_rope_form_init", "mv_rope_rotate", "mv_plan_positions", "mv_rope_write_kv_form",
-           "mv_rope_write_kv_fp8_blk_form", "mv_pages_copy", "mv_sched_clone_request", "mv_sched_compact", "mv_selftest_bounded_wait", "mv_selftest_tmap_cache",
+           "mv_rope_write_kv_fp8_blk_form", "mv_pages_copy", "mv_chunk_tables_workspace_bytes", "mv_chunk_tables_build",
+           "mv_chunk_tables_read_status", "mv_chunk_attn_workspace_bytes", "mv_dag_chunk_attn_fp8_blk", "mv_sched_clone_request", "mv_sched_compact", "mv_selftest_bounded_wait", "mv_selftest_tmap_cache",
            "mv_sched_create", "mv_sched_destroy", "mv_sched_add_request", "mv_sched_step", "mv_sched_rows",
            "mv_sched_commit", "mv_sched_page_refs", "mv_sched_get_stats"]
 
@@ -80,6 +81,11 @@ class _StepTables(C.Structure):
 
 class _RopeForm(C.Structure):
     _fields_ = [("layout", C.c_int32), ("first", C.c_int32), ("rotary_dim", C.c_int32), ("amplitude", C.c_float), ("theta", C.c_double * 64)]
+
+
+class _ChunkTables(C.Structure):
+    _fields_ = [("max_rows", C.c_int32), ("max_tiles", C.c_int32), ("max_entries", C.c_int32), ("rows_per_tile", C.c_int32)] + [
+        (n, C.c_void_p) for n in ("tiles", "entries", "counts")]
 
 
 class _PagePool(C.Structure):
@@ -129,6 +135,13 @@ def _load():
     lib.mv_plan_positions.argtypes = [vp, C.POINTER(vp)]
     lib.mv_rope_write_kv_form.argtypes = [vp, C.POINTER(_Geom)] + [vp] * 9
     lib.mv_rope_write_kv_fp8_blk_form.argtypes = [vp] * 12
+    lib.mv_chunk_tables_workspace_bytes.argtypes = [i32]
+    lib.mv_chunk_tables_workspace_bytes.restype = sz
+    lib.mv_chunk_tables_build.argtypes = [vp, vp, vp, vp, sz, vp]
+    lib.mv_chunk_tables_read_status.argtypes = [vp, vp, C.POINTER(i32)]
+    lib.mv_chunk_attn_workspace_bytes.argtypes = [C.POINTER(_Geom)]
+    lib.mv_chunk_attn_workspace_bytes.restype = sz
+    lib.mv_dag_chunk_attn_fp8_blk.argtypes = [vp] * 8 + [sz, vp]
     lib.mv_pages_copy.argtypes = [vp, i32, i64, vp, vp, i32, vp, vp, vp]
     lib.mv_sched_clone_request.argtypes = [vp, i32, C.POINTER(i32), i32, vp, vp, C.POINTER(i32)]
     lib.mv_sched_compact.argtypes = [vp, i32, vp, vp, C.POINTER(i32), C.POINTER(i32)]
@@ -538,6 +551,59 @@ def mv_dag_decode_attn_fp8_blk(tables: StepTables, geom: _Geom, q_rot, k_pages8,
         tables._ref, C.byref(geom), _arr(q_rot, "q_rot", T.bfloat16, nq, i), _arr(k_pages8, "k_pages8", T.uint8, pool, i),
         _arr(v_pages8, "v_pages8", T.uint8, pool, i), _arr(kv_scale, "kv_scale", T.float32, blocks * 2, i),
         _arr(out, "out", T.bfloat16, nq, i), _arr(workspace, "workspace", T.uint8, 0, i), workspace.numel(), s), "mv_dag_decode_attn_fp8_blk")
+
+
+# ---- chunks of new tokens over the block-scaled 8-bit cache
+
+class ChunkTables:
+    """The tables of a step with any number of new tokens per node: caller-owned CUDA tensors whose sizes are the capacities (see
+    ``mv_chunk_tables`` in the header)."""
+
+    def __init__(self, tiles, entries, counts, max_rows, rows_per_tile):
+        T = _torch()
+        self.index = counts.get_device()
+        i = max(0, self.index)
+        self.max_rows = int(max_rows)
+        p = [_arr(tiles, "tiles", T.int32, 0, i), _arr(entries, "entries", T.int32, 0, i), _arr(counts, "counts", T.int32, 8, i)]
+        self._keep = (tiles, entries, counts)
+        self.c_tables = _ChunkTables(self.max_rows, tiles.numel() // 8, entries.numel() // 2, int(rows_per_tile), *p)
+        self._ref = C.byref(self.c_tables)
+
+
+def mv_chunk_tables_workspace_bytes(batch) -> int:
+    return int(lib.mv_chunk_tables_workspace_bytes(batch.n_req))
+
+
+def mv_chunk_tables_build(batch: DeviceBatch, tables: ChunkTables, workspace, stream=None):
+    """Query tiles and page lists of a step from its batch on the device; the outcome is in ``counts`` (asynchronous)."""
+    i = tables.index
+    s = _launch_stream(i, stream)
+    ws = _arr(workspace, "workspace", _Torch.uint8, 0, i)
+    if batch.index != i:
+        raise ValueError(f"the batch is on cuda:{batch.index}, the tables on cuda:{i}")
+    _check(lib.mv_chunk_tables_build(*batch._ref, tables._ref, ws, workspace.numel(), s), "mv_chunk_tables_build")
+
+
+def mv_chunk_tables_read_status(tables: ChunkTables, stream=None) -> int:
+    """Status word of the step (0 = fine); synchronises the stream."""
+    out = C.c_int32(-1)
+    _check(lib.mv_chunk_tables_read_status(tables._ref, _launch_stream(tables.index, stream), C.byref(out)), "mv_chunk_tables_read_status")
+    return int(out.value)
+
+
+def mv_chunk_attn_workspace_bytes(geom: _Geom) -> int:
+    return int(lib.mv_chunk_attn_workspace_bytes(C.byref(geom)))
+
+
+def mv_dag_chunk_attn_fp8_blk(tables: ChunkTables, geom: _Geom, q_rot, k_pages8, v_pages8, kv_scale, out, workspace, stream=None):
+    i, T = tables.index, _Torch
+    s = _launch_stream(i, stream)
+    d, blocks = geom.head_dim, geom.num_pages * geom.n_kv_heads
+    nq, pool = tables.max_rows * geom.n_q_heads * d, blocks * 16 * d
+    _check(lib.mv_dag_chunk_attn_fp8_blk(
+        tables._ref, C.byref(geom), _arr(q_rot, "q_rot", T.bfloat16, nq, i), _arr(k_pages8, "k_pages8", T.uint8, pool, i),
+        _arr(v_pages8, "v_pages8", T.uint8, pool, i), _arr(kv_scale, "kv_scale", T.float32, blocks * 2, i),
+        _arr(out, "out", T.bfloat16, nq, i), _arr(workspace, "workspace", T.uint8, 0, i), workspace.numel(), s), "mv_dag_chunk_attn_fp8_blk")
 
 
 # ---- pages

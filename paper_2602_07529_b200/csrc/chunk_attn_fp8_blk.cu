@@ -1,0 +1,932 @@
+// Attention of chunks of new tokens over the block-scaled 8-bit cache, on the 5th-generation tensor cores.
+// For query head h of KV head g and new token i of a node,
+//   out_i = sum_j 2^(c (<q_i, K_j> - r_i)) V_j / sum_j 2^(c (<q_i, K_j> - r_i)),   c = softmax scale * log2 e,
+// over the tokens j of the pages on the node's list; of its own pages, which stand last, only those up to i itself.
+//
+// A query tile is 2 R consecutive new tokens of a node, R = 128 / G for a group of G query heads: two operands of 128 rows, row
+// token * G + head, so that any number of tokens and any group fill the tensor cores' rows and every tile of 128 keys that comes in
+// serves 256 q-vectors.  The second half is left out where the tile has no more than R tokens.
+//
+// The cache holds bytes with four exponent and three mantissa bits at a power-of-two scale per (page, KV head).  Each is a bf16 number
+// exactly (three mantissa bits of seven, exponents within range), so a warpgroup turns the bytes of a tile into bf16 operands between
+// TMA and the products, and everything behind it is plain bf16 arithmetic with 32-bit accumulators: the byte's exponent
+// and mantissa are moved to the low end of a bf16 pattern, which is the value times 2^-120 (the format's subnormals are bf16 subnormals
+// there), and one multiplication by 2^(120 + e) brings the page's scale in.  Softmax weights are rounded to bf16 (2^-9 of each, as
+// in the other prefill kernels); their sum is of the unrounded ones, in 32 bits.
+// A page whose scale is NaN: its keys become NaN, so the scores of whoever sees it; its values stay finite, so whoever does not
+// see it multiplies them by zero.
+//
+// Warps (512 threads): 0 TMA for K, 1 issuer of the products, 2 TMA for V, 3 the walk over the work and TMA for q; 4-7 bytes to bf16; 8-11 and
+// 12-15 softmax of the two halves, a thread per q-vector (online softmax in log2 units, weights written over the scores as packed
+// bf16, O in tensor memory rescaled only when the row's maximum moved by more than 2^8).
+// One CTA per SM walks its share of the work: (query tile, KV head) after (query tile, KV head) lie on a line of cost, a constant
+// and then one unit per key tile, which the shares cut evenly.  What a cut leaves in two or more shares is joined by a second kernel.
+// Every wait is bounded.
+#include <algorithm>
+#include <cmath>
+
+#include "blk_stream.cuh"
+#include "trace.h"
+#include "umma.cuh"
+
+namespace {
+
+using bf16 = __nv_bfloat16;
+constexpr int PS = 16, KEYS = 8;        // tokens of a page; pages of a key tile
+constexpr int BQ = 128, BK = 128;       // q-vectors of a half; keys of a tile
+constexpr int SHARES = 148;             // CTAs
+constexpr int SETUP = 2;                // cost of a (query tile, head) besides its key tiles
+constexpr int NT = 512;
+constexpr int RAW = 2;                  // slots for bytes of K, and of V
+constexpr int RING = 3;                 // bf16 tiles (K0 V0 K1 V1 ...)
+constexpr int METAS = 8;                // descriptions of key tiles: K of tile t waits for bytes of t - 2, converted once V of t - 4 is used up
+constexpr int SEGS = 4;                 // segments handed over
+constexpr int MAXQV = 2 * BQ;
+constexpr float RESCALE_THRESHOLD = 8.f;  // log2 units: weights stay below 2^8
+// A reference is kept as the raw score it was.  Weights are 2^(c s - c r) by one fused multiply-add per pair of scores, where c r is a rounded
+// product: off by 2^-24 of it, the same for all of a row.  Up to FAR that is below 2^-12 of a weight; beyond, the scores are first
+// brought near zero by subtracting r, which is exact for those that matter (scales of a cache go up to 2^40).
+constexpr float FAR = 4096.f;
+constexpr int kMaxList = 1 << 26;       // pages of a list: its slots are counted in 32 bits
+constexpr int V_MIN = -80;              // a scale of zero (a block nobody has quantised) counts as 2^-80
+
+struct Cut {  // a cut (tile, head) at one end of a share
+  int item, row0, rows, ends;  // item: tile * Hkv + head, -1: none; ends: its last key tile is here
+};
+
+struct Args {
+  const int4* tiles;
+  const int2* entries;
+  int32_t* counts;
+  const float2* scale;  // [pages][Hkv]: K, V
+  bf16* out;
+  float* part_o;        // [2 SHARES][MAXQV][D]
+  float2* part_ml;      // [2 SHARES][MAXQV]: reference (a score), sum
+  Cut* cuts;            // [2 SHARES]: item begun earlier, item that goes on in a later share
+  int64_t num_pages;
+  int max_rows, max_tiles, max_entries;
+  int Hq, Hkv, G, R;
+  float scale_log2;
+};
+
+constexpr size_t part_o_bytes(int d) { return size_t(2) * SHARES * MAXQV * d * sizeof(float); }
+constexpr size_t part_ml_bytes() { return size_t(2) * SHARES * MAXQV * sizeof(float2); }
+constexpr size_t workspace_need(int d) { return part_o_bytes(d) + part_ml_bytes() + ((2 * SHARES * sizeof(Cut) + 255) & ~size_t(255)); }
+
+// A run of key tiles of one (query tile, KV head) inside a share.
+struct Segment {
+  int row0, rows, key0;    // tokens of the query tile; index of the first one inside its node
+  int ent0, before, n_ent; // its list: first entry, entries of other nodes, entries up to its last token
+  int head, item;
+  int k0, k1;              // key tiles
+  int slot;                // partial result, or -1: all key tiles are here
+  bool ends;
+};
+
+// The segments of a share, in order: one warp walks and hands them to the others through shared memory (their code and registers
+// would not bear it: 660 bytes of spills a thread where every warp walked by itself).
+struct Walk {
+  int n_tiles, share, t, head, k, units;
+  int64_t base, x_end;     // cost position of tile t; end of the share
+  Segment s;
+
+  __device__ __forceinline__ int64_t point(const Args& a, int unit0, int tile) const { return (int64_t(unit0) + int64_t(SETUP) * tile) * a.Hkv; }
+  // Tile t's record.  One that is not a tile's (rows or entries outside the arrays, key tiles that do not follow) counts as
+  // having no key tiles: what lies behind this check stays inside the arrays whatever the tables hold.
+  __device__ __forceinline__ void take(const Args& a) {
+    const int4 p = __ldcg(a.tiles + 2 * t), q = __ldcg(a.tiles + 2 * t + 1);
+    s.row0 = p.x;
+    s.rows = p.y;
+    s.ent0 = p.z;
+    s.before = p.w;
+    s.key0 = q.x;
+    base = point(a, q.y, t);
+    bool sound = p.x >= 0 && p.y >= 1 && p.y <= 2 * a.R && p.x <= a.max_rows - p.y && p.z >= 0 && p.w >= 0 && q.x >= 0 && q.x < (1 << 30) && q.y >= 0;
+    const int64_t n = sound ? int64_t(p.w) + (q.x + p.y + PS - 1) / PS : 0;
+    sound = sound && n <= int64_t(a.max_entries) - p.z && n <= kMaxList && (n + KEYS - 1) / KEYS == q.z;
+    if (!sound && (threadIdx.x & 31) == 0) atomicExch(a.counts + 4, int(MV_ERR_INVALID_ARG));
+    s.n_ent = sound ? int(n) : 0;
+    units = sound ? q.z : 0;
+  }
+  __device__ __forceinline__ void begin(const Args& a, int c) {
+    const int lane = threadIdx.x & 31;
+    share = c;
+    n_tiles = max(0, min(__ldcg(a.counts + 1), a.max_tiles));
+    const int total_units = max(0, __ldcg(a.counts + 3));
+    const int64_t total = n_tiles > 0 ? point(a, total_units, n_tiles) : 0;
+    const int64_t each = total / SHARES, more = total % SHARES;
+    const int64_t x = each * c + min(int64_t(c), more);
+    x_end = x + each + (c < more ? 1 : 0);
+    t = n_tiles;
+    if (x >= x_end) return;
+    // the last tile whose position is not behind x: 32 probes at a time
+    int lo = 0, hi = n_tiles;  // tile lo is not behind x (or lo = 0), tile hi is
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 31) / 32, at = min(lo + lane * step, hi - 1);
+      const bool before = lane == 0 || point(a, __ldcg(reinterpret_cast<const int32_t*>(a.tiles) + 8 * int64_t(at) + 5), at) <= x;
+      const unsigned m = __ballot_sync(0xffffffffu, before);
+      const int top = 31 - __clz(m);  // the highest lane whose tile is not behind x
+      const int new_lo = min(lo + top * step, hi - 1);
+      if (top < 31) hi = min(hi, max(new_lo + 1, min(lo + (top + 1) * step, hi)));
+      lo = new_lo;
+    }
+    t = lo;
+    take(a);
+    const int64_t per = SETUP + units, at = max(int64_t(0), x - base);
+    head = int(min(int64_t(a.Hkv), at / per));
+    const int64_t in = at - head * per;
+    k = in > SETUP ? int(min(in - SETUP, int64_t(units))) : 0;
+  }
+  // The next segment in s; false at the end of the share.
+  __device__ __forceinline__ bool next(const Args& a) {
+    while (t < n_tiles) {
+      if (head >= a.Hkv || units == 0) {
+        head = k = 0;
+        if (++t < n_tiles) take(a);
+        continue;
+      }
+      if (k >= units) {
+        k = 0;
+        ++head;
+        continue;
+      }
+      const int64_t first = base + int64_t(head) * (SETUP + units) + SETUP;  // point of its first key tile
+      const int end = int(max(int64_t(0), min(int64_t(units), x_end - first)));
+      if (end <= k) return false;
+      s.head = head;
+      s.item = t * a.Hkv + head;
+      s.k0 = k;
+      s.k1 = end;
+      s.ends = end == units;
+      s.slot = k == 0 && s.ends ? -1 : 2 * share + (k > 0 ? 0 : 1);
+      k = end;
+      return true;
+    }
+    return false;
+  }
+};
+
+// What the converters and the softmax threads need of a key tile.
+struct alignas(16) Meta {
+  uint32_t k1[KEYS], k2[KEYS], v1[KEYS], v2[KEYS];  // factors of a page as pairs of bf16: the byte's pattern times the first times the second
+  uint32_t valid[BK / 32];                          // keys that hold a token
+  uint32_t twice;                                   // some second factor is not one
+  uint32_t pad[3];
+};
+struct Shared {
+  Meta meta[METAS];
+  Segment seg[SEGS];
+  uint64_t seg_full[SEGS], seg_empty[SEGS], q_full, q_empty, raw_full[2][RAW], raw_empty[2][RAW], described[METAS], kv_full[RING], kv_empty[RING], s_full[2], p_full[2], o_done[2], drained;
+  int abort;
+  uint32_t tmem;
+};
+
+template <int D>
+struct Lay {
+  static constexpr int TILE = BK * D * 2;   // a bf16 tile: [D / 64 column blocks][128 rows][128 bytes]
+  static constexpr int BLOCK = BK * 128;    // a column block
+  static constexpr int BYTES = BK * D;      // a tile of the cache
+  static constexpr int Q = 0;               // both halves
+  static constexpr int KV = 2 * TILE;
+  static constexpr int RAWS = KV + RING * TILE;
+  static constexpr int SHARED = RAWS + 2 * RAW * BYTES;
+  static constexpr int SMEM = SHARED + ((int(sizeof(Shared)) + 127) & ~127);
+  static_assert(SMEM <= 227 * 1024, "shared memory of an SM");
+};
+
+__device__ __forceinline__ uint32_t bar(const void* p) { return mv::smem_u32(p); }
+
+// Bounded waits.  False once a wait of this CTA has run out (this one or an earlier one, of any role): the caller then issues
+// nothing further, leaves its loops, and whoever has copies or products in flight waits for them (again bounded) before the CTA ends.
+struct Cta {
+  const Args* a;
+  unsigned char* smem;
+  uint32_t base;
+  Shared* sh;
+  __device__ __forceinline__ bool wait(const uint64_t& b, uint32_t parity) const {
+    if (mv::mbar_try_wait(bar(&b), parity)) return true;
+    if (*reinterpret_cast<volatile int*>(&sh->abort)) return false;
+    if (!mv::mbar_wait_bounded(bar(&b), parity, 2000000000ull, &sh->abort)) {
+      if (!*reinterpret_cast<volatile int*>(&sh->abort)) atomicExch(a->counts + 4, int(MV_ERR_TIMEOUT));
+      *reinterpret_cast<volatile int*>(&sh->abort) = 1;
+      return false;
+    }
+    return true;
+  }
+  __device__ __forceinline__ bool warp_wait(const uint64_t& b, uint32_t parity) const { return __all_sync(0xffffffffu, wait(b, parity)); }
+};
+
+// The segments as the other warps get them.  next() is null at the end of the share and after a wait has run out (then ok is false).
+struct Reader {
+  int n = 0;
+  __device__ __forceinline__ const Segment* next(const Cta& c, bool& ok) {
+    if (!ok) return nullptr;
+    ok = c.warp_wait(c.sh->seg_full[n % SEGS], (n / SEGS) & 1);
+    const Segment* s = &c.sh->seg[n % SEGS];
+    return ok && s->item >= 0 ? s : nullptr;
+  }
+  __device__ __forceinline__ void done(const Cta& c) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mv::mbar_arrive(bar(&c.sh->seg_empty[n % SEGS]));
+    ++n;
+  }
+};
+constexpr int READERS = 3 + 4 + 8;  // warps
+
+// ---- bytes of K (and the tiles' descriptions) or of V: eight boxes, a page each, make a tile
+__device__ __forceinline__ uint32_t twice_bf16(int exponent) {  // a pair of bf16 numbers 2^exponent
+  const uint32_t h = uint32_t(127 + exponent) << 7;
+  return h | (h << 16);
+}
+
+template <int D, bool IS_K>
+__device__ __forceinline__ void byte_loader(const Cta& c, const CUtensorMap* map) {
+  const Args& a = *c.a;
+  const int lane = threadIdx.x & 31;
+  const bool lead = mv::um::elect_one();
+  int tile = 0;  // key tiles of the share so far
+  bool ok = true;
+  Reader rd;
+  for (const Segment* at_seg; (at_seg = rd.next(c, ok)); rd.done(c)) {
+    const Segment s = *at_seg;
+    const int first = s.k0 * KEYS, last = min(s.n_ent, s.k1 * KEYS);
+    // a window of 32 entries, one per lane
+    auto entry_at = [&](int i0) {
+      int2 e = make_int2(-1, 0);
+      if (i0 + lane < last) {
+        e = __ldcg(a.entries + s.ent0 + i0 + lane);
+        if (e.x < 0 || e.x >= a.num_pages || e.y < 1 || e.y > PS) {
+          atomicExch(a.counts + 4, int(MV_ERR_INVALID_ARG));
+          e = make_int2(-1, 0);
+        }
+      }
+      return e;
+    };
+    auto scale_at = [&](const int2& e) { return IS_K && e.x >= 0 ? __ldcg(a.scale + int64_t(e.x) * a.Hkv + s.head) : make_float2(1.f, 1.f); };
+    int2 e0 = entry_at(first), e1 = entry_at(first + 32);
+    float2 s0 = scale_at(e0);
+#pragma unroll 1
+    for (int t = s.k0; t < s.k1; ++t, ++tile) {
+      const int at = ((t - s.k0) * KEYS) & 31;
+      if (at == 0 && t > s.k0) {
+        e0 = e1;
+        s0 = scale_at(e0);
+        e1 = entry_at(t * KEYS + 32);
+      }
+      const unsigned present = (__ballot_sync(0xffffffffu, e0.x >= 0) >> at) & 0xffu;
+      const int my_row = (e0.x * a.Hkv + s.head) * PS;
+      const int slot = tile % RAW;
+      ok = c.warp_wait(c.sh->raw_empty[IS_K ? 0 : 1][slot], ((tile / RAW) & 1) ^ 1);
+      if (!ok) break;
+      const uint32_t fb = bar(&c.sh->raw_full[IS_K ? 0 : 1][slot]), dst = c.base + Lay<D>::RAWS + ((IS_K ? 0 : RAW) + slot) * Lay<D>::BYTES;
+      if (lead) mv::mbar_arrive_expect_tx(fb, uint32_t(__popc(present)) * (PS * D));
+#pragma unroll
+      for (int j = 0; j < KEYS; ++j) {
+        const int row = __shfl_sync(0xffffffffu, my_row, at + j);
+        if (lead && ((present >> j) & 1)) mv::tma_load_2d(dst + j * (PS * D), map, 0, row, fb);
+      }
+      __syncwarp();
+      if (IS_K) {
+        Meta& m = c.sh->meta[tile % METAS];
+        const bool mine = lane >= at && lane < at + KEYS;
+        uint32_t k1 = 0, k2 = 0x3f803f80u, v1 = 0, v2 = 0x3f803f80u;  // a page that is not there: zeros
+        if (e0.x >= 0) {
+          const int ek = mv::blk::scale_exponent(s0.x);
+          int ev = mv::blk::scale_exponent(s0.y);
+          if (ek == 128 || ev == 128) {
+            k1 = 0x7fc07fc0u;
+            ev = 0;
+          } else {
+            k1 = twice_bf16(min(120 + max(ek, V_MIN), 127));
+            k2 = twice_bf16(max(ek - 7, 0));
+          }
+          v1 = twice_bf16(min(120 + max(ev, V_MIN), 127));
+          v2 = twice_bf16(max(ev - 7, 0));
+        }
+        // keys that hold a token: sixteen bits per page
+        const uint32_t bits = e0.x >= 0 ? (1u << e0.y) - 1 : 0;
+        const uint32_t pair = bits | (__shfl_down_sync(0xffffffffu, bits, 1) << 16);
+        const bool more_than_one = __any_sync(0xffffffffu, mine && (k2 != 0x3f803f80u || v2 != 0x3f803f80u));
+        if (mine) {
+          m.k1[lane - at] = k1;
+          m.k2[lane - at] = k2;
+          m.v1[lane - at] = v1;
+          m.v2[lane - at] = v2;
+          if (((lane - at) & 1) == 0) m.valid[(lane - at) / 2] = pair;
+        }
+        if (lane == 0) m.twice = more_than_one ? 1 : 0;
+        __syncwarp();
+        if (lane == 0) mv::mbar_arrive(bar(&c.sh->described[tile % METAS]));
+      }
+    }
+  }
+  if (!ok) {
+    // what is in flight must land before the CTA may leave: the last fills of this warp's slots
+    if (lane == 0)
+      for (int k = 1; k <= min(tile, RAW); ++k)
+        (void)mv::mbar_wait_bounded(bar(&c.sh->raw_full[IS_K ? 0 : 1][(tile - k) % RAW]), ((tile - k) / RAW) & 1, 20000000ull);
+    __syncwarp();
+  }
+}
+
+// ---- the walk, and q: both halves of the segment's query tile
+template <int D>
+__device__ __forceinline__ void q_loader(const Cta& c, const CUtensorMap* map) {
+  const Args& a = *c.a;
+  Shared* const sh = c.sh;
+  const bool lead = mv::um::elect_one();
+  Walk w;
+  w.begin(a, blockIdx.x);
+  Cut first{-1, 0, 0, 0}, last{-1, 0, 0, 0};
+  int n = 0, loads = 0;
+  bool ok = true;
+  for (bool more = true; ok && more; ++n) {
+    more = w.next(a);
+    ok = c.warp_wait(sh->seg_empty[n % SEGS], ((n / SEGS) & 1) ^ 1);
+    if (!ok) break;
+    const Segment& s = w.s;
+    if (lead) {
+      sh->seg[n % SEGS] = s;
+      if (!more) sh->seg[n % SEGS].item = -1;
+      mv::mbar_arrive(bar(&sh->seg_full[n % SEGS]));
+    }
+    __syncwarp();
+    if (!more) break;
+    if (s.slot >= 0) (s.k0 > 0 ? first : last) = Cut{s.item, s.row0, s.rows, s.ends ? 1 : 0};
+    ok = c.warp_wait(sh->q_empty, (n & 1) ^ 1);
+    if (!ok) break;
+    const int halves = s.rows > a.R ? 2 : 1;
+    if (lead) {
+      mv::mbar_arrive_expect_tx(bar(&sh->q_full), uint32_t(halves * (D / 64) * a.G * a.R * 128));
+      for (int i = 0; i < halves; ++i)
+        for (int b = 0; b < D / 64; ++b)
+          mv::tma_load_3d(c.base + Lay<D>::Q + i * Lay<D>::TILE + b * Lay<D>::BLOCK, map, b * 64, s.head * a.G, s.row0 + i * a.R, bar(&sh->q_full));
+    }
+    ++loads;
+    __syncwarp();
+  }
+  if (lead) {  // the share's cut items, for the merge
+    int4* const cuts = reinterpret_cast<int4*>(a.cuts) + 2 * blockIdx.x;
+    cuts[0] = make_int4(first.item, first.row0, first.rows, first.ends);
+    cuts[1] = make_int4(last.item, last.row0, last.rows, last.ends);
+  }
+  if (!ok && loads > 0 && lead) (void)mv::mbar_wait_bounded(bar(&sh->q_full), (loads - 1) & 1, 20000000ull);  // in flight
+  __syncwarp();
+}
+
+// ---- bytes to bf16
+// Four bytes to two pairs of bf16: value * 2^-120 in each half, then the factor.
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t x, uint32_t y) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+  return r;
+}
+__device__ __forceinline__ uint32_t widen(uint32_t w, uint32_t selector) {  // two bytes into the upper halves of two half-words, then into place
+  const uint32_t p = __byte_perm(w, 0, selector);
+  return ((p >> 4) & 0x07f007f0u) | (p & 0x80008000u);
+}
+template <int D>
+__device__ __forceinline__ void convert_tile(const unsigned char* raw, unsigned char* dst, const uint32_t* f1, const uint32_t* f2, bool twice) {
+  const int tid = threadIdx.x & 127, q8 = tid >> 3, j = tid & 7;
+  // Eight threads read 16 bytes each and write 32.  The rows of a pair are chosen so that both meet all banks once: of
+  // 128-byte rows, r and r xor 5 (bit 2 sets the read pieces apart, bit 0 the written ones); of 64-byte rows, r and r + 1.
+#pragma unroll 2
+  for (int i = 0; i < 4; ++i) {
+    int row;
+    if (D == 128) {
+      const int p = q8 & 3;
+      row = 32 * i + (q8 >> 2) * 8 + ((j >> 2) ? (p ^ 5) : p);
+    } else {
+      row = 32 * i + q8 * 2 + (j >> 2);
+    }
+    const uint32_t f = f1[row >> 4], g = f2[row >> 4];
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h) {
+      const int ch = h * 4 + (j & 3);  // 16-byte piece of the row
+      const uint4 in = *reinterpret_cast<const uint4*>(raw + row * D + ((D == 128 ? ch ^ (row & 7) : ch ^ ((row >> 1) & 3)) << 4));
+      const uint32_t w[4] = {in.x, in.y, in.z, in.w};
+      uint32_t o[8];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        o[2 * k] = mul_bf16x2(widen(w[k], 0x1404), f);
+        o[2 * k + 1] = mul_bf16x2(widen(w[k], 0x3424), f);
+      }
+      if (twice) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = mul_bf16x2(o[k], g);
+      }
+      unsigned char* const at = dst + h * Lay<D>::BLOCK + row * 128;
+      const int k0 = (2 * (j & 3)) ^ (row & 7), k1 = (2 * (j & 3) + 1) ^ (row & 7);
+      *reinterpret_cast<uint4*>(at + (k0 << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+      *reinterpret_cast<uint4*>(at + (k1 << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+    }
+  }
+}
+template <int D>
+__device__ __forceinline__ void converters(const Cta& c) {
+  const int lane = threadIdx.x & 31;
+  Shared* const sh = c.sh;
+  int tile = 0;
+  bool ok = true;
+  Reader rd;
+  for (const Segment* s; (s = rd.next(c, ok)); rd.done(c)) {
+#pragma unroll 1
+    for (int left = s->k1 - s->k0; left > 0 && ok; --left, ++tile) {
+      const Meta& m = sh->meta[tile % METAS];
+      ok = c.warp_wait(sh->described[tile % METAS], (tile / METAS) & 1);
+#pragma unroll 1
+      for (int kv = 0; kv < 2 && ok; ++kv) {
+        const int e = 2 * tile + kv, slot = tile % RAW;
+        ok = c.warp_wait(sh->raw_full[kv][slot], (tile / RAW) & 1) && c.warp_wait(sh->kv_empty[e % RING], ((e / RING) & 1) ^ 1);
+        if (!ok) break;
+        convert_tile<D>(c.smem + Lay<D>::RAWS + (kv * RAW + slot) * Lay<D>::BYTES, c.smem + Lay<D>::KV + (e % RING) * Lay<D>::TILE,
+                        kv ? m.v1 : m.k1, kv ? m.v2 : m.k2, m.twice != 0);
+        mv::fence_proxy_async();  // ordinary stores, read next by the tensor core
+        __syncwarp();
+        if (lane == 0) {
+          mv::mbar_arrive(bar(&sh->kv_full[e % RING]));
+          mv::mbar_arrive(bar(&sh->raw_empty[kv][slot]));
+        }
+      }
+    }
+  }
+}
+
+// ---- products: the whole warp walks and waits, one elected lane issues
+// S_i = Q_i K^T over the first n_cols keys (a multiple of 16): both operands K-major
+template <int D>
+__device__ __forceinline__ void issue_qk(uint32_t s_tmem, uint64_t q_desc, uint64_t k_desc, int n_cols) {
+  const uint32_t idesc = mv::um::idesc_bf16(BQ, n_cols, 0, 0);
+  mv::um::mma_ss<false>(s_tmem, q_desc, k_desc, idesc);
+#pragma unroll
+  for (int k = 1; k < D / 16; ++k) {
+    const uint32_t off = ((k >> 2) * Lay<D>::BLOCK + (k & 3) * 32) >> 4;
+    mv::um::mma_ss<true>(s_tmem, q_desc + off, k_desc + off, idesc);
+  }
+}
+// O_i (+)= P_i V over the first k_steps * 16 keys: P from tensor memory (two bf16 per column), V MN-major
+template <int D>
+__device__ __forceinline__ void issue_pv(uint32_t o_tmem, uint32_t p_tmem, uint64_t v_desc, bool accumulate, int k_steps) {
+  constexpr uint32_t idesc = mv::um::idesc_bf16(BQ, D, 0, 1);
+  if (accumulate) mv::um::mma_ts<true>(o_tmem, p_tmem, v_desc, idesc);
+  else mv::um::mma_ts<false>(o_tmem, p_tmem, v_desc, idesc);
+#pragma unroll
+  for (int k = 1; k < BK / 16; ++k)
+    if (k < k_steps) mv::um::mma_ts<true>(o_tmem, p_tmem + k * 8, v_desc + uint32_t((k * 2048) >> 4), idesc);
+}
+
+template <int D>
+__device__ __forceinline__ void issuer(const Cta& c) {
+  const Args& a = *c.a;
+  Shared* const sh = c.sh;
+  const bool lead = mv::um::elect_one();
+  const uint32_t tmem = sh->tmem;
+  const uint64_t q0 = mv::um::smem_desc(c.base + Lay<D>::Q, 16, 1024), q1 = mv::um::smem_desc(c.base + Lay<D>::Q + Lay<D>::TILE, 16, 1024);
+  const uint32_t s0 = tmem, s1 = tmem + 128, o0 = tmem + 256, o1 = tmem + 384;
+  auto k_desc = [&](int e) { return mv::um::smem_desc(c.base + Lay<D>::KV + (e % RING) * Lay<D>::TILE, 16, 1024); };
+  auto v_desc = [&](int e) { return mv::um::smem_desc(c.base + Lay<D>::KV + (e % RING) * Lay<D>::TILE, Lay<D>::BLOCK, 1024); };
+  bool ok = true;
+  auto full = [&](int e) { ok = ok && c.warp_wait(sh->kv_full[e % RING], (e / RING) & 1); };
+  auto release = [&](int e) { if (lead) mv::um::commit(bar(&sh->kv_empty[e % RING])); };
+  int tile = 0, na = 0, nb = 0;  // key tiles, and tiles of either half so far
+  Reader rd;
+  for (const Segment* at_seg; (at_seg = rd.next(c, ok)); rd.done(c)) {
+    const Segment s = *at_seg;
+    const bool both = s.rows > a.R;
+    auto pages = [&](int t) { return min(KEYS, s.n_ent - t * KEYS); };
+    ok = c.warp_wait(sh->q_full, rd.n & 1);
+    full(2 * tile);
+    if (!ok) break;
+    mv::um::fence_after();
+    int here = pages(s.k0);
+    if (lead) {
+      issue_qk<D>(s0, q0, k_desc(2 * tile), here * 16);
+      mv::um::commit(bar(&sh->s_full[0]));
+      if (both) {
+        issue_qk<D>(s1, q1, k_desc(2 * tile), here * 16);
+        mv::um::commit(bar(&sh->s_full[1]));
+      }
+    }
+    release(2 * tile);
+    if (s.k1 - s.k0 == 1 && lead) mv::um::commit(bar(&sh->q_empty));
+#pragma unroll 1
+    for (int t = s.k0; t < s.k1; ++t, ++tile) {
+      const int ev = 2 * tile + 1, ek = 2 * tile + 2;
+      const bool go_on = t + 1 < s.k1;
+      const int next = go_on ? pages(t + 1) : 0;
+      full(ev);
+      if (go_on) full(ek);  // here, while the weights of the first half are still being computed
+      ok = ok && c.warp_wait(sh->p_full[0], na & 1);
+      ++na;
+      if (!ok) break;
+      mv::um::fence_after();
+      if (lead) {
+        issue_pv<D>(o0, s0, v_desc(ev), t > s.k0, here);
+        mv::um::commit(bar(&sh->o_done[0]));
+        if (go_on) {
+          issue_qk<D>(s0, q0, k_desc(ek), next * 16);
+          mv::um::commit(bar(&sh->s_full[0]));
+        }
+      }
+      __syncwarp();
+      if (both) {
+        ok = c.warp_wait(sh->p_full[1], nb & 1);
+        ++nb;
+        if (!ok) break;
+        mv::um::fence_after();
+        if (lead) {
+          issue_pv<D>(o1, s1, v_desc(ev), t > s.k0, here);
+          mv::um::commit(bar(&sh->o_done[1]));
+        }
+      }
+      release(ev);
+      if (go_on) {
+        if (both && lead) {
+          issue_qk<D>(s1, q1, k_desc(ek), next * 16);
+          mv::um::commit(bar(&sh->s_full[1]));
+        }
+        release(ek);
+        if (t + 2 == s.k1 && lead) mv::um::commit(bar(&sh->q_empty));  // the segment's last scores
+      }
+      here = next;
+      __syncwarp();
+    }
+  }
+  if (!ok) {  // products may still be in flight: they must have completed before the tensor memory is freed
+    __syncwarp();
+    if (lead) mv::um::commit(bar(&sh->drained));
+    (void)mv::mbar_wait_bounded(bar(&sh->drained), 0, 20000000ull);
+    __syncwarp();
+  }
+}
+
+// ---- softmax of half i: thread = q-vector
+template <int D>
+__device__ __forceinline__ void softmax_group(const Cta& c, int i) {
+  const Args& a = *c.a;
+  Shared* const sh = c.sh;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int v = (warp & 3) * 32 + lane;                       // q-vector of the half = tensor-memory lane
+  const uint32_t lane_base = sh->tmem + (uint32_t((warp & 3) * 32) << 16);
+  const uint32_t s_t = lane_base + i * 128, o_t = lane_base + 256 + i * 128;
+  const int token = v / a.G, in_group = v - token * a.G;      // token inside the half, head inside the group
+  int tile = 0, j = 0;                                        // key tiles of the share; of this half
+  bool ok = true;
+  Reader rd;
+  for (const Segment* s; (s = rd.next(c, ok)); rd.done(c)) {
+    const int first = i * a.R, rows = min(a.R, s->rows - first);  // tokens of the half
+    const int k0 = s->k0, k1 = s->k1;
+    if (rows <= 0) {
+      tile += k1 - k0;
+      continue;
+    }
+    const bool live = token < rows;
+    const int own = s->before * PS + s->key0 + first;            // slot of the half's first token in the node's list
+    float r = -INFINITY, l = 0.f;                                // reference (a score), and sum
+#pragma unroll 1
+    for (int t = k0; t < k1; ++t, ++tile, ++j) {
+      // The scores first: a half that was left out of earlier tiles has not followed the phases of `described`.  With this tile's scores
+      // there, its description is (and the one eight tiles on is not).
+      ok = c.warp_wait(sh->s_full[i], j & 1) && c.warp_wait(sh->described[tile % METAS], (tile / METAS) & 1);
+      if (!ok) break;
+      mv::um::fence_after();
+      // all 128 columns are read: on a ragged tile only the leading ones were computed, the rest holds something older and is masked
+      uint32_t x[BK];
+#pragma unroll
+      for (int k = 0; k < BK / 32; ++k) mv::um::ld32(s_t + k * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[k * 32]));
+      const uint4 valid = *reinterpret_cast<const uint4*>(sh->meta[tile % METAS].valid);
+      mv::um::wait_ld();
+      float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      const int seen = own + 1 - t * BK;  // slots of the tile that the half's first token sees
+      if (seen >= BK && (valid.x & valid.y & valid.z & valid.w) == ~0u) {
+#pragma unroll
+        for (int k = 0; k < BK; k += 2) mx4[(k >> 1) & 3] = mv::max3(mx4[(k >> 1) & 3], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+      } else {
+        const uint32_t vw[4] = {valid.x, valid.y, valid.z, valid.w};
+        const int lim = seen + token;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int n = lim - 32 * q;
+          const uint32_t see = n >= 32 ? vw[q] : n <= 0 ? 0u : vw[q] & ((1u << n) - 1);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            if (!((see >> k) & 1)) x[32 * q + k] = __float_as_uint(-INFINITY);
+            mx4[k & 3] = fmaxf(mx4[k & 3], __uint_as_float(x[32 * q + k]));
+          }
+        }
+      }
+      const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+      // the reference moves only when a weight would otherwise pass 2^8
+      const bool move = live && (r == -INFINITY ? mx > -INFINITY : (mx - r) * a.scale_log2 > RESCALE_THRESHOLD);
+      if (t > k0 && __any_sync(0xffffffffu, move)) {
+        const float f = (move && r != -INFINITY) ? mv::fast_exp2((r - mx) * a.scale_log2) : 1.f;
+        ok = c.warp_wait(sh->o_done[i], (j - 1) & 1);  // O holds the tiles before and no product is writing it
+        if (!ok) break;
+        mv::um::fence_after();
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+          uint32_t o[32];
+          mv::um::ld32(o_t + k * 32, o);
+          mv::um::wait_ld();
+#pragma unroll
+          for (int n = 0; n < 32; ++n) o[n] = __float_as_uint(__uint_as_float(o[n]) * f);
+          mv::um::st32(o_t + k * 32, o);
+        }
+        l *= f;
+      }
+      if (move) r = mx;
+      float ref = r == -INFINITY ? 0.f : r * a.scale_log2;
+      const bool far = fabsf(ref) > FAR;  // (a row's own matter: its neighbours in the warp subtract zero)
+      if (__any_sync(0xffffffffu, far)) {
+        const uint64_t minus = mv::pack_f32x2(far ? -r : 0.f, far ? -r : 0.f);
+#pragma unroll
+        for (int k = 0; k < BK; k += 2) {
+          float x0, x1;
+          mv::unpack_f32x2(mv::add_f32x2(mv::pack_f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), minus), x0, x1);
+          x[k] = __float_as_uint(x0);
+          x[k + 1] = __float_as_uint(x1);
+        }
+        if (far) ref = 0.f;
+      }
+      const uint64_t scale2 = mv::pack_f32x2(a.scale_log2, a.scale_log2), nmref2 = mv::pack_f32x2(-ref, -ref);
+      uint64_t sum2[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < BK / 2; ++k) {  // weights over the scores in place: columns 2k, 2k+1 -> packed column k
+        float x0, x1;
+        mv::unpack_f32x2(mv::fma_f32x2(mv::pack_f32x2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])), scale2, nmref2), x0, x1);
+        const float p0 = mv::fast_exp2(x0), p1 = mv::fast_exp2(x1);
+        sum2[k & 3] = mv::add_f32x2(sum2[k & 3], mv::pack_f32x2(p0, p1));
+        x[k] = mv::pack_bf16(p0, p1);
+      }
+      {
+        float e, o;
+        mv::unpack_f32x2(mv::add_f32x2(mv::add_f32x2(sum2[0], sum2[1]), mv::add_f32x2(sum2[2], sum2[3])), e, o);
+        l += e + o;
+      }
+      mv::um::st32(s_t, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
+      mv::um::st32(s_t + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
+      mv::um::wait_st();
+      mv::um::fence_before();
+      __syncwarp();
+      if (lane == 0) mv::mbar_arrive(bar(&sh->p_full[i]));  // the weights (and a rescaled O) are in place
+    }
+    if (!ok) break;
+    ok = c.warp_wait(sh->o_done[i], (j - 1) & 1);
+    if (!ok) break;
+    mv::um::fence_after();
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int slot = s->slot;
+    const int64_t row = int64_t(s->row0) + first + token;
+    bf16* const dst = a.out + (row * a.Hq + s->head * a.G + in_group) * D;
+    const int64_t at = int64_t(slot) * MAXQV + i * BQ + v;
+    if (slot >= 0 && live) a.part_ml[at] = make_float2(r, l);
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) {
+      uint32_t o[32];
+      mv::um::ld32(o_t + k * 32, o);
+      mv::um::wait_ld();
+      if (live) {
+        if (slot < 0) {
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            uint4 y;
+            y.x = mv::pack_bf16(__uint_as_float(o[8 * n]) * inv, __uint_as_float(o[8 * n + 1]) * inv);
+            y.y = mv::pack_bf16(__uint_as_float(o[8 * n + 2]) * inv, __uint_as_float(o[8 * n + 3]) * inv);
+            y.z = mv::pack_bf16(__uint_as_float(o[8 * n + 4]) * inv, __uint_as_float(o[8 * n + 5]) * inv);
+            y.w = mv::pack_bf16(__uint_as_float(o[8 * n + 6]) * inv, __uint_as_float(o[8 * n + 7]) * inv);
+            *reinterpret_cast<uint4*>(dst + k * 32 + n * 8) = y;
+          }
+        } else {
+#pragma unroll
+          for (int n = 0; n < 8; ++n)
+            *reinterpret_cast<uint4*>(a.part_o + at * D + k * 32 + n * 4) = make_uint4(o[4 * n], o[4 * n + 1], o[4 * n + 2], o[4 * n + 3]);
+        }
+      }
+    }
+    mv::um::fence_before();
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(NT, 1) chunk_attn_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap tm_q,
+                                                           const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  Shared* const sh = reinterpret_cast<Shared*>(smem + Lay<D>::SHARED);
+  const int tid = threadIdx.x, warp = tid >> 5;
+  const uint32_t base = mv::smem_u32(smem);
+  if ((base & 1023u) != 0) {  // the swizzle pattern is anchored at 1024-byte boundaries
+    mv::grid_dependency_wait();
+    if (tid == 0) atomicExch(a.counts + 4, int(MV_ERR_UNSUPPORTED));
+    if (tid < 2) reinterpret_cast<int4*>(a.cuts)[2 * blockIdx.x + tid] = make_int4(-1, 0, 0, 0);
+    return;
+  }
+  if (tid == 0) {
+    sh->abort = 0;
+    for (int i = 0; i < SEGS; ++i) {
+      mv::mbar_init(bar(&sh->seg_full[i]), 1);
+      mv::mbar_init(bar(&sh->seg_empty[i]), READERS);
+    }
+    mv::mbar_init(bar(&sh->q_full), 1);
+    mv::mbar_init(bar(&sh->q_empty), 1);
+    for (int i = 0; i < 2; ++i)
+      for (int k = 0; k < RAW; ++k) {
+        mv::mbar_init(bar(&sh->raw_full[i][k]), 1);
+        mv::mbar_init(bar(&sh->raw_empty[i][k]), 4);  // the converters' warps
+      }
+    for (int i = 0; i < METAS; ++i) mv::mbar_init(bar(&sh->described[i]), 1);
+    for (int i = 0; i < RING; ++i) {
+      mv::mbar_init(bar(&sh->kv_full[i]), 4);
+      mv::mbar_init(bar(&sh->kv_empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mv::mbar_init(bar(&sh->s_full[i]), 1);
+      mv::mbar_init(bar(&sh->p_full[i]), 4);
+      mv::mbar_init(bar(&sh->o_done[i]), 1);
+    }
+    mv::mbar_init(bar(&sh->drained), 1);
+    mv::mbar_fence_init();
+    mv::fence_proxy_async();
+  }
+  if (warp == 2) {  // the whole tensor memory of the SM: S0 S1 O0 O1, 128 columns each
+    mv::um::tmem_alloc(mv::smem_u32(&sh->tmem), 512);
+    mv::um::tmem_relinquish();
+  }
+  mv::um::fence_before();
+  __syncthreads();
+  mv::um::fence_after();
+  // launched with programmatic stream serialisation: what is above may overlap the end of the kernel before
+  mv::grid_dependency_wait();
+  mv::grid_dependency_launch_dependents();
+  const Cta c{&a, smem, base, sh};
+  // launched with 128 registers per thread: 56 + 56 + 2 * 200 = 4 * 128
+  if (warp < 4) {
+    mv::um::reg_dec<56>();
+    if (warp == 0) byte_loader<D, true>(c, &tm_k);
+    else if (warp == 1) issuer<D>(c);
+    else if (warp == 2) byte_loader<D, false>(c, &tm_v);
+    else q_loader<D>(c, &tm_q);
+  } else if (warp < 8) {
+    mv::um::reg_dec<56>();
+    converters<D>(c);
+  } else {
+    mv::um::reg_inc<200>();
+    softmax_group<D>(c, (warp - 8) >> 2);
+  }
+  mv::um::fence_before();
+  __syncthreads();
+  if (warp == 2) mv::um::tmem_dealloc(sh->tmem, 512);
+}
+
+// Joins the cut items: out = sum_i w_i O_i / sum_i w_i l_i, w_i = 2^(c (r_i - max r)) over the item's parts i.  CTA (c, y): the item that starts in
+// share c and ends in a later one, a slice of its q-vectors; a warp per q-vector, four parts in flight.
+constexpr int MERGE_WARPS = 8, SLICES = 8;
+template <int D>
+__global__ void __launch_bounds__(MERGE_WARPS * 32) chunk_merge_kernel(const Args a) {
+  constexpr int VEC = D / 32, FLY = 4;
+  mv::grid_dependency_wait();
+  const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int4* const cuts = reinterpret_cast<const int4*>(a.cuts);
+  const int4 own = __ldcg(cuts + 2 * c + 1);
+  if (own.x < 0) return;
+  // the parts: slot 2 c + 1, then slots 2 i of the shares behind, without gaps
+  int parts = 1;
+  for (int i0 = c + 1; i0 < SHARES; i0 += 32) {
+    const bool here = i0 + lane < SHARES && __ldcg(reinterpret_cast<const int*>(cuts + 2 * (i0 + lane))) == own.x;
+    const unsigned m = __ballot_sync(0xffffffffu, here);
+    const int run = m == ~0u ? 32 : __ffs(~m) - 1;
+    parts += run;
+    if (run < 32) break;
+  }
+  const int head = own.x % a.Hkv;
+  for (int q = blockIdx.y * MERGE_WARPS + warp; q < MAXQV; q += SLICES * MERGE_WARPS) {
+    const int half = q / BQ, v = q % BQ, token = v / a.G;
+    if (token >= min(a.R, own.z - half * a.R)) continue;
+    float top = -INFINITY, sum = 0.f, acc[VEC] = {};
+    for (int p0 = 0; p0 < parts; p0 += FLY) {
+      float2 ml[FLY];
+      float y[FLY][VEC];
+#pragma unroll
+      for (int k = 0; k < FLY; ++k) {
+        const int p = p0 + k;
+        ml[k] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) y[k][e] = 0.f;
+        if (p < parts) {
+          const int64_t at = int64_t(p == 0 ? 2 * c + 1 : 2 * (c + p)) * MAXQV + q;
+          ml[k] = __ldcg(a.part_ml + at);
+          const float* src = a.part_o + at * D + lane * VEC;
+          if (VEC == 4) {
+            const float4 z = __ldcg(reinterpret_cast<const float4*>(src));
+            y[k][0] = z.x; y[k][1] = z.y; y[k][VEC - 2] = z.z; y[k][VEC - 1] = z.w;
+          } else {
+            const float2 z = __ldcg(reinterpret_cast<const float2*>(src));
+            y[k][0] = z.x; y[k][1] = z.y;
+          }
+        }
+      }
+      float now = top;
+#pragma unroll
+      for (int k = 0; k < FLY; ++k) now = fmaxf(now, ml[k].x);
+      const float f = top == -INFINITY ? 1.f : mv::fast_exp2((top - now) * a.scale_log2);  // nothing seen so far: zeros (or NaN)
+      sum *= f;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) acc[e] *= f;
+#pragma unroll
+      for (int k = 0; k < FLY; ++k) {
+        const float wt = ml[k].x == -INFINITY ? 1.f : mv::fast_exp2((ml[k].x - now) * a.scale_log2);
+        sum = fmaf(wt, ml[k].y, sum);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) acc[e] = fmaf(wt, y[k][e], acc[e]);
+      }
+      top = now;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int64_t row = int64_t(own.y) + half * a.R + token;
+    uint32_t* const out = reinterpret_cast<uint32_t*>(a.out + (row * a.Hq + head * a.G + (v - token * a.G)) * D + lane * VEC);
+    if (VEC == 4) *reinterpret_cast<uint2*>(out) = make_uint2(mv::pack_bf16(acc[0] * inv, acc[1] * inv), mv::pack_bf16(acc[VEC - 2] * inv, acc[VEC - 1] * inv));
+    else *out = mv::pack_bf16(acc[0] * inv, acc[1] * inv);
+  }
+}
+
+template <typename K, typename... T>
+mv_status launch_after(K kernel, dim3 grid, int threads, int smem, cudaStream_t st, const T&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(unsigned(threads), 1, 1);
+  cfg.dynamicSmemBytes = size_t(smem);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+  mv::g_launches++;
+  if (e != cudaSuccess) (void)cudaGetLastError();
+  return e == cudaSuccess ? MV_OK : MV_ERR_CUDA;
+}
+
+template <int D>
+mv_status launch(const Args& a, const void* q, const void* k8, const void* v8, cudaStream_t st) {
+  static std::atomic<uint64_t> opted{0};  // per device
+  if (!mv::opt_in_smem(chunk_attn_kernel<D>, Lay<D>::SMEM, opted)) return MV_ERR_CUDA;
+  // a pool's row is a token of a KV head (no pages: no entry is accepted, nothing is read)
+  const int64_t rows = std::max<int64_t>(1, a.num_pages * a.Hkv * PS);
+  CUtensorMap tm_q, tm_k, tm_v;
+  if (!mv::make_tmap_bf16_heads(&tm_q, q, uint64_t(a.max_rows), uint64_t(a.Hq), D, uint32_t(a.G), uint32_t(a.R)) ||
+      !mv::make_tmap_u8_2d(&tm_k, k8, uint64_t(rows), PS, D) || !mv::make_tmap_u8_2d(&tm_v, v8, uint64_t(rows), PS, D))
+    return MV_ERR_CUDA;
+  const mv_status e = launch_after(chunk_attn_kernel<D>, dim3(SHARES), NT, Lay<D>::SMEM, st, a, tm_q, tm_k, tm_v);
+  if (e != MV_OK) return e;
+  return launch_after(chunk_merge_kernel<D>, dim3(SHARES, SLICES), MERGE_WARPS * 32, 0, st, a);
+}
+
+}  // namespace
+
+extern "C" size_t mv_chunk_attn_workspace_bytes(const mv_attn_geom* g) {
+  if (mv::check_geom(g) != MV_OK) return 0;
+  return workspace_need(g->head_dim);
+}
+
+extern "C" mv_status mv_dag_chunk_attn_fp8_blk(const mv_chunk_tables* t, const mv_attn_geom* g, const void* q_rot, const void* k_pages8,
+                                               const void* v_pages8, const float* kv_scale, void* out, void* workspace,
+                                               size_t workspace_bytes, void* cuda_stream) {
+  mv::NvtxRange nvtx_range("mv_dag_chunk_attn_fp8_blk");
+  if (!t || t->max_rows < 0 || t->max_tiles < 0 || t->max_entries < 0 || !t->counts) return MV_ERR_INVALID_ARG;
+  const mv_status st = mv::check_geom(g);
+  if (st != MV_OK) return st;
+  if (g->dtype != MV_BF16) return MV_ERR_UNSUPPORTED;
+  if (!(g->sm_scale >= 0.f) || !std::isfinite(g->sm_scale)) return MV_ERR_INVALID_ARG;  // (the largest score is found before it is scaled)
+  const int G = g->n_q_heads / g->n_kv_heads;
+  if (G > BQ || t->rows_per_tile < 1 || t->rows_per_tile > 2 * (BQ / G)) return MV_ERR_UNSUPPORTED;
+  if (g->num_pages > INT32_MAX / PS / g->n_kv_heads) return MV_ERR_UNSUPPORTED;  // the rows of a pool are TMA coordinates
+  if (t->max_tiles > INT32_MAX / g->n_kv_heads) return MV_ERR_UNSUPPORTED;       // (tile, head) is counted in an int
+  if (t->max_rows == 0 || t->max_tiles == 0) return t->max_rows > 0 && (q_rot || out) ? MV_ERR_INVALID_ARG : MV_OK;
+  if (!t->tiles || (t->max_entries > 0 && !t->entries)) return MV_ERR_INVALID_ARG;
+  if (!q_rot || !k_pages8 || !v_pages8 || !kv_scale || !out || q_rot == out) return MV_ERR_INVALID_ARG;
+  for (const void* p : {q_rot, k_pages8, v_pages8, static_cast<const void*>(kv_scale), static_cast<const void*>(out),
+                        static_cast<const void*>(t->tiles), static_cast<const void*>(t->entries)})
+    if ((reinterpret_cast<uintptr_t>(p) & 15) != 0) return MV_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(t->counts) & 3) return MV_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < workspace_need(g->head_dim) || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MV_ERR_WORKSPACE;
+  Args a;
+  a.tiles = reinterpret_cast<const int4*>(t->tiles);
+  a.entries = reinterpret_cast<const int2*>(t->entries);
+  a.counts = t->counts;
+  a.scale = reinterpret_cast<const float2*>(kv_scale);
+  a.out = static_cast<bf16*>(out);
+  a.part_o = static_cast<float*>(workspace);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + part_o_bytes(g->head_dim));
+  a.cuts = reinterpret_cast<Cut*>(static_cast<char*>(workspace) + part_o_bytes(g->head_dim) + part_ml_bytes());
+  a.num_pages = g->num_pages;
+  a.max_rows = t->max_rows;
+  a.max_tiles = t->max_tiles;
+  a.max_entries = t->max_entries;
+  a.Hq = g->n_q_heads;
+  a.Hkv = g->n_kv_heads;
+  a.G = G;
+  a.R = BQ / G;
+  a.scale_log2 = mv::softmax_scale(g) * 1.4426950408889634f;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  return g->head_dim == 128 ? launch<128>(a, q_rot, k_pages8, v_pages8, s) : launch<64>(a, q_rot, k_pages8, v_pages8, s);
+}

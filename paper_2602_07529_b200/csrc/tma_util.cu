@@ -38,6 +38,18 @@ bool make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_tmap_bf16_heads(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint64_t d, uint32_t box_heads, uint32_t box_rows) {
+  EncodeFn fn = encode_fn();
+  if (!fn || !map || !base || rows == 0 || heads == 0 || d < 64 || (d % 64) != 0 || box_heads == 0 || box_heads > 256 || box_rows == 0 || box_rows > 256) return false;
+  if ((reinterpret_cast<uintptr_t>(base) & 15) != 0) return false;
+  const cuuint64_t dims[3] = {d, heads, rows};
+  const cuuint64_t strides[2] = {d * 2, heads * d * 2};
+  const cuuint32_t box[3] = {64, box_heads, box_rows};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool make_tmap_u8_2d(CUtensorMap* map, const void* base, uint64_t rows, uint32_t box_rows, uint32_t cols) {
   EncodeFn fn = encode_fn();
   if (!fn || !map || !base || rows == 0 || (cols != 64 && cols != 128)) return false;

@@ -210,6 +210,76 @@ class StepOnDevice:
         return B.mv_step_tables_read_status(self.tables, stream)
 
 
+class ChunkOnDevice:
+    """A step with any number of new tokens per node, planned on the device: positions and slots (``self.steps``, a StepOnDevice) and
+    the query tiles and page lists of the chunk attention.  ``build()`` may be called (or replayed) again after the tensors in
+    ``self.arrays`` have changed; the capacities are those of the batch given here unless stated."""
+
+    def __init__(self, batch, group: int, device="cuda", max_rows: int | None = None, max_tiles: int | None = None, max_entries: int | None = None):
+        self.steps = StepOnDevice(batch, group, device, blocks=False, max_rows=max_rows)
+        self.arrays, self.batch = self.steps.arrays, self.steps.batch
+        per = 2 * (128 // group)
+        new, off = np.asarray(batch.node_new, np.int64), np.asarray(batch.node_off)
+        page_off = np.asarray(batch.page_off, np.int64)
+        if max_tiles is None:
+            max_tiles = int(((new + per - 1) // per).sum())
+        if max_entries is None:   # every page of the request for each of its receiving nodes
+            max_entries = sum(int((new[lo:hi] > 0).sum()) * int(page_off[hi] - page_off[lo]) for lo, hi in zip(off[:-1], off[1:]))
+        empty = lambda *n: torch.zeros(*n, dtype=torch.int32, device=device)
+        self.t = {"tiles": empty(max(1, max_tiles), 8), "entries": empty(max(1, max_entries), 2), "counts": empty(8)}
+        self.tables = B.ChunkTables(**self.t, max_rows=self.steps.tables.max_rows, rows_per_tile=per)
+        self.workspace = _dev_bytes(B.mv_chunk_tables_workspace_bytes(self.batch), device)
+
+    def build(self, stream=None):
+        self.steps.build(stream)
+        B.mv_chunk_tables_build(self.batch, self.tables, self.workspace, stream)
+        return self.tables
+
+    def read_status(self, stream=None) -> int:
+        return max(self.steps.read_status(stream), B.mv_chunk_tables_read_status(self.tables, stream))
+
+
+class ChunkStateFP8Blk:
+    """A step that writes its new tokens (any number per node) into the block-scaled 8-bit cache and attends over it.  ``form``: a rotary form in
+    place of the geometry's own."""
+
+    def __init__(self, wl: synth.Workload, device="cuda", form=None):
+        assert wl.geom.dtype == "bf16"
+        self.wl, self.device, self.form = wl, device, form
+        g, b = wl.geom, wl.batch
+        self.geom = B.make_geom(g.n_q_heads, g.n_kv_heads, g.head_dim, b.num_pages, g.dtype, g.page_size, 0.0, g.rope_base)
+        shape = (b.num_pages, g.n_kv_heads, g.page_size, g.head_dim)
+        self.k_pages, self.v_pages = (torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2))
+        self.kv_scale = torch.zeros(b.num_pages, g.n_kv_heads, 2, dtype=torch.float32, device=device)
+        if int(np.asarray(b.node_len).sum()) > 0:
+            hist = synth.DagBatch(b.n_req, b.node_off, np.zeros_like(b.node_len), b.node_len, b.parent_off, b.parent_idx,
+                                  b.page_off, b.page_idx, b.page_size, b.num_pages, b.vis_mode, b.pos_mode)
+            _, kh, vh = _stack_values(wl, "history", device)
+            hs = StepOnDevice(hist, g.group, device, blocks=False)
+            self._write(hs.build(), None, kh, vh, None, None)
+            torch.cuda.synchronize()
+            assert hs.read_status() == 0
+            del kh, vh, hs
+        self.q, self.k, self.v = _stack_values(wl, "new" if wl.kind == "decode" else "all", device)
+        self.chunk = ChunkOnDevice(b, g.group, device)
+        self.q_rot = torch.empty_like(self.q)
+        self.out = torch.empty_like(self.q)
+        self.workspace = _dev_bytes(B.mv_chunk_attn_workspace_bytes(self.geom), device)
+
+    def _write(self, tables, q, k, v, q_rot, stream):
+        args = (q, k, v, q_rot, None, self.k_pages, self.v_pages, self.kv_scale, stream)
+        if self.form is None:
+            B.mv_rope_write_kv_fp8_blk(tables, self.geom, *args)
+        else:
+            B.mv_rope_write_kv_fp8_blk_form(tables, self.geom, self.form, *args)
+
+    def step(self, stream=None):
+        t = self.chunk.build(stream)
+        self._write(self.chunk.steps.tables, self.q, self.k, self.v, self.q_rot, stream)
+        B.mv_dag_chunk_attn_fp8_blk(t, self.geom, self.q_rot, self.k_pages, self.v_pages, self.kv_scale, self.out, self.workspace, stream)
+        return self.out
+
+
 class DecodeStateFP8Blk(DecodeState):
     """The same decode workload planned on the device, with the KV history in FP8 pools that carry a scale per (page, KV head)."""
 
