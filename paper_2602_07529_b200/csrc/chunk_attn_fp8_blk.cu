@@ -16,9 +16,9 @@
 // A page whose scale is NaN: its keys become NaN, so the scores of whoever sees it; its values stay finite, so whoever does not
 // see it multiplies them by zero.
 //
-// Warps (512 threads): 0 TMA for K, 1 issuer of the products, 2 TMA for V, 3 the walk over the work and TMA for q; 4-7 bytes to bf16; 8-11 and
-// 12-15 softmax of the two halves, a thread per q-vector (online softmax in log2 units, weights written over the scores as packed
-// bf16, O in tensor memory rescaled only when the row's maximum moved by more than 2^8).
+// Warps (768 threads): 0 TMA for K and V, 1 and 2 issue the products of the two halves, 3 the walk over the work and TMA for q; 4-7 bytes to
+// bf16; 8-15 and 16-23 softmax of the two halves, two threads per q-vector with half of the keys each (weights written over the
+// scores as packed bf16, O in tensor memory rescaled only when the row's reference moved by more than 2^8).
 // One CTA per SM walks its share of the work: (query tile, KV head) after (query tile, KV head) lie on a line of cost, a constant
 // and then one unit per key tile, which the shares cut evenly.  What a cut leaves in two or more shares is joined by a second kernel.
 // Every wait is bounded.
@@ -36,10 +36,11 @@ constexpr int PS = 16, KEYS = 8;        // tokens of a page; pages of a key tile
 constexpr int BQ = 128, BK = 128;       // q-vectors of a half; keys of a tile
 constexpr int SHARES = 148;             // CTAs
 constexpr int SETUP = 2;                // cost of a (query tile, head) besides its key tiles
-constexpr int NT = 512;
-constexpr int RAW = 2;                  // slots for bytes of K, and of V
-constexpr int RING = 3;                 // bf16 tiles (K0 V0 K1 V1 ...)
-constexpr int METAS = 8;                // descriptions of key tiles: K of tile t waits for bytes of t - 2, converted once V of t - 4 is used up
+constexpr int NT = 768;
+constexpr int RAW = 4;                  // pieces of bytes in flight: half a tile of K, the other half, then of V
+constexpr int RING = 4;                 // bf16 tiles (K0 V0 K1 V1 ...)
+constexpr int METAS = 4;                // descriptions of key tiles: K of tile t waits for K of t - 1 converted, so for the scores of t - 3, so for the weights of t - 4
+constexpr int PER_ROW = 2, COLS = BK / PER_ROW;  // threads of a q-vector, keys of a thread
 constexpr int SEGS = 4;                 // segments handed over
 constexpr int MAXQV = 2 * BQ;
 constexpr float RESCALE_THRESHOLD = 8.f;  // log2 units: weights stay below 2^8
@@ -168,15 +169,15 @@ struct Walk {
 
 // What the converters and the softmax threads need of a key tile.
 struct alignas(16) Meta {
-  uint32_t k1[KEYS], k2[KEYS], v1[KEYS], v2[KEYS];  // factors of a page as pairs of bf16: the byte's pattern times the first times the second
-  uint32_t valid[BK / 32];                          // keys that hold a token
-  uint32_t twice;                                   // some second factor is not one
-  uint32_t pad[3];
+  uint32_t factor[2][KEYS];  // of a page of K, of V, as two bf16 numbers: the byte's pattern times the lower times the upper one
+  uint32_t valid[BK / 32];   // keys that hold a token
+  uint32_t twice;            // some upper factor is not one
 };
 struct Shared {
   Meta meta[METAS];
   Segment seg[SEGS];
-  uint64_t seg_full[SEGS], seg_empty[SEGS], q_full, q_empty, raw_full[2][RAW], raw_empty[2][RAW], described[METAS], kv_full[RING], kv_empty[RING], s_full[2], p_full[2], o_done[2], drained;
+  uint64_t seg_full[SEGS], seg_empty[SEGS], q_full, q_empty, raw_full[RAW], raw_empty[RAW], described[METAS], kv_full[RING], kv_empty[RING], s_full[2], p_full[2], o_done[2], drained[2];
+  float exchange[2][PER_ROW][BQ];  // between the threads of a q-vector
   int abort;
   uint32_t tmem;
 };
@@ -185,11 +186,11 @@ template <int D>
 struct Lay {
   static constexpr int TILE = BK * D * 2;   // a bf16 tile: [D / 64 column blocks][128 rows][128 bytes]
   static constexpr int BLOCK = BK * 128;    // a column block
-  static constexpr int BYTES = BK * D;      // a tile of the cache
+  static constexpr int BYTES = BK / 2 * D;  // half a tile of the cache
   static constexpr int Q = 0;               // both halves
   static constexpr int KV = 2 * TILE;
   static constexpr int RAWS = KV + RING * TILE;
-  static constexpr int SHARED = RAWS + 2 * RAW * BYTES;
+  static constexpr int SHARED = RAWS + RAW * BYTES;
   static constexpr int SMEM = SHARED + ((int(sizeof(Shared)) + 127) & ~127);
   static_assert(SMEM <= 227 * 1024, "shared memory of an SM");
 };
@@ -231,30 +232,29 @@ struct Reader {
     ++n;
   }
 };
-constexpr int READERS = 3 + 4 + 8;  // warps
+constexpr int READERS = 3 + 4 + 8 * PER_ROW;  // warps
 
-// ---- bytes of K (and the tiles' descriptions) or of V: eight boxes, a page each, make a tile
-__device__ __forceinline__ uint32_t twice_bf16(int exponent) {  // a pair of bf16 numbers 2^exponent
-  const uint32_t h = uint32_t(127 + exponent) << 7;
-  return h | (h << 16);
-}
+// ---- bytes of K and V: four boxes, a page each, make a piece; and the tiles' descriptions
+__device__ __forceinline__ uint32_t bf16_power(int exponent) { return uint32_t(127 + exponent) << 7; }
 
-template <int D, bool IS_K>
-__device__ __forceinline__ void byte_loader(const Cta& c, const CUtensorMap* map) {
+template <int D>
+__device__ __forceinline__ void byte_loader(const Cta& c, const CUtensorMap* map_k, const CUtensorMap* map_v) {
   const Args& a = *c.a;
+  Shared* const sh = c.sh;
   const int lane = threadIdx.x & 31;
   const bool lead = mv::um::elect_one();
   int tile = 0;  // key tiles of the share so far
+  int pieces = 0;
   bool ok = true;
   Reader rd;
   for (const Segment* at_seg; (at_seg = rd.next(c, ok)); rd.done(c)) {
-    const Segment s = *at_seg;
-    const int first = s.k0 * KEYS, last = min(s.n_ent, s.k1 * KEYS);
+    const int first = at_seg->k0 * KEYS, n_tiles = at_seg->k1 - at_seg->k0, last = min(at_seg->n_ent, at_seg->k1 * KEYS), head = at_seg->head;
+    const int2* const list = a.entries + at_seg->ent0;
     // a window of 32 entries, one per lane
     auto entry_at = [&](int i0) {
       int2 e = make_int2(-1, 0);
       if (i0 + lane < last) {
-        e = __ldcg(a.entries + s.ent0 + i0 + lane);
+        e = __ldcg(list + i0 + lane);
         if (e.x < 0 || e.x >= a.num_pages || e.y < 1 || e.y > PS) {
           atomicExch(a.counts + 4, int(MV_ERR_INVALID_ARG));
           e = make_int2(-1, 0);
@@ -262,69 +262,71 @@ __device__ __forceinline__ void byte_loader(const Cta& c, const CUtensorMap* map
       }
       return e;
     };
-    auto scale_at = [&](const int2& e) { return IS_K && e.x >= 0 ? __ldcg(a.scale + int64_t(e.x) * a.Hkv + s.head) : make_float2(1.f, 1.f); };
+    auto scale_at = [&](const int2& e) { return e.x >= 0 ? __ldcg(a.scale + int64_t(e.x) * a.Hkv + head) : make_float2(1.f, 1.f); };
     int2 e0 = entry_at(first), e1 = entry_at(first + 32);
     float2 s0 = scale_at(e0);
 #pragma unroll 1
-    for (int t = s.k0; t < s.k1; ++t, ++tile) {
-      const int at = ((t - s.k0) * KEYS) & 31;
-      if (at == 0 && t > s.k0) {
+    for (int t = 0; t < n_tiles; ++t, ++tile) {
+      const int at = (t * KEYS) & 31;
+      if (at == 0 && t > 0) {
         e0 = e1;
         s0 = scale_at(e0);
-        e1 = entry_at(t * KEYS + 32);
+        e1 = entry_at(first + t * KEYS + 32);
       }
       const unsigned present = (__ballot_sync(0xffffffffu, e0.x >= 0) >> at) & 0xffu;
-      const int my_row = (e0.x * a.Hkv + s.head) * PS;
-      const int slot = tile % RAW;
-      ok = c.warp_wait(c.sh->raw_empty[IS_K ? 0 : 1][slot], ((tile / RAW) & 1) ^ 1);
-      if (!ok) break;
-      const uint32_t fb = bar(&c.sh->raw_full[IS_K ? 0 : 1][slot]), dst = c.base + Lay<D>::RAWS + ((IS_K ? 0 : RAW) + slot) * Lay<D>::BYTES;
-      if (lead) mv::mbar_arrive_expect_tx(fb, uint32_t(__popc(present)) * (PS * D));
+      const int my_row = (e0.x * a.Hkv + head) * PS;
+#pragma unroll 1
+      for (int p = 0; p < 4 && ok; ++p) {  // K, K, V, V
+        const int half = (p & 1) * 4;
+        ok = c.warp_wait(sh->raw_empty[p], (tile & 1) ^ 1);
+        if (!ok) break;
+        const uint32_t fb = bar(&sh->raw_full[p]), dst = c.base + Lay<D>::RAWS + p * Lay<D>::BYTES;
+        if (lead) mv::mbar_arrive_expect_tx(fb, uint32_t(__popc((present >> half) & 0xfu)) * (PS * D));
 #pragma unroll
-      for (int j = 0; j < KEYS; ++j) {
-        const int row = __shfl_sync(0xffffffffu, my_row, at + j);
-        if (lead && ((present >> j) & 1)) mv::tma_load_2d(dst + j * (PS * D), map, 0, row, fb);
-      }
-      __syncwarp();
-      if (IS_K) {
-        Meta& m = c.sh->meta[tile % METAS];
-        const bool mine = lane >= at && lane < at + KEYS;
-        uint32_t k1 = 0, k2 = 0x3f803f80u, v1 = 0, v2 = 0x3f803f80u;  // a page that is not there: zeros
-        if (e0.x >= 0) {
-          const int ek = mv::blk::scale_exponent(s0.x);
-          int ev = mv::blk::scale_exponent(s0.y);
-          if (ek == 128 || ev == 128) {
-            k1 = 0x7fc07fc0u;
-            ev = 0;
-          } else {
-            k1 = twice_bf16(min(120 + max(ek, V_MIN), 127));
-            k2 = twice_bf16(max(ek - 7, 0));
-          }
-          v1 = twice_bf16(min(120 + max(ev, V_MIN), 127));
-          v2 = twice_bf16(max(ev - 7, 0));
+        for (int j = 0; j < 4; ++j) {
+          const int row = __shfl_sync(0xffffffffu, my_row, at + half + j);
+          if (lead && ((present >> (half + j)) & 1)) mv::tma_load_2d(dst + j * (PS * D), p < 2 ? map_k : map_v, 0, row, fb);
         }
-        // keys that hold a token: sixteen bits per page
-        const uint32_t bits = e0.x >= 0 ? (1u << e0.y) - 1 : 0;
-        const uint32_t pair = bits | (__shfl_down_sync(0xffffffffu, bits, 1) << 16);
-        const bool more_than_one = __any_sync(0xffffffffu, mine && (k2 != 0x3f803f80u || v2 != 0x3f803f80u));
-        if (mine) {
-          m.k1[lane - at] = k1;
-          m.k2[lane - at] = k2;
-          m.v1[lane - at] = v1;
-          m.v2[lane - at] = v2;
-          if (((lane - at) & 1) == 0) m.valid[(lane - at) / 2] = pair;
-        }
-        if (lane == 0) m.twice = more_than_one ? 1 : 0;
+        ++pieces;
         __syncwarp();
-        if (lane == 0) mv::mbar_arrive(bar(&c.sh->described[tile % METAS]));
+        if (p == 0) {
+          // its description: the slot's last readers were through before the wait above ended (see METAS)
+          Meta& m = sh->meta[tile % METAS];
+          const bool mine = lane >= at && lane < at + KEYS;
+          uint32_t fk = 0x3f800000u, fv = 0x3f800000u;  // a page that is not there: zeros
+          if (e0.x >= 0) {
+            const int ek = mv::blk::scale_exponent(s0.x);
+            int ev = mv::blk::scale_exponent(s0.y);
+            if (ek == 128 || ev == 128) {
+              fk |= 0x7fc0u;
+              ev = 0;
+            } else {
+              fk = bf16_power(min(120 + max(ek, V_MIN), 127)) | bf16_power(max(ek - 7, 0)) << 16;
+            }
+            fv = bf16_power(min(120 + max(ev, V_MIN), 127)) | bf16_power(max(ev - 7, 0)) << 16;
+          }
+          // keys that hold a token: sixteen bits per page
+          const uint32_t bits = e0.x >= 0 ? (1u << e0.y) - 1 : 0;
+          const uint32_t pair = bits | (__shfl_down_sync(0xffffffffu, bits, 1) << 16);
+          const bool twice = __any_sync(0xffffffffu, mine && ((fk >> 16) != 0x3f80u || (fv >> 16) != 0x3f80u));
+          if (mine) {
+            m.factor[0][lane - at] = fk;
+            m.factor[1][lane - at] = fv;
+            if (((lane - at) & 1) == 0) m.valid[(lane - at) / 2] = pair;
+          }
+          if (lane == 0) m.twice = twice ? 1 : 0;
+          __syncwarp();
+          if (lane == 0) mv::mbar_arrive(bar(&sh->described[tile % METAS]));
+        }
       }
+      if (!ok) break;
     }
   }
   if (!ok) {
-    // what is in flight must land before the CTA may leave: the last fills of this warp's slots
+    // what is in flight must land before the CTA may leave: the last fill of every piece's slot
     if (lane == 0)
-      for (int k = 1; k <= min(tile, RAW); ++k)
-        (void)mv::mbar_wait_bounded(bar(&c.sh->raw_full[IS_K ? 0 : 1][(tile - k) % RAW]), ((tile - k) / RAW) & 1, 20000000ull);
+      for (int k = 1; k <= min(pieces, RAW); ++k)
+        (void)mv::mbar_wait_bounded(bar(&sh->raw_full[(pieces - k) % RAW]), ((pieces - k) / RAW) & 1, 20000000ull);
     __syncwarp();
   }
 }
@@ -385,21 +387,23 @@ __device__ __forceinline__ uint32_t widen(uint32_t w, uint32_t selector) {  // t
   const uint32_t p = __byte_perm(w, 0, selector);
   return ((p >> 4) & 0x07f007f0u) | (p & 0x80008000u);
 }
+// Half a tile: 64 keys from row0 on.
 template <int D>
-__device__ __forceinline__ void convert_tile(const unsigned char* raw, unsigned char* dst, const uint32_t* f1, const uint32_t* f2, bool twice) {
+__device__ __forceinline__ void convert_half(const unsigned char* raw, unsigned char* dst, int row0, const uint32_t* factor, bool twice) {
   const int tid = threadIdx.x & 127, q8 = tid >> 3, j = tid & 7;
   // Eight threads read 16 bytes each and write 32.  The rows of a pair are chosen so that both meet all banks once: of
   // 128-byte rows, r and r xor 5 (bit 2 sets the read pieces apart, bit 0 the written ones); of 64-byte rows, r and r + 1.
-#pragma unroll 2
-  for (int i = 0; i < 4; ++i) {
-    int row;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int row;  // inside the half
     if (D == 128) {
       const int p = q8 & 3;
       row = 32 * i + (q8 >> 2) * 8 + ((j >> 2) ? (p ^ 5) : p);
     } else {
       row = 32 * i + q8 * 2 + (j >> 2);
     }
-    const uint32_t f = f1[row >> 4], g = f2[row >> 4];
+    const uint32_t both = factor[(row0 + row) >> 4];
+    const uint32_t f = __byte_perm(both, 0, 0x1010);
 #pragma unroll
     for (int h = 0; h < D / 64; ++h) {
       const int ch = h * 4 + (j & 3);  // 16-byte piece of the row
@@ -412,10 +416,11 @@ __device__ __forceinline__ void convert_tile(const unsigned char* raw, unsigned 
         o[2 * k + 1] = mul_bf16x2(widen(w[k], 0x3424), f);
       }
       if (twice) {
+        const uint32_t g = __byte_perm(both, 0, 0x3232);
 #pragma unroll
         for (int k = 0; k < 8; ++k) o[k] = mul_bf16x2(o[k], g);
       }
-      unsigned char* const at = dst + h * Lay<D>::BLOCK + row * 128;
+      unsigned char* const at = dst + h * Lay<D>::BLOCK + (row0 + row) * 128;
       const int k0 = (2 * (j & 3)) ^ (row & 7), k1 = (2 * (j & 3) + 1) ^ (row & 7);
       *reinterpret_cast<uint4*>(at + (k0 << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
       *reinterpret_cast<uint4*>(at + (k1 << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
@@ -435,17 +440,16 @@ __device__ __forceinline__ void converters(const Cta& c) {
       const Meta& m = sh->meta[tile % METAS];
       ok = c.warp_wait(sh->described[tile % METAS], (tile / METAS) & 1);
 #pragma unroll 1
-      for (int kv = 0; kv < 2 && ok; ++kv) {
-        const int e = 2 * tile + kv, slot = tile % RAW;
-        ok = c.warp_wait(sh->raw_full[kv][slot], (tile / RAW) & 1) && c.warp_wait(sh->kv_empty[e % RING], ((e / RING) & 1) ^ 1);
+      for (int p = 0; p < 4 && ok; ++p) {
+        const int e = 2 * tile + (p >> 1);
+        ok = ((p & 1) || c.warp_wait(sh->kv_empty[e % RING], ((e / RING) & 1) ^ 1)) && c.warp_wait(sh->raw_full[p], tile & 1);
         if (!ok) break;
-        convert_tile<D>(c.smem + Lay<D>::RAWS + (kv * RAW + slot) * Lay<D>::BYTES, c.smem + Lay<D>::KV + (e % RING) * Lay<D>::TILE,
-                        kv ? m.v1 : m.k1, kv ? m.v2 : m.k2, m.twice != 0);
-        mv::fence_proxy_async();  // ordinary stores, read next by the tensor core
+        convert_half<D>(c.smem + Lay<D>::RAWS + p * Lay<D>::BYTES, c.smem + Lay<D>::KV + (e % RING) * Lay<D>::TILE, (p & 1) * 64, m.factor[p >> 1], m.twice != 0);
+        if (p & 1) mv::fence_proxy_async();  // ordinary stores, read next by the tensor core
         __syncwarp();
         if (lane == 0) {
-          mv::mbar_arrive(bar(&sh->kv_full[e % RING]));
-          mv::mbar_arrive(bar(&sh->raw_empty[kv][slot]));
+          if (p & 1) mv::mbar_arrive(bar(&sh->kv_full[e % RING]));
+          mv::mbar_arrive(bar(&sh->raw_empty[p]));
         }
       }
     }
@@ -475,105 +479,101 @@ __device__ __forceinline__ void issue_pv(uint32_t o_tmem, uint32_t p_tmem, uint6
     if (k < k_steps) mv::um::mma_ts<true>(o_tmem, p_tmem + k * 8, v_desc + uint32_t((k * 2048) >> 4), idesc);
 }
 
+// One warp per half: its scores, weights and products follow one another (the weights take the place of the scores), and what one half
+// waits for leaves the tensor cores to the other.
 template <int D>
-__device__ __forceinline__ void issuer(const Cta& c) {
+__device__ __forceinline__ void issuer(const Cta& c, int i) {
   const Args& a = *c.a;
   Shared* const sh = c.sh;
   const bool lead = mv::um::elect_one();
-  const uint32_t tmem = sh->tmem;
-  const uint64_t q0 = mv::um::smem_desc(c.base + Lay<D>::Q, 16, 1024), q1 = mv::um::smem_desc(c.base + Lay<D>::Q + Lay<D>::TILE, 16, 1024);
-  const uint32_t s0 = tmem, s1 = tmem + 128, o0 = tmem + 256, o1 = tmem + 384;
+  const uint32_t s_t = sh->tmem + 128 * i, o_t = sh->tmem + 256 + 128 * i;
+  const uint64_t q = mv::um::smem_desc(c.base + Lay<D>::Q + i * Lay<D>::TILE, 16, 1024);
   auto k_desc = [&](int e) { return mv::um::smem_desc(c.base + Lay<D>::KV + (e % RING) * Lay<D>::TILE, 16, 1024); };
   auto v_desc = [&](int e) { return mv::um::smem_desc(c.base + Lay<D>::KV + (e % RING) * Lay<D>::TILE, Lay<D>::BLOCK, 1024); };
   bool ok = true;
   auto full = [&](int e) { ok = ok && c.warp_wait(sh->kv_full[e % RING], (e / RING) & 1); };
-  auto release = [&](int e) { if (lead) mv::um::commit(bar(&sh->kv_empty[e % RING])); };
-  int tile = 0, na = 0, nb = 0;  // key tiles, and tiles of either half so far
+  int tile = 0, n = 0;  // key tiles; those of this half
   Reader rd;
-  for (const Segment* at_seg; (at_seg = rd.next(c, ok)); rd.done(c)) {
-    const Segment s = *at_seg;
-    const bool both = s.rows > a.R;
-    auto pages = [&](int t) { return min(KEYS, s.n_ent - t * KEYS); };
+  for (const Segment* s; (s = rd.next(c, ok)); rd.done(c)) {
+    const int n_tiles = s->k1 - s->k0;
+    int pages = s->n_ent - s->k0 * KEYS;  // left
     ok = c.warp_wait(sh->q_full, rd.n & 1);
+    if (i == 1 && s->rows <= a.R) {  // nothing for this half: it lets go of each tile as it comes
+      if (ok && lead) mv::mbar_arrive(bar(&sh->q_empty));
+#pragma unroll 1
+      for (int e = 2 * tile; e < 2 * (tile + n_tiles) && ok; ++e) {
+        full(e);
+        if (ok && lead) mv::mbar_arrive(bar(&sh->kv_empty[e % RING]));
+      }
+      tile += n_tiles;
+      continue;
+    }
     full(2 * tile);
     if (!ok) break;
     mv::um::fence_after();
-    int here = pages(s.k0);
-    if (lead) {
-      issue_qk<D>(s0, q0, k_desc(2 * tile), here * 16);
-      mv::um::commit(bar(&sh->s_full[0]));
-      if (both) {
-        issue_qk<D>(s1, q1, k_desc(2 * tile), here * 16);
-        mv::um::commit(bar(&sh->s_full[1]));
+    auto scores = [&](int e, int left, bool last) {
+      if (lead) {
+        issue_qk<D>(s_t, q, k_desc(e), min(left, KEYS) * 16);
+        mv::um::commit(bar(&sh->s_full[i]));
+        mv::um::commit(bar(&sh->kv_empty[e % RING]));
+        if (last) mv::um::commit(bar(&sh->q_empty));
       }
-    }
-    release(2 * tile);
-    if (s.k1 - s.k0 == 1 && lead) mv::um::commit(bar(&sh->q_empty));
+      __syncwarp();
+    };
+    scores(2 * tile, pages, n_tiles == 1);
 #pragma unroll 1
-    for (int t = s.k0; t < s.k1; ++t, ++tile) {
-      const int ev = 2 * tile + 1, ek = 2 * tile + 2;
-      const bool go_on = t + 1 < s.k1;
-      const int next = go_on ? pages(t + 1) : 0;
-      full(ev);
-      if (go_on) full(ek);  // here, while the weights of the first half are still being computed
-      ok = ok && c.warp_wait(sh->p_full[0], na & 1);
-      ++na;
+    for (int t = 0; t < n_tiles; ++t, ++tile, ++n, pages -= KEYS) {
+      const int e = 2 * tile + 1;
+      full(e);
+      ok = ok && c.warp_wait(sh->p_full[i], n & 1);
       if (!ok) break;
       mv::um::fence_after();
       if (lead) {
-        issue_pv<D>(o0, s0, v_desc(ev), t > s.k0, here);
-        mv::um::commit(bar(&sh->o_done[0]));
-        if (go_on) {
-          issue_qk<D>(s0, q0, k_desc(ek), next * 16);
-          mv::um::commit(bar(&sh->s_full[0]));
-        }
+        issue_pv<D>(o_t, s_t, v_desc(e), t > 0, min(pages, KEYS));
+        mv::um::commit(bar(&sh->o_done[i]));
+        mv::um::commit(bar(&sh->kv_empty[e % RING]));
       }
       __syncwarp();
-      if (both) {
-        ok = c.warp_wait(sh->p_full[1], nb & 1);
-        ++nb;
-        if (!ok) break;
-        mv::um::fence_after();
-        if (lead) {
-          issue_pv<D>(o1, s1, v_desc(ev), t > s.k0, here);
-          mv::um::commit(bar(&sh->o_done[1]));
-        }
-      }
-      release(ev);
-      if (go_on) {
-        if (both && lead) {
-          issue_qk<D>(s1, q1, k_desc(ek), next * 16);
-          mv::um::commit(bar(&sh->s_full[1]));
-        }
-        release(ek);
-        if (t + 2 == s.k1 && lead) mv::um::commit(bar(&sh->q_empty));  // the segment's last scores
-      }
-      here = next;
-      __syncwarp();
+      if (t + 1 == n_tiles) continue;
+      full(e + 1);
+      if (!ok) break;
+      mv::um::fence_after();
+      scores(e + 1, pages - KEYS, t + 2 == n_tiles);
     }
+    if (!ok) break;
   }
   if (!ok) {  // products may still be in flight: they must have completed before the tensor memory is freed
     __syncwarp();
-    if (lead) mv::um::commit(bar(&sh->drained));
-    (void)mv::mbar_wait_bounded(bar(&sh->drained), 0, 20000000ull);
+    if (lead) mv::um::commit(bar(&sh->drained[i]));
+    (void)mv::mbar_wait_bounded(bar(&sh->drained[i]), 0, 20000000ull);
     __syncwarp();
   }
 }
 
-// ---- softmax of half i: thread = q-vector
+// ---- softmax of half i: a q-vector has two threads, part 0 for the first 64 keys of a tile and the first half of O's columns, part 1 for the rest
+// Barrier of a half's threads that carries a predicate.
+__device__ __forceinline__ bool vote_any(int id, bool p) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(uint32_t(p)), "r"(id), "n"(BQ * PER_ROW) : "memory");
+  return r != 0;
+}
+
 template <int D>
-__device__ __forceinline__ void softmax_group(const Cta& c, int i) {
+__device__ __forceinline__ void softmax_group(const Cta& c, int i, int part) {
   const Args& a = *c.a;
   Shared* const sh = c.sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int v = (warp & 3) * 32 + lane;                       // q-vector of the half = tensor-memory lane
   const uint32_t lane_base = sh->tmem + (uint32_t((warp & 3) * 32) << 16);
-  const uint32_t s_t = lane_base + i * 128, o_t = lane_base + 256 + i * 128;
+  const uint32_t s_t = lane_base + i * 128, o_t = lane_base + 256 + i * 128 + part * (D / 2);
   const int token = v / a.G, in_group = v - token * a.G;      // token inside the half, head inside the group
   int tile = 0, j = 0;                                        // key tiles of the share; of this half
   bool ok = true;
   Reader rd;
-  for (const Segment* s; (s = rd.next(c, ok)); rd.done(c)) {
+  for (;; rd.done(c)) {
+    // (the warps of a half meet at barriers, so they leave together)
+    const Segment* const s = rd.next(c, ok);
+    if (vote_any(1 + i, !ok) || !s) break;
     const int first = i * a.R, rows = min(a.R, s->rows - first);  // tokens of the half
     const int k0 = s->k0, k1 = s->k1;
     if (rows <= 0) {
@@ -581,33 +581,31 @@ __device__ __forceinline__ void softmax_group(const Cta& c, int i) {
       continue;
     }
     const bool live = token < rows;
-    const int own = s->before * PS + s->key0 + first;            // slot of the half's first token in the node's list
-    float r = -INFINITY, l = 0.f;                                // reference (a score), and sum
+    const int own = s->before * PS + s->key0 + first - part * COLS;  // slot of the half's first token in the node's list, counted from this part's keys
+    float r = -INFINITY, l = 0.f;                                    // reference (a score) of the q-vector, sum of this part
 #pragma unroll 1
     for (int t = k0; t < k1; ++t, ++tile, ++j) {
       // The scores first: a half that was left out of earlier tiles has not followed the phases of `described`.  With this tile's scores
-      // there, its description is (and the one eight tiles on is not).
+      // there, its description is (and the next one in its place is not).
       ok = c.warp_wait(sh->s_full[i], j & 1) && c.warp_wait(sh->described[tile % METAS], (tile / METAS) & 1);
-      if (!ok) break;
       mv::um::fence_after();
-      // all 128 columns are read: on a ragged tile only the leading ones were computed, the rest holds something older and is masked
-      uint32_t x[BK];
+      // all columns are read: on a ragged tile only the leading ones were computed, the rest holds something older and is masked
+      uint32_t x[COLS];
 #pragma unroll
-      for (int k = 0; k < BK / 32; ++k) mv::um::ld32(s_t + k * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[k * 32]));
-      const uint4 valid = *reinterpret_cast<const uint4*>(sh->meta[tile % METAS].valid);
+      for (int k = 0; k < COLS / 32; ++k) mv::um::ld32(s_t + part * COLS + k * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[k * 32]));
+      const uint2 valid = reinterpret_cast<const uint2*>(sh->meta[tile % METAS].valid)[part];
       mv::um::wait_ld();
       float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      const int seen = own + 1 - t * BK;  // slots of the tile that the half's first token sees
-      if (seen >= BK && (valid.x & valid.y & valid.z & valid.w) == ~0u) {
+      const int seen = own + 1 - t * BK;  // of this part's slots, those that the half's first token sees
+      if (seen >= COLS && (valid.x & valid.y) == ~0u) {
 #pragma unroll
-        for (int k = 0; k < BK; k += 2) mx4[(k >> 1) & 3] = mv::max3(mx4[(k >> 1) & 3], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+        for (int k = 0; k < COLS; k += 2) mx4[(k >> 1) & 3] = mv::max3(mx4[(k >> 1) & 3], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
       } else {
-        const uint32_t vw[4] = {valid.x, valid.y, valid.z, valid.w};
         const int lim = seen + token;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < COLS / 32; ++q) {
           const int n = lim - 32 * q;
-          const uint32_t see = n >= 32 ? vw[q] : n <= 0 ? 0u : vw[q] & ((1u << n) - 1);
+          const uint32_t held = q ? valid.y : valid.x, see = n >= 32 ? held : n <= 0 ? 0u : held & ((1u << n) - 1);
 #pragma unroll
           for (int k = 0; k < 32; ++k) {
             if (!((see >> k) & 1)) x[32 * q + k] = __float_as_uint(-INFINITY);
@@ -615,32 +613,44 @@ __device__ __forceinline__ void softmax_group(const Cta& c, int i) {
           }
         }
       }
-      const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
-      // the reference moves only when a weight would otherwise pass 2^8
-      const bool move = live && (r == -INFINITY ? mx > -INFINITY : (mx - r) * a.scale_log2 > RESCALE_THRESHOLD);
-      if (t > k0 && __any_sync(0xffffffffu, move)) {
-        const float f = (move && r != -INFINITY) ? mv::fast_exp2((r - mx) * a.scale_log2) : 1.f;
-        ok = c.warp_wait(sh->o_done[i], (j - 1) & 1);  // O holds the tiles before and no product is writing it
-        if (!ok) break;
-        mv::um::fence_after();
-#pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
-          uint32_t o[32];
-          mv::um::ld32(o_t + k * 32, o);
-          mv::um::wait_ld();
-#pragma unroll
-          for (int n = 0; n < 32; ++n) o[n] = __float_as_uint(__uint_as_float(o[n]) * f);
-          mv::um::st32(o_t + k * 32, o);
+      float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+      // The reference moves only when a weight would otherwise pass 2^8.  The barrier carries that, a wait that ran out, and says that all
+      // scores have been read: the weights of part 1 go where part 0 read.
+      const auto moves = [&](float m) { return live && (r == -INFINITY ? m > -INFINITY : (m - r) * a.scale_log2 > RESCALE_THRESHOLD); };
+      mv::um::fence_before();
+      if (vote_any(1 + i, moves(mx) || !ok)) {
+        if (vote_any(1 + i, !ok)) {
+          ok = false;
+          break;
         }
-        l *= f;
+        sh->exchange[i][part][v] = mx;
+        (void)vote_any(1 + i, false);
+        mx = fmaxf(mx, sh->exchange[i][part ^ 1][v]);
+        const bool move = moves(mx);
+        if (t > k0 && __any_sync(0xffffffffu, move)) {
+          // (the tile's scores were issued behind the product before, so O holds the tiles before and no product is writing it)
+          const float f = (move && r != -INFINITY) ? mv::fast_exp2((r - mx) * a.scale_log2) : 1.f;
+          mv::um::fence_after();
+#pragma unroll 1
+          for (int k = 0; k < D / 2; k += 16) {
+            uint32_t o[16];
+            mv::um::ld16(o_t + k, o);
+            mv::um::wait_ld();
+#pragma unroll
+            for (int n = 0; n < 16; ++n) o[n] = __float_as_uint(__uint_as_float(o[n]) * f);
+            mv::um::st16(o_t + k, o);
+          }
+          l *= f;
+        }
+        if (move) r = mx;
       }
-      if (move) r = mx;
+      mv::um::fence_after();
       float ref = r == -INFINITY ? 0.f : r * a.scale_log2;
       const bool far = fabsf(ref) > FAR;  // (a row's own matter: its neighbours in the warp subtract zero)
       if (__any_sync(0xffffffffu, far)) {
         const uint64_t minus = mv::pack_f32x2(far ? -r : 0.f, far ? -r : 0.f);
 #pragma unroll
-        for (int k = 0; k < BK; k += 2) {
+        for (int k = 0; k < COLS; k += 2) {
           float x0, x1;
           mv::unpack_f32x2(mv::add_f32x2(mv::pack_f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), minus), x0, x1);
           x[k] = __float_as_uint(x0);
@@ -651,7 +661,7 @@ __device__ __forceinline__ void softmax_group(const Cta& c, int i) {
       const uint64_t scale2 = mv::pack_f32x2(a.scale_log2, a.scale_log2), nmref2 = mv::pack_f32x2(-ref, -ref);
       uint64_t sum2[4] = {0, 0, 0, 0};
 #pragma unroll
-      for (int k = 0; k < BK / 2; ++k) {  // weights over the scores in place: columns 2k, 2k+1 -> packed column k
+      for (int k = 0; k < COLS / 2; ++k) {  // weights, two to a column
         float x0, x1;
         mv::unpack_f32x2(mv::fma_f32x2(mv::pack_f32x2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])), scale2, nmref2), x0, x1);
         const float p0 = mv::fast_exp2(x0), p1 = mv::fast_exp2(x1);
@@ -663,43 +673,48 @@ __device__ __forceinline__ void softmax_group(const Cta& c, int i) {
         mv::unpack_f32x2(mv::add_f32x2(mv::add_f32x2(sum2[0], sum2[1]), mv::add_f32x2(sum2[2], sum2[3])), e, o);
         l += e + o;
       }
-      mv::um::st32(s_t, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
-      mv::um::st32(s_t + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
+      mv::um::st32(s_t + part * (COLS / 2), *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
       mv::um::wait_st();
       mv::um::fence_before();
       __syncwarp();
       if (lane == 0) mv::mbar_arrive(bar(&sh->p_full[i]));  // the weights (and a rescaled O) are in place
     }
     if (!ok) break;
+    // ---- the segment's result
     ok = c.warp_wait(sh->o_done[i], (j - 1) & 1);
-    if (!ok) break;
+    sh->exchange[i][part][v] = l;
+    if (vote_any(1 + i, !ok)) {
+      ok = false;
+      break;
+    }
     mv::um::fence_after();
+    l = sh->exchange[i][0][v] + sh->exchange[i][1][v];
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int slot = s->slot;
     const int64_t row = int64_t(s->row0) + first + token;
-    bf16* const dst = a.out + (row * a.Hq + s->head * a.G + in_group) * D;
+    bf16* const dst = a.out + (row * a.Hq + s->head * a.G + in_group) * D + part * (D / 2);
     const int64_t at = int64_t(slot) * MAXQV + i * BQ + v;
-    if (slot >= 0 && live) a.part_ml[at] = make_float2(r, l);
-#pragma unroll
-    for (int k = 0; k < D / 32; ++k) {
-      uint32_t o[32];
-      mv::um::ld32(o_t + k * 32, o);
+    if (slot >= 0 && live && part == 0) a.part_ml[at] = make_float2(r, l);
+#pragma unroll 1
+    for (int k = 0; k < D / 2; k += 16) {
+      uint32_t o[16];
+      mv::um::ld16(o_t + k, o);
       mv::um::wait_ld();
       if (live) {
         if (slot < 0) {
 #pragma unroll
-          for (int n = 0; n < 4; ++n) {
+          for (int n = 0; n < 2; ++n) {
             uint4 y;
             y.x = mv::pack_bf16(__uint_as_float(o[8 * n]) * inv, __uint_as_float(o[8 * n + 1]) * inv);
             y.y = mv::pack_bf16(__uint_as_float(o[8 * n + 2]) * inv, __uint_as_float(o[8 * n + 3]) * inv);
             y.z = mv::pack_bf16(__uint_as_float(o[8 * n + 4]) * inv, __uint_as_float(o[8 * n + 5]) * inv);
             y.w = mv::pack_bf16(__uint_as_float(o[8 * n + 6]) * inv, __uint_as_float(o[8 * n + 7]) * inv);
-            *reinterpret_cast<uint4*>(dst + k * 32 + n * 8) = y;
+            *reinterpret_cast<uint4*>(dst + k + n * 8) = y;
           }
         } else {
 #pragma unroll
-          for (int n = 0; n < 8; ++n)
-            *reinterpret_cast<uint4*>(a.part_o + at * D + k * 32 + n * 4) = make_uint4(o[4 * n], o[4 * n + 1], o[4 * n + 2], o[4 * n + 3]);
+          for (int n = 0; n < 4; ++n)
+            *reinterpret_cast<uint4*>(a.part_o + at * D + part * (D / 2) + k + n * 4) = make_uint4(o[4 * n], o[4 * n + 1], o[4 * n + 2], o[4 * n + 3]);
         }
       }
     }
@@ -727,23 +742,22 @@ __global__ void __launch_bounds__(NT, 1) chunk_attn_kernel(const __grid_constant
       mv::mbar_init(bar(&sh->seg_empty[i]), READERS);
     }
     mv::mbar_init(bar(&sh->q_full), 1);
-    mv::mbar_init(bar(&sh->q_empty), 1);
-    for (int i = 0; i < 2; ++i)
-      for (int k = 0; k < RAW; ++k) {
-        mv::mbar_init(bar(&sh->raw_full[i][k]), 1);
-        mv::mbar_init(bar(&sh->raw_empty[i][k]), 4);  // the converters' warps
-      }
+    mv::mbar_init(bar(&sh->q_empty), 2);  // the two issuers
+    for (int i = 0; i < RAW; ++i) {
+      mv::mbar_init(bar(&sh->raw_full[i]), 1);
+      mv::mbar_init(bar(&sh->raw_empty[i]), 4);  // the converters' warps
+    }
     for (int i = 0; i < METAS; ++i) mv::mbar_init(bar(&sh->described[i]), 1);
     for (int i = 0; i < RING; ++i) {
       mv::mbar_init(bar(&sh->kv_full[i]), 4);
-      mv::mbar_init(bar(&sh->kv_empty[i]), 1);
+      mv::mbar_init(bar(&sh->kv_empty[i]), 2);
     }
     for (int i = 0; i < 2; ++i) {
       mv::mbar_init(bar(&sh->s_full[i]), 1);
-      mv::mbar_init(bar(&sh->p_full[i]), 4);
+      mv::mbar_init(bar(&sh->p_full[i]), 4 * PER_ROW);
       mv::mbar_init(bar(&sh->o_done[i]), 1);
+      mv::mbar_init(bar(&sh->drained[i]), 1);
     }
-    mv::mbar_init(bar(&sh->drained), 1);
     mv::mbar_fence_init();
     mv::fence_proxy_async();
   }
@@ -758,19 +772,18 @@ __global__ void __launch_bounds__(NT, 1) chunk_attn_kernel(const __grid_constant
   mv::grid_dependency_wait();
   mv::grid_dependency_launch_dependents();
   const Cta c{&a, smem, base, sh};
-  // launched with 128 registers per thread: 56 + 56 + 2 * 200 = 4 * 128
+  // launched with 80 registers per thread: 48 + 48 + 4 * 96 = 6 * 80
   if (warp < 4) {
-    mv::um::reg_dec<56>();
-    if (warp == 0) byte_loader<D, true>(c, &tm_k);
-    else if (warp == 1) issuer<D>(c);
-    else if (warp == 2) byte_loader<D, false>(c, &tm_v);
-    else q_loader<D>(c, &tm_q);
+    mv::um::reg_dec<48>();
+    if (warp == 0) byte_loader<D>(c, &tm_k, &tm_v);
+    else if (warp == 3) q_loader<D>(c, &tm_q);
+    else issuer<D>(c, warp - 1);
   } else if (warp < 8) {
-    mv::um::reg_dec<56>();
+    mv::um::reg_dec<48>();
     converters<D>(c);
   } else {
-    mv::um::reg_inc<200>();
-    softmax_group<D>(c, (warp - 8) >> 2);
+    mv::um::reg_inc<96>();
+    softmax_group<D>(c, (warp - 8) >> 3, ((warp - 8) >> 2) & 1);
   }
   mv::um::fence_before();
   __syncthreads();
