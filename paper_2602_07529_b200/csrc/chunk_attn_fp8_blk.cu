@@ -16,9 +16,10 @@
 // A page whose scale is NaN: its keys become NaN, so the scores of whoever sees it; its values stay finite, so whoever does not
 // see it multiplies them by zero.
 //
-// Warps (768 threads): 0 TMA for K and V, 1 and 2 issue the products of the two halves, 3 the walk over the work and TMA for q; 4-7 bytes to
-// bf16; 8-15 and 16-23 softmax of the two halves, two threads per q-vector with half of the keys each (weights written over the
-// scores as packed bf16, O in tensor memory rescaled only when the row's reference moved by more than 2^8).
+// Warps (512 threads): 0 TMA for K and V, 1 and 2 issue the products of the two halves, 3 the walk over the work and TMA for q; 4-7
+// bytes to bf16; 8-11 and 12-15 softmax of the two halves, a thread per q-vector (weights written over the scores as packed bf16, O in tensor
+// memory rescaled only when the row's reference moved by more than 2^8).  A tile that is seen whole and moves nothing goes straight
+// through registers; the others read their scores twice, 32 columns at a time, in loops that are small.
 // One CTA per SM walks its share of the work: (query tile, KV head) after (query tile, KV head) lie on a line of cost, a constant
 // and then one unit per key tile, which the shares cut evenly.  What a cut leaves in two or more shares is joined by a second kernel.
 // Every wait is bounded.
@@ -36,11 +37,11 @@ constexpr int PS = 16, KEYS = 8;        // tokens of a page; pages of a key tile
 constexpr int BQ = 128, BK = 128;       // q-vectors of a half; keys of a tile
 constexpr int SHARES = 148;             // CTAs
 constexpr int SETUP = 2;                // cost of a (query tile, head) besides its key tiles
-constexpr int NT = 768;
+constexpr int NT = 512;
 constexpr int RAW = 4;                  // pieces of bytes in flight: half a tile of K, the other half, then of V
 constexpr int RING = 4;                 // bf16 tiles (K0 V0 K1 V1 ...)
 constexpr int METAS = 4;                // descriptions of key tiles: K of tile t waits for K of t - 1 converted, so for the scores of t - 3, so for the weights of t - 4
-constexpr int PER_ROW = 2, COLS = BK / PER_ROW;  // threads of a q-vector, keys of a thread
+constexpr int SOFTMAX_WARPS = 4;        // of a half
 constexpr int SEGS = 4;                 // segments handed over
 constexpr int MAXQV = 2 * BQ;
 constexpr float RESCALE_THRESHOLD = 8.f;  // log2 units: weights stay below 2^8
@@ -176,8 +177,7 @@ struct alignas(16) Meta {
 struct Shared {
   Meta meta[METAS];
   Segment seg[SEGS];
-  uint64_t seg_full[SEGS], seg_empty[SEGS], q_full, q_empty, raw_full[RAW], raw_empty[RAW], described[METAS], kv_full[RING], kv_empty[RING], s_full[2], p_full[2], o_done[2], drained[2];
-  float exchange[2][PER_ROW][BQ];  // between the threads of a q-vector
+  uint64_t seg_full[SEGS], seg_empty[SEGS], q_full, q_empty, raw_full[RAW], raw_empty[RAW], described[METAS], kv_full[RING], kv_empty[RING], s_full[2], p_full[2][2], o_done[2], drained[2];
   int abort;
   uint32_t tmem;
 };
@@ -232,7 +232,7 @@ struct Reader {
     ++n;
   }
 };
-constexpr int READERS = 3 + 4 + 8 * PER_ROW;  // warps
+constexpr int READERS = 3 + 4 + 2 * SOFTMAX_WARPS;  // warps
 
 // ---- bytes of K and V: four boxes, a page each, make a piece; and the tiles' descriptions
 __device__ __forceinline__ uint32_t bf16_power(int exponent) { return uint32_t(127 + exponent) << 7; }
@@ -383,45 +383,59 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t x, uint32_t y) {
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
   return r;
 }
-__device__ __forceinline__ uint32_t widen(uint32_t w, uint32_t selector) {  // two bytes into the upper halves of two half-words, then into place
+// Two bytes, each to the low end of a half-word (the selector), exponent and mantissa four bits up to where bf16 has them, the sign with them
+// to bit 11 and from there to bit 15.  Shifts as multiplications: those have a pipe of their own and twice the rate.
+__device__ __forceinline__ uint32_t widen(uint32_t w, uint32_t selector) {
   const uint32_t p = __byte_perm(w, 0, selector);
-  return ((p >> 4) & 0x07f007f0u) | (p & 0x80008000u);
+  uint32_t r;
+  asm("mad.lo.u32 %0, %1, 16, 0;" : "=r"(r) : "r"(p));
+  asm("mad.lo.u32 %0, %1, 240, %0;" : "+r"(r) : "r"(p & 0x00800080u));
+  return r;
 }
-// Half a tile: 64 keys from row0 on.
+// Half a tile: 64 keys from row0 on.  A thread has two rows and D / 64 pieces of 16 bytes of each.
 template <int D>
 __device__ __forceinline__ void convert_half(const unsigned char* raw, unsigned char* dst, int row0, const uint32_t* factor, bool twice) {
   const int tid = threadIdx.x & 127, q8 = tid >> 3, j = tid & 7;
   // Eight threads read 16 bytes each and write 32.  The rows of a pair are chosen so that both meet all banks once: of
   // 128-byte rows, r and r xor 5 (bit 2 sets the read pieces apart, bit 0 the written ones); of 64-byte rows, r and r + 1.
+  auto row_of = [&](int i) {  // inside the half
+    if (D == 64) return 32 * i + q8 * 2 + (j >> 2);
+    const int p = q8 & 3;
+    return 32 * i + (q8 >> 2) * 8 + ((j >> 2) ? (p ^ 5) : p);
+  };
+  constexpr int PIECES = D / 64;
+  uint4 in[2][PIECES];
+  uint32_t both[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {  // all loads before the first store (the compiler cannot tell the areas apart): 2760 -> 1930 cycles a tile
+    const int row = row_of(i);
+    both[i] = factor[(row0 + row) >> 4];
+#pragma unroll
+    for (int h = 0; h < PIECES; ++h) {
+      const int ch = h * 4 + (j & 3);  // 16-byte piece of the row
+      in[i][h] = *reinterpret_cast<const uint4*>(raw + row * D + ((D == 128 ? ch ^ (row & 7) : ch ^ ((row >> 1) & 3)) << 4));
+    }
+  }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    int row;  // inside the half
-    if (D == 128) {
-      const int p = q8 & 3;
-      row = 32 * i + (q8 >> 2) * 8 + ((j >> 2) ? (p ^ 5) : p);
-    } else {
-      row = 32 * i + q8 * 2 + (j >> 2);
-    }
-    const uint32_t both = factor[(row0 + row) >> 4];
-    const uint32_t f = __byte_perm(both, 0, 0x1010);
+    const int row = row_of(i);
+    const uint32_t f = __byte_perm(both[i], 0, 0x1010);
+    const int k0 = (2 * (j & 3)) ^ (row & 7), k1 = (2 * (j & 3) + 1) ^ (row & 7);
 #pragma unroll
-    for (int h = 0; h < D / 64; ++h) {
-      const int ch = h * 4 + (j & 3);  // 16-byte piece of the row
-      const uint4 in = *reinterpret_cast<const uint4*>(raw + row * D + ((D == 128 ? ch ^ (row & 7) : ch ^ ((row >> 1) & 3)) << 4));
-      const uint32_t w[4] = {in.x, in.y, in.z, in.w};
+    for (int h = 0; h < PIECES; ++h) {
+      const uint32_t w[4] = {in[i][h].x, in[i][h].y, in[i][h].z, in[i][h].w};
       uint32_t o[8];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        o[2 * k] = mul_bf16x2(widen(w[k], 0x1404), f);
-        o[2 * k + 1] = mul_bf16x2(widen(w[k], 0x3424), f);
+        o[2 * k] = mul_bf16x2(widen(w[k], 0x4140), f);
+        o[2 * k + 1] = mul_bf16x2(widen(w[k], 0x4342), f);
       }
       if (twice) {
-        const uint32_t g = __byte_perm(both, 0, 0x3232);
+        const uint32_t g = __byte_perm(both[i], 0, 0x3232);
 #pragma unroll
         for (int k = 0; k < 8; ++k) o[k] = mul_bf16x2(o[k], g);
       }
       unsigned char* const at = dst + h * Lay<D>::BLOCK + (row0 + row) * 128;
-      const int k0 = (2 * (j & 3)) ^ (row & 7), k1 = (2 * (j & 3) + 1) ^ (row & 7);
       *reinterpret_cast<uint4*>(at + (k0 << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
       *reinterpret_cast<uint4*>(at + (k1 << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
     }
@@ -468,15 +482,17 @@ __device__ __forceinline__ void issue_qk(uint32_t s_tmem, uint64_t q_desc, uint6
     mv::um::mma_ss<true>(s_tmem, q_desc + off, k_desc + off, idesc);
   }
 }
-// O_i (+)= P_i V over the first k_steps * 16 keys: P from tensor memory (two bf16 per column), V MN-major
+// O_i (+)= P_i V over keys 64 part .. of the first k_steps * 16: P from tensor memory (two bf16 per column), V MN-major
 template <int D>
-__device__ __forceinline__ void issue_pv(uint32_t o_tmem, uint32_t p_tmem, uint64_t v_desc, bool accumulate, int k_steps) {
+__device__ __forceinline__ void issue_pv(uint32_t o_tmem, uint32_t p_tmem, uint64_t v_desc, bool accumulate, int part, int k_steps) {
   constexpr uint32_t idesc = mv::um::idesc_bf16(BQ, D, 0, 1);
-  if (accumulate) mv::um::mma_ts<true>(o_tmem, p_tmem, v_desc, idesc);
-  else mv::um::mma_ts<false>(o_tmem, p_tmem, v_desc, idesc);
 #pragma unroll
-  for (int k = 1; k < BK / 16; ++k)
-    if (k < k_steps) mv::um::mma_ts<true>(o_tmem, p_tmem + k * 8, v_desc + uint32_t((k * 2048) >> 4), idesc);
+  for (int k = 0; k < BK / 32; ++k) {
+    const int step = part * (BK / 32) + k;
+    if (step >= k_steps) break;
+    if (k > 0 || accumulate) mv::um::mma_ts<true>(o_tmem, p_tmem + step * 8, v_desc + uint32_t((step * 2048) >> 4), idesc);
+    else mv::um::mma_ts<false>(o_tmem, p_tmem + step * 8, v_desc + uint32_t((step * 2048) >> 4), idesc);
+  }
 }
 
 // One warp per half: its scores, weights and products follow one another (the weights take the place of the scores), and what one half
@@ -524,18 +540,25 @@ __device__ __forceinline__ void issuer(const Cta& c, int i) {
 #pragma unroll 1
     for (int t = 0; t < n_tiles; ++t, ++tile, ++n, pages -= KEYS) {
       const int e = 2 * tile + 1;
+      const bool go_on = t + 1 < n_tiles;
       full(e);
-      ok = ok && c.warp_wait(sh->p_full[i], n & 1);
+      const bool next_there = go_on && __all_sync(0xffffffffu, mv::mbar_try_wait(bar(&sh->kv_full[(e + 1) % RING]), ((e + 1) / RING) & 1));  // asked while there is time
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {  // the first 64 keys while the weights of the others are being computed
+        ok = ok && c.warp_wait(sh->p_full[i][part], n & 1);
+        if (!ok) break;
+        mv::um::fence_after();
+        if (lead) issue_pv<D>(o_t, s_t, v_desc(e), t > 0 || part > 0, part, min(pages, KEYS));
+        __syncwarp();
+      }
       if (!ok) break;
-      mv::um::fence_after();
       if (lead) {
-        issue_pv<D>(o_t, s_t, v_desc(e), t > 0, min(pages, KEYS));
-        mv::um::commit(bar(&sh->o_done[i]));
+        if (!go_on) mv::um::commit(bar(&sh->o_done[i]));
         mv::um::commit(bar(&sh->kv_empty[e % RING]));
       }
       __syncwarp();
-      if (t + 1 == n_tiles) continue;
-      full(e + 1);
+      if (!go_on) continue;
+      if (!next_there) full(e + 1);
       if (!ok) break;
       mv::um::fence_after();
       scores(e + 1, pages - KEYS, t + 2 == n_tiles);
@@ -550,160 +573,174 @@ __device__ __forceinline__ void issuer(const Cta& c, int i) {
   }
 }
 
-// ---- softmax of half i: a q-vector has two threads, part 0 for the first 64 keys of a tile and the first half of O's columns, part 1 for the rest
-// Barrier of a half's threads that carries a predicate.
-__device__ __forceinline__ bool vote_any(int id, bool p) {
-  uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(uint32_t(p)), "r"(id), "n"(BQ * PER_ROW) : "memory");
-  return r != 0;
-}
-
+// ---- softmax of half i: thread = q-vector = tensor-memory lane
 template <int D>
-__device__ __forceinline__ void softmax_group(const Cta& c, int i, int part) {
+__device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
   const Args& a = *c.a;
   Shared* const sh = c.sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int v = (warp & 3) * 32 + lane;                       // q-vector of the half = tensor-memory lane
-  const uint32_t lane_base = sh->tmem + (uint32_t((warp & 3) * 32) << 16);
-  const uint32_t s_t = lane_base + i * 128, o_t = lane_base + 256 + i * 128 + part * (D / 2);
-  const int token = v / a.G, in_group = v - token * a.G;      // token inside the half, head inside the group
-  int tile = 0, j = 0;                                        // key tiles of the share; of this half
+  const int v = (warp & 3) * 32 + lane;                       // q-vector of the half
+  const uint32_t lanes = sh->tmem + (uint32_t((warp & 3) * 32) << 16);
+  const uint32_t s_t = lanes + i * 128, o_t = lanes + 256 + i * 128;
+  int tile = 0, j = 0, done = 0;                              // key tiles of the share, of this half; its segments
   bool ok = true;
   Reader rd;
-  for (;; rd.done(c)) {
-    // (the warps of a half meet at barriers, so they leave together)
-    const Segment* const s = rd.next(c, ok);
-    if (vote_any(1 + i, !ok) || !s) break;
+  for (const Segment* s; (s = rd.next(c, ok)); rd.done(c)) {
     const int first = i * a.R, rows = min(a.R, s->rows - first);  // tokens of the half
     const int k0 = s->k0, k1 = s->k1;
     if (rows <= 0) {
       tile += k1 - k0;
       continue;
     }
-    const bool live = token < rows;
-    const int own = s->before * PS + s->key0 + first - part * COLS;  // slot of the half's first token in the node's list, counted from this part's keys
-    float r = -INFINITY, l = 0.f;                                    // reference (a score) of the q-vector, sum of this part
-#pragma unroll 1
-    for (int t = k0; t < k1; ++t, ++tile, ++j) {
-      // The scores first: a half that was left out of earlier tiles has not followed the phases of `described`.  With this tile's scores
-      // there, its description is (and the next one in its place is not).
-      ok = c.warp_wait(sh->s_full[i], j & 1) && c.warp_wait(sh->described[tile % METAS], (tile / METAS) & 1);
-      mv::um::fence_after();
-      // all columns are read: on a ragged tile only the leading ones were computed, the rest holds something older and is masked
-      uint32_t x[COLS];
+    const int own = s->before * PS + s->key0 + first;            // slot of the half's first token in the node's list
+    // reference (a score); a row that is no token's has one that nothing passes, so that its weights are zero
+    float r = v / a.G < rows ? -INFINITY : INFINITY;
+    uint64_t l[2] = {0, 0};                                      // sums: two chains of even and odd columns
+    bool far = false;                                            // some row's reference is beyond FAR
+    const uint64_t scale2 = mv::pack_f32x2(a.scale_log2, a.scale_log2);
+    auto weights = [&](int k, const uint32_t* x, uint64_t nref) {  // of 32 columns, two to a column
+      uint32_t p[16];
 #pragma unroll
-      for (int k = 0; k < COLS / 32; ++k) mv::um::ld32(s_t + part * COLS + k * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[k * 32]));
-      const uint2 valid = reinterpret_cast<const uint2*>(sh->meta[tile % METAS].valid)[part];
-      mv::um::wait_ld();
-      float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      const int seen = own + 1 - t * BK;  // of this part's slots, those that the half's first token sees
-      if (seen >= COLS && (valid.x & valid.y) == ~0u) {
-#pragma unroll
-        for (int k = 0; k < COLS; k += 2) mx4[(k >> 1) & 3] = mv::max3(mx4[(k >> 1) & 3], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
-      } else {
-        const int lim = seen + token;
-#pragma unroll
-        for (int q = 0; q < COLS / 32; ++q) {
-          const int n = lim - 32 * q;
-          const uint32_t held = q ? valid.y : valid.x, see = n >= 32 ? held : n <= 0 ? 0u : held & ((1u << n) - 1);
-#pragma unroll
-          for (int k = 0; k < 32; ++k) {
-            if (!((see >> k) & 1)) x[32 * q + k] = __float_as_uint(-INFINITY);
-            mx4[k & 3] = fmaxf(mx4[k & 3], __uint_as_float(x[32 * q + k]));
-          }
-        }
-      }
-      float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
-      // The reference moves only when a weight would otherwise pass 2^8.  The barrier carries that, a wait that ran out, and says that all
-      // scores have been read: the weights of part 1 go where part 0 read.
-      const auto moves = [&](float m) { return live && (r == -INFINITY ? m > -INFINITY : (m - r) * a.scale_log2 > RESCALE_THRESHOLD); };
-      mv::um::fence_before();
-      if (vote_any(1 + i, moves(mx) || !ok)) {
-        if (vote_any(1 + i, !ok)) {
-          ok = false;
-          break;
-        }
-        sh->exchange[i][part][v] = mx;
-        (void)vote_any(1 + i, false);
-        mx = fmaxf(mx, sh->exchange[i][part ^ 1][v]);
-        const bool move = moves(mx);
-        if (t > k0 && __any_sync(0xffffffffu, move)) {
-          // (the tile's scores were issued behind the product before, so O holds the tiles before and no product is writing it)
-          const float f = (move && r != -INFINITY) ? mv::fast_exp2((r - mx) * a.scale_log2) : 1.f;
-          mv::um::fence_after();
-#pragma unroll 1
-          for (int k = 0; k < D / 2; k += 16) {
-            uint32_t o[16];
-            mv::um::ld16(o_t + k, o);
-            mv::um::wait_ld();
-#pragma unroll
-            for (int n = 0; n < 16; ++n) o[n] = __float_as_uint(__uint_as_float(o[n]) * f);
-            mv::um::st16(o_t + k, o);
-          }
-          l *= f;
-        }
-        if (move) r = mx;
-      }
-      mv::um::fence_after();
-      float ref = r == -INFINITY ? 0.f : r * a.scale_log2;
-      const bool far = fabsf(ref) > FAR;  // (a row's own matter: its neighbours in the warp subtract zero)
-      if (__any_sync(0xffffffffu, far)) {
-        const uint64_t minus = mv::pack_f32x2(far ? -r : 0.f, far ? -r : 0.f);
-#pragma unroll
-        for (int k = 0; k < COLS; k += 2) {
-          float x0, x1;
-          mv::unpack_f32x2(mv::add_f32x2(mv::pack_f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), minus), x0, x1);
-          x[k] = __float_as_uint(x0);
-          x[k + 1] = __float_as_uint(x1);
-        }
-        if (far) ref = 0.f;
-      }
-      const uint64_t scale2 = mv::pack_f32x2(a.scale_log2, a.scale_log2), nmref2 = mv::pack_f32x2(-ref, -ref);
-      uint64_t sum2[4] = {0, 0, 0, 0};
-#pragma unroll
-      for (int k = 0; k < COLS / 2; ++k) {  // weights, two to a column
+      for (int e = 0; e < 16; ++e) {
         float x0, x1;
-        mv::unpack_f32x2(mv::fma_f32x2(mv::pack_f32x2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])), scale2, nmref2), x0, x1);
+        mv::unpack_f32x2(mv::fma_f32x2(mv::pack_u32x2(x[2 * e], x[2 * e + 1]), scale2, nref), x0, x1);
         const float p0 = mv::fast_exp2(x0), p1 = mv::fast_exp2(x1);
-        sum2[k & 3] = mv::add_f32x2(sum2[k & 3], mv::pack_f32x2(p0, p1));
-        x[k] = mv::pack_bf16(p0, p1);
+        l[e & 1] = mv::add_f32x2(l[e & 1], mv::pack_f32x2(p0, p1));
+        p[e] = mv::pack_bf16(p0, p1);
       }
-      {
-        float e, o;
-        mv::unpack_f32x2(mv::add_f32x2(mv::add_f32x2(sum2[0], sum2[1]), mv::add_f32x2(sum2[2], sum2[3])), e, o);
-        l += e + o;
-      }
-      mv::um::st32(s_t + part * (COLS / 2), *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
+      mv::um::st16(s_t + 16 * k, p);
+    };
+    auto hand_over = [&](int half) {  // the weights of 64 keys (and a rescaled O) are in place
       mv::um::wait_st();
       mv::um::fence_before();
       __syncwarp();
-      if (lane == 0) mv::mbar_arrive(bar(&sh->p_full[i]));  // the weights (and a rescaled O) are in place
+      if (lane == 0) mv::mbar_arrive(bar(&sh->p_full[i][half]));
+    };
+    // Is every key of the tile held?  Its description is waited for with the tile before still in flight; for a segment's first tile after its
+    // scores have come: a half that was left out of earlier tiles has not followed the phases of `described`, but with a tile's scores there,
+    // its description is (and the next one in its place is not).
+    bool held = false;
+    auto look = [&](int at) {
+      ok = c.warp_wait(sh->described[at % METAS], (at / METAS) & 1);
+      const uint4 valid = *reinterpret_cast<const uint4*>(sh->meta[at % METAS].valid);
+      held = (valid.x & valid.y & valid.z & valid.w) == ~0u;
+    };
+#pragma unroll 1
+    for (int t = k0; t < k1; ++t, ++tile, ++j) {
+      ok = ok && c.warp_wait(sh->s_full[i], j & 1);
+      if (ok && t == k0) look(tile);
+      if (!ok) break;
+      mv::um::fence_after();
+      if (t > k0 && held && own + 1 - t * BK >= BK && !far) {
+        // The way of nearly all tiles: every key is seen, no reference moves, none is far.  The scores stay in registers.
+        uint32_t x[4][32];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mv::um::ld32(s_t + 32 * k, x[k]);
+        mv::um::wait_ld();
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = mv::max3(mx[(e >> 1) & 3], __uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1]));
+        // a reference moves only when a weight would otherwise pass 2^8
+        const float most = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        if (__all_sync(0xffffffffu, r != -INFINITY && !((most - r) * a.scale_log2 > RESCALE_THRESHOLD))) {
+          const float n = -(r * a.scale_log2);
+          const uint64_t nref = mv::pack_f32x2(n, n);
+          weights(0, x[0], nref);
+          weights(1, x[1], nref);
+          hand_over(0);
+          weights(2, x[2], nref);
+          weights(3, x[3], nref);
+          hand_over(1);
+          if (t + 1 < k1) look(tile + 1);
+          continue;
+        }
+      }
+      // The other tiles: masked, first ones, such that move a reference.  The scores are read again, 32 columns at a time.
+      const uint32_t* const valid = sh->meta[tile % METAS].valid;
+      const int seen = own + 1 - t * BK + v / a.G;  // slots of the tile that the row sees
+      auto read = [&](int k, uint32_t (&x)[32]) {
+        // (on a ragged tile only the leading columns were computed, the rest holds something older and is masked)
+        mv::um::ld32(s_t + 32 * k, x);
+        mv::um::wait_ld();
+        const int n = seen - 32 * k;
+        const uint32_t held = valid[k], see = n >= 32 ? held : n <= 0 ? 0u : held & ((1u << n) - 1);
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          if (!((see >> e) & 1)) x[e] = __float_as_uint(-INFINITY);
+      };
+      float mx = -INFINITY;
+#pragma unroll 1
+      for (int k = 0; k < 4; ++k) {
+        uint32_t x[32];
+        read(k, x);
+        float m2[2] = {mx, -INFINITY};
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) m2[(e >> 1) & 1] = mv::max3(m2[(e >> 1) & 1], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+        mx = fmaxf(m2[0], m2[1]);
+      }
+      const bool move = r == -INFINITY ? mx > -INFINITY : (mx - r) * a.scale_log2 > RESCALE_THRESHOLD;
+      const float f = (move && r != -INFINITY) ? mv::fast_exp2((r - mx) * a.scale_log2) : 1.f;
+      if (move) r = mx;
+      if (t > k0 && __any_sync(0xffffffffu, f != 1.f)) {
+        // (the tile's scores were issued behind the product before, so O holds the tiles before and no product is writing it)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) l[h] = mv::mul_f32x2(l[h], mv::pack_f32x2(f, f));
+#pragma unroll 1
+        for (int k = 0; k < D; k += 32) {
+          uint32_t o[32];
+          mv::um::ld32(o_t + k, o);
+          mv::um::wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+          mv::um::st32(o_t + k, o);
+        }
+      }
+      const float ref = r == -INFINITY ? 0.f : r * a.scale_log2;
+      const bool beyond = fabsf(ref) > FAR && r != INFINITY;  // (a row's own matter: its neighbours subtract zero)
+      const uint64_t nref = beyond ? 0 : mv::pack_f32x2(-ref, -ref), minus = beyond ? mv::pack_f32x2(-r, -r) : 0;
+      far = __any_sync(0xffffffffu, beyond);
+#pragma unroll 1
+      for (int k = 0; k < 4; ++k) {
+        uint32_t x[32];
+        read(k, x);
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          float x0, x1;
+          mv::unpack_f32x2(mv::add_f32x2(mv::pack_u32x2(x[e], x[e + 1]), minus), x0, x1);
+          x[e] = __float_as_uint(x0);
+          x[e + 1] = __float_as_uint(x1);
+        }
+        weights(k, x, nref);
+        if (k & 1) hand_over(k >> 1);
+      }
+      if (t + 1 < k1) look(tile + 1);
     }
     if (!ok) break;
     // ---- the segment's result
-    ok = c.warp_wait(sh->o_done[i], (j - 1) & 1);
-    sh->exchange[i][part][v] = l;
-    if (vote_any(1 + i, !ok)) {
-      ok = false;
-      break;
-    }
+    ok = c.warp_wait(sh->o_done[i], done & 1);
+    ++done;
+    if (!ok) break;
     mv::um::fence_after();
-    l = sh->exchange[i][0][v] + sh->exchange[i][1][v];
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int slot = s->slot;
-    const int64_t row = int64_t(s->row0) + first + token;
-    bf16* const dst = a.out + (row * a.Hq + s->head * a.G + in_group) * D + part * (D / 2);
+    float sum, odd;
+    mv::unpack_f32x2(mv::add_f32x2(l[0], l[1]), sum, odd);
+    sum += odd;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int slot = s->slot, token = v / a.G;  // token inside the half
+    const bool live = token < rows;
+    bf16* const dst = a.out + ((int64_t(s->row0) + first + token) * a.Hq + s->head * a.G + (v - token * a.G)) * D;
     const int64_t at = int64_t(slot) * MAXQV + i * BQ + v;
-    if (slot >= 0 && live && part == 0) a.part_ml[at] = make_float2(r, l);
+    if (slot >= 0 && live) a.part_ml[at] = make_float2(r, sum);
 #pragma unroll 1
-    for (int k = 0; k < D / 2; k += 16) {
-      uint32_t o[16];
-      mv::um::ld16(o_t + k, o);
+    for (int k = 0; k < D; k += 32) {
+      uint32_t o[32];
+      mv::um::ld32(o_t + k, o);
       mv::um::wait_ld();
       if (live) {
         if (slot < 0) {
 #pragma unroll
-          for (int n = 0; n < 2; ++n) {
+          for (int n = 0; n < 4; ++n) {
             uint4 y;
             y.x = mv::pack_bf16(__uint_as_float(o[8 * n]) * inv, __uint_as_float(o[8 * n + 1]) * inv);
             y.y = mv::pack_bf16(__uint_as_float(o[8 * n + 2]) * inv, __uint_as_float(o[8 * n + 3]) * inv);
@@ -713,10 +750,11 @@ __device__ __forceinline__ void softmax_group(const Cta& c, int i, int part) {
           }
         } else {
 #pragma unroll
-          for (int n = 0; n < 4; ++n)
-            *reinterpret_cast<uint4*>(a.part_o + at * D + part * (D / 2) + k + n * 4) = make_uint4(o[4 * n], o[4 * n + 1], o[4 * n + 2], o[4 * n + 3]);
+          for (int n = 0; n < 8; ++n)
+            *reinterpret_cast<uint4*>(a.part_o + at * D + k + n * 4) = make_uint4(o[4 * n], o[4 * n + 1], o[4 * n + 2], o[4 * n + 3]);
         }
       }
+      __syncwarp();
     }
     mv::um::fence_before();
   }
@@ -754,7 +792,7 @@ __global__ void __launch_bounds__(NT, 1) chunk_attn_kernel(const __grid_constant
     }
     for (int i = 0; i < 2; ++i) {
       mv::mbar_init(bar(&sh->s_full[i]), 1);
-      mv::mbar_init(bar(&sh->p_full[i]), 4 * PER_ROW);
+      for (int k = 0; k < 2; ++k) mv::mbar_init(bar(&sh->p_full[i][k]), SOFTMAX_WARPS);
       mv::mbar_init(bar(&sh->o_done[i]), 1);
       mv::mbar_init(bar(&sh->drained[i]), 1);
     }
@@ -772,18 +810,18 @@ __global__ void __launch_bounds__(NT, 1) chunk_attn_kernel(const __grid_constant
   mv::grid_dependency_wait();
   mv::grid_dependency_launch_dependents();
   const Cta c{&a, smem, base, sh};
-  // launched with 80 registers per thread: 48 + 48 + 4 * 96 = 6 * 80
+  // launched with 128 registers per thread: 56 + 72 + 2 * 192 = 4 * 128
   if (warp < 4) {
-    mv::um::reg_dec<48>();
+    mv::um::reg_dec<56>();
     if (warp == 0) byte_loader<D>(c, &tm_k, &tm_v);
     else if (warp == 3) q_loader<D>(c, &tm_q);
     else issuer<D>(c, warp - 1);
   } else if (warp < 8) {
-    mv::um::reg_dec<48>();
+    mv::um::reg_dec<72>();
     converters<D>(c);
   } else {
-    mv::um::reg_inc<96>();
-    softmax_group<D>(c, (warp - 8) >> 3, ((warp - 8) >> 2) & 1);
+    mv::um::reg_inc<192>();
+    softmax_warp<D>(c, (warp - 8) >> 2);
   }
   mv::um::fence_before();
   __syncthreads();
