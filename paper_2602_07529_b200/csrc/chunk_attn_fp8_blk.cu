@@ -16,10 +16,9 @@
 // A page whose scale is NaN: its keys become NaN, so the scores of whoever sees it; its values stay finite, so whoever does not
 // see it multiplies them by zero.
 //
-// Warps (512 threads): 0 TMA for K and V, 1 and 2 issue the products of the two halves, 3 the walk over the work and TMA for q; 4-7
-// bytes to bf16; 8-11 and 12-15 softmax of the two halves, a thread per q-vector (weights written over the scores as packed bf16, O in tensor
-// memory rescaled only when the row's reference moved by more than 2^8).  A tile that is seen whole and moves nothing goes straight
-// through registers; the others read their scores twice, 32 columns at a time, in loops that are small.
+// Warps (512 threads): 0 TMA for K and V, 1 issues the products, 3 the walk over the work and TMA for q; 4-7 bytes to bf16; 8-11 and 12-15
+// softmax of the two halves, a thread per q-vector (weights written over the scores as packed bf16, O in tensor memory rescaled only when the
+// row's reference moved by more than 2^8).  A tile that is seen whole and moves nothing has a way of its own, without a branch.
 // One CTA per SM walks its share of the work: (query tile, KV head) after (query tile, KV head) lie on a line of cost, a constant
 // and then one unit per key tile, which the shares cut evenly.  What a cut leaves in two or more shares is joined by a second kernel.
 // Every wait is bounded.
@@ -68,6 +67,7 @@ struct Args {
   int64_t num_pages;
   int max_rows, max_tiles, max_entries;
   int Hq, Hkv, G, R;
+  int out_32;           // out is aligned to 32 bytes
   float scale_log2;
 };
 
@@ -177,7 +177,7 @@ struct alignas(16) Meta {
 struct Shared {
   Meta meta[METAS];
   Segment seg[SEGS];
-  uint64_t seg_full[SEGS], seg_empty[SEGS], q_full, q_empty, raw_full[RAW], raw_empty[RAW], described[METAS], kv_full[RING], kv_empty[RING], s_full[2], p_full[2][2], o_done[2], drained[2];
+  uint64_t seg_full[SEGS], seg_empty[SEGS], q_full, q_empty, raw_full[RAW], raw_empty[RAW], described[METAS], kv_full[RING], kv_empty[RING], s_full[2], p_full[2][2], o_done[2], drained;
   int abort;
   uint32_t tmem;
 };
@@ -232,7 +232,7 @@ struct Reader {
     ++n;
   }
 };
-constexpr int READERS = 3 + 4 + 2 * SOFTMAX_WARPS;  // warps
+constexpr int READERS = 2 + 4 + 2 * SOFTMAX_WARPS;  // warps
 
 // ---- bytes of K and V: four boxes, a page each, make a piece; and the tiles' descriptions
 __device__ __forceinline__ uint32_t bf16_power(int exponent) { return uint32_t(127 + exponent) << 7; }
@@ -495,85 +495,94 @@ __device__ __forceinline__ void issue_pv(uint32_t o_tmem, uint32_t p_tmem, uint6
   }
 }
 
-// One warp per half: its scores, weights and products follow one another (the weights take the place of the scores), and what one half
-// waits for leaves the tensor cores to the other.
+// The two halves in turn: P V of one tile and the scores of the next for the first half, then for the second.  (With a warp for each half
+// their products alternate in the pipe, both are done late, and the halves fall into step: either all compute weights or all wait.)
 template <int D>
-__device__ __forceinline__ void issuer(const Cta& c, int i) {
+__device__ __forceinline__ void issuer(const Cta& c) {
   const Args& a = *c.a;
   Shared* const sh = c.sh;
   const bool lead = mv::um::elect_one();
-  const uint32_t s_t = sh->tmem + 128 * i, o_t = sh->tmem + 256 + 128 * i;
-  const uint64_t q = mv::um::smem_desc(c.base + Lay<D>::Q + i * Lay<D>::TILE, 16, 1024);
+  const uint32_t tmem = sh->tmem;
+  const uint64_t q0 = mv::um::smem_desc(c.base + Lay<D>::Q, 16, 1024);
   auto k_desc = [&](int e) { return mv::um::smem_desc(c.base + Lay<D>::KV + (e % RING) * Lay<D>::TILE, 16, 1024); };
   auto v_desc = [&](int e) { return mv::um::smem_desc(c.base + Lay<D>::KV + (e % RING) * Lay<D>::TILE, Lay<D>::BLOCK, 1024); };
   bool ok = true;
   auto full = [&](int e) { ok = ok && c.warp_wait(sh->kv_full[e % RING], (e / RING) & 1); };
-  int tile = 0, n = 0;  // key tiles; those of this half
+  int tile = 0, n[2] = {0, 0};  // key tiles; those of either half
   Reader rd;
   for (const Segment* s; (s = rd.next(c, ok)); rd.done(c)) {
-    const int n_tiles = s->k1 - s->k0;
+    const int n_tiles = s->k1 - s->k0, halves = s->rows > a.R ? 2 : 1;
     int pages = s->n_ent - s->k0 * KEYS;  // left
     ok = c.warp_wait(sh->q_full, rd.n & 1);
-    if (i == 1 && s->rows <= a.R) {  // nothing for this half: it lets go of each tile as it comes
-      if (ok && lead) mv::mbar_arrive(bar(&sh->q_empty));
-#pragma unroll 1
-      for (int e = 2 * tile; e < 2 * (tile + n_tiles) && ok; ++e) {
-        full(e);
-        if (ok && lead) mv::mbar_arrive(bar(&sh->kv_empty[e % RING]));
-      }
-      tile += n_tiles;
-      continue;
-    }
     full(2 * tile);
     if (!ok) break;
     mv::um::fence_after();
-    auto scores = [&](int e, int left, bool last) {
-      if (lead) {
-        issue_qk<D>(s_t, q, k_desc(e), min(left, KEYS) * 16);
-        mv::um::commit(bar(&sh->s_full[i]));
-        mv::um::commit(bar(&sh->kv_empty[e % RING]));
-        if (last) mv::um::commit(bar(&sh->q_empty));
-      }
-      __syncwarp();
+    auto scores = [&](int i, int e, int left) {
+      issue_qk<D>(tmem + 128 * i, q0 + uint32_t((i * Lay<D>::TILE) >> 4), k_desc(e), min(left, KEYS) * 16);
+      mv::um::commit(bar(&sh->s_full[i]));
     };
-    scores(2 * tile, pages, n_tiles == 1);
+    auto scores_done = [&](int e, bool last) {  // of both halves
+      mv::um::commit(bar(&sh->kv_empty[e % RING]));
+      if (last) mv::um::commit(bar(&sh->q_empty));
+    };
+    if (lead) {
+      scores(0, 2 * tile, pages);
+      if (halves == 2) scores(1, 2 * tile, pages);
+      scores_done(2 * tile, n_tiles == 1);
+    }
+    __syncwarp();
 #pragma unroll 1
-    for (int t = 0; t < n_tiles; ++t, ++tile, ++n, pages -= KEYS) {
+    for (int t = 0; t < n_tiles; ++t, ++tile, pages -= KEYS) {
       const int e = 2 * tile + 1;
       const bool go_on = t + 1 < n_tiles;
       full(e);
-      const bool next_there = go_on && __all_sync(0xffffffffu, mv::mbar_try_wait(bar(&sh->kv_full[(e + 1) % RING]), ((e + 1) / RING) & 1));  // asked while there is time
+      bool next_there = go_on && __all_sync(0xffffffffu, mv::mbar_try_wait(bar(&sh->kv_full[(e + 1) % RING]), ((e + 1) / RING) & 1));  // asked while there is time
 #pragma unroll
-      for (int part = 0; part < 2; ++part) {  // the first 64 keys while the weights of the others are being computed
-        ok = ok && c.warp_wait(sh->p_full[i][part], n & 1);
+      for (int i = 0; i < 2; ++i) {
+        if (i == halves) break;
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {  // the first 64 keys while the weights of the others are being computed
+          ok = ok && c.warp_wait(sh->p_full[i][part], n[i] & 1);
+          if (!ok) break;
+          mv::um::fence_after();
+          if (lead) issue_pv<D>(tmem + 256 + 128 * i, tmem + 128 * i, v_desc(e), t > 0 || part > 0, part, min(pages, KEYS));
+          __syncwarp();
+        }
+        ++n[i];
         if (!ok) break;
-        mv::um::fence_after();
-        if (lead) issue_pv<D>(o_t, s_t, v_desc(e), t > 0 || part > 0, part, min(pages, KEYS));
+        if (go_on && !next_there) {
+          full(e + 1);
+          if (!ok) break;
+          next_there = true;
+        }
+        if (go_on) mv::um::fence_after();
+        if (lead) {
+          if (go_on) scores(i, e + 1, pages - KEYS);
+          else mv::um::commit(bar(&sh->o_done[i]));
+        }
         __syncwarp();
       }
       if (!ok) break;
       if (lead) {
-        if (!go_on) mv::um::commit(bar(&sh->o_done[i]));
         mv::um::commit(bar(&sh->kv_empty[e % RING]));
+        if (go_on) scores_done(e + 1, t + 2 == n_tiles);
       }
       __syncwarp();
-      if (!go_on) continue;
-      if (!next_there) full(e + 1);
-      if (!ok) break;
-      mv::um::fence_after();
-      scores(e + 1, pages - KEYS, t + 2 == n_tiles);
     }
     if (!ok) break;
   }
   if (!ok) {  // products may still be in flight: they must have completed before the tensor memory is freed
     __syncwarp();
-    if (lead) mv::um::commit(bar(&sh->drained[i]));
-    (void)mv::mbar_wait_bounded(bar(&sh->drained[i]), 0, 20000000ull);
+    if (lead) mv::um::commit(bar(&sh->drained));
+    (void)mv::mbar_wait_bounded(bar(&sh->drained), 0, 20000000ull);
     __syncwarp();
   }
 }
 
 // ---- softmax of half i: thread = q-vector = tensor-memory lane
+__device__ __forceinline__ void store_32_bytes(void* p, const uint32_t (&x)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n" ::"l"(p), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
+}
 template <int D>
 __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
   const Args& a = *c.a;
@@ -729,7 +738,14 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const int slot = s->slot, token = v / a.G;  // token inside the half
     const bool live = token < rows;
-    bf16* const dst = a.out + ((int64_t(s->row0) + first + token) * a.Hq + s->head * a.G + (v - token * a.G)) * D;
+    bf16* pair_dst[2];  // of this thread's row and its neighbour's, the even one first
+    bool pair_live[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const int w = (v & ~1) + n, t = w / a.G;
+      pair_dst[n] = a.out + ((int64_t(s->row0) + first + t) * a.Hq + s->head * a.G + (w - t * a.G)) * D;
+      pair_live[n] = t < rows;
+    }
     const int64_t at = int64_t(slot) * MAXQV + i * BQ + v;
     if (slot >= 0 && live) a.part_ml[at] = make_float2(r, sum);
 #pragma unroll 1
@@ -737,22 +753,33 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
       uint32_t o[32];
       mv::um::ld32(o_t + k, o);
       mv::um::wait_ld();
-      if (live) {
-        if (slot < 0) {
+      if (slot < 0) {
+        // 64 bytes of a row.  Two neighbouring rows are exchanged in halves, so that a pair of threads writes 64 bytes side by side: what
+        // costs is the number of places a store goes to.
+        const bool odd_row = lane & 1;
+        uint32_t p[2][8];
 #pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            uint4 y;
-            y.x = mv::pack_bf16(__uint_as_float(o[8 * n]) * inv, __uint_as_float(o[8 * n + 1]) * inv);
-            y.y = mv::pack_bf16(__uint_as_float(o[8 * n + 2]) * inv, __uint_as_float(o[8 * n + 3]) * inv);
-            y.z = mv::pack_bf16(__uint_as_float(o[8 * n + 4]) * inv, __uint_as_float(o[8 * n + 5]) * inv);
-            y.w = mv::pack_bf16(__uint_as_float(o[8 * n + 6]) * inv, __uint_as_float(o[8 * n + 7]) * inv);
-            *reinterpret_cast<uint4*>(dst + k + n * 8) = y;
-          }
-        } else {
-#pragma unroll
-          for (int n = 0; n < 8; ++n)
-            *reinterpret_cast<uint4*>(a.part_o + at * D + k + n * 4) = make_uint4(o[4 * n], o[4 * n + 1], o[4 * n + 2], o[4 * n + 3]);
+        for (int n = 0; n < 8; ++n) {
+          const uint32_t lo = mv::pack_bf16(__uint_as_float(o[2 * n]) * inv, __uint_as_float(o[2 * n + 1]) * inv);
+          const uint32_t hi = mv::pack_bf16(__uint_as_float(o[2 * n + 16]) * inv, __uint_as_float(o[2 * n + 17]) * inv);
+          const uint32_t got = __shfl_xor_sync(0xffffffffu, odd_row ? lo : hi, 1);
+          p[0][n] = odd_row ? got : lo;  // of the even row
+          p[1][n] = odd_row ? hi : got;  // of the odd one
         }
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+          if (pair_live[n]) {
+            bf16* const to = pair_dst[n] + k + (odd_row ? 16 : 0);
+            if (a.out_32) {
+              store_32_bytes(to, p[n]);
+            } else {
+              reinterpret_cast<uint4*>(to)[0] = make_uint4(p[n][0], p[n][1], p[n][2], p[n][3]);
+              reinterpret_cast<uint4*>(to)[1] = make_uint4(p[n][4], p[n][5], p[n][6], p[n][7]);
+            }
+          }
+      } else if (live) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) store_32_bytes(a.part_o + at * D + k + n * 8, *reinterpret_cast<uint32_t(*)[8]>(&o[8 * n]));
       }
       __syncwarp();
     }
@@ -780,7 +807,7 @@ __global__ void __launch_bounds__(NT, 1) chunk_attn_kernel(const __grid_constant
       mv::mbar_init(bar(&sh->seg_empty[i]), READERS);
     }
     mv::mbar_init(bar(&sh->q_full), 1);
-    mv::mbar_init(bar(&sh->q_empty), 2);  // the two issuers
+    mv::mbar_init(bar(&sh->q_empty), 1);
     for (int i = 0; i < RAW; ++i) {
       mv::mbar_init(bar(&sh->raw_full[i]), 1);
       mv::mbar_init(bar(&sh->raw_empty[i]), 4);  // the converters' warps
@@ -788,14 +815,14 @@ __global__ void __launch_bounds__(NT, 1) chunk_attn_kernel(const __grid_constant
     for (int i = 0; i < METAS; ++i) mv::mbar_init(bar(&sh->described[i]), 1);
     for (int i = 0; i < RING; ++i) {
       mv::mbar_init(bar(&sh->kv_full[i]), 4);
-      mv::mbar_init(bar(&sh->kv_empty[i]), 2);
+      mv::mbar_init(bar(&sh->kv_empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
       mv::mbar_init(bar(&sh->s_full[i]), 1);
       for (int k = 0; k < 2; ++k) mv::mbar_init(bar(&sh->p_full[i][k]), SOFTMAX_WARPS);
       mv::mbar_init(bar(&sh->o_done[i]), 1);
-      mv::mbar_init(bar(&sh->drained[i]), 1);
     }
+    mv::mbar_init(bar(&sh->drained), 1);
     mv::mbar_fence_init();
     mv::fence_proxy_async();
   }
@@ -814,8 +841,8 @@ __global__ void __launch_bounds__(NT, 1) chunk_attn_kernel(const __grid_constant
   if (warp < 4) {
     mv::um::reg_dec<56>();
     if (warp == 0) byte_loader<D>(c, &tm_k, &tm_v);
+    else if (warp == 1) issuer<D>(c);
     else if (warp == 3) q_loader<D>(c, &tm_q);
-    else issuer<D>(c, warp - 1);
   } else if (warp < 8) {
     mv::um::reg_dec<72>();
     converters<D>(c);
@@ -977,6 +1004,7 @@ extern "C" mv_status mv_dag_chunk_attn_fp8_blk(const mv_chunk_tables* t, const m
   a.Hkv = g->n_kv_heads;
   a.G = G;
   a.R = BQ / G;
+  a.out_32 = (reinterpret_cast<uintptr_t>(out) & 31) == 0;
   a.scale_log2 = mv::softmax_scale(g) * 1.4426950408889634f;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   return g->head_dim == 128 ? launch<128>(a, q_rot, k_pages8, v_pages8, s) : launch<64>(a, q_rot, k_pages8, v_pages8, s);
