@@ -16,7 +16,7 @@
 // A page whose scale is NaN: its keys become NaN, so the scores of whoever sees it; its values stay finite, so whoever does not
 // see it multiplies them by zero.
 //
-// Warps (512 threads): 0 TMA for K and V, 1 issues the products, 3 the walk over the work and TMA for q; 4-7 bytes to bf16; 8-11 and 12-15
+// Warps (512 threads): 0 and 2 TMA for K and V, 1 issues the products, 3 the walk over the work and TMA for q; 4-7 bytes to bf16; 8-11 and 12-15
 // softmax of the two halves, a thread per q-vector (weights written over the scores as packed bf16, O in tensor memory rescaled only when the
 // row's reference moved by more than 2^8).  A tile that is seen whole and moves nothing has a way of its own, without a branch.
 // One CTA per SM walks its share of the work: (query tile, KV head) after (query tile, KV head) lie on a line of cost, a constant
@@ -204,12 +204,18 @@ struct Cta {
   unsigned char* smem;
   uint32_t base;
   Shared* sh;
+  // (Small: all roles run at once, and what they execute has to stay in the SM's instruction cache.  With the polling loops of
+  // mbar_wait_bounded in each of these places the kernel took 1.6 times as long as soon as one more loop was added to it.)
   __device__ __forceinline__ bool wait(const uint64_t& b, uint32_t parity) const {
-    if (mv::mbar_try_wait(bar(&b), parity)) return true;
-    if (*reinterpret_cast<volatile int*>(&sh->abort)) return false;
-    if (!mv::mbar_wait_bounded(bar(&b), parity, 2000000000ull, &sh->abort)) {
-      if (!*reinterpret_cast<volatile int*>(&sh->abort)) atomicExch(a->counts + 4, int(MV_ERR_TIMEOUT));
-      *reinterpret_cast<volatile int*>(&sh->abort) = 1;
+    uint64_t since = 0;
+    for (uint32_t n = 1; !mv::mbar_try_wait(bar(&b), parity); ++n) {
+      if (n % 256 != 0) continue;
+      const uint64_t now = mv::global_timer_ns();
+      if (since == 0) since = now;
+      volatile int* const abort = &sh->abort;
+      if (*abort == 0 && now - since <= 2000000000ull) continue;
+      if (*abort == 0) atomicExch(a->counts + 4, int(MV_ERR_TIMEOUT));
+      *abort = 1;
       return false;
     }
     return true;
@@ -264,13 +270,13 @@ __device__ __forceinline__ void byte_loader(const Cta& c, const CUtensorMap* map
     };
     auto scale_at = [&](const int2& e) { return e.x >= 0 ? __ldcg(a.scale + int64_t(e.x) * a.Hkv + head) : make_float2(1.f, 1.f); };
     int2 e0 = entry_at(first), e1 = entry_at(first + 32);
-    float2 s0 = scale_at(e0);
+    float2 s0 = scale_at(e0), s1 = make_float2(1.f, 1.f);
 #pragma unroll 1
     for (int t = 0; t < n_tiles; ++t, ++tile) {
       const int at = (t * KEYS) & 31;
       if (at == 0 && t > 0) {
         e0 = e1;
-        s0 = scale_at(e0);
+        s0 = s1;
         e1 = entry_at(first + t * KEYS + 32);
       }
       const unsigned present = (__ballot_sync(0xffffffffu, e0.x >= 0) >> at) & 0xffu;
@@ -320,6 +326,7 @@ __device__ __forceinline__ void byte_loader(const Cta& c, const CUtensorMap* map
         }
       }
       if (!ok) break;
+      if (at == 16) s1 = scale_at(e1);
     }
   }
   if (!ok) {
@@ -430,14 +437,19 @@ __device__ __forceinline__ void convert_half(const unsigned char* raw, unsigned 
         o[2 * k] = mul_bf16x2(widen(w[k], 0x4140), f);
         o[2 * k + 1] = mul_bf16x2(widen(w[k], 0x4342), f);
       }
-      if (twice) {
-        const uint32_t g = __byte_perm(both[i], 0, 0x3232);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = mul_bf16x2(o[k], g);
-      }
       unsigned char* const at = dst + h * Lay<D>::BLOCK + (row0 + row) * 128;
       *reinterpret_cast<uint4*>(at + (k0 << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
       *reinterpret_cast<uint4*>(at + (k1 << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+    }
+  }
+  if (twice) {  // (scales above 2^7) the upper factors, over what this thread has just stored
+#pragma unroll 1
+    for (int n = 0; n < 4 * PIECES; ++n) {
+      const int i = n & 1, h = (n >> 1) & (PIECES - 1), row = row_of(i), k = (2 * (j & 3) + n / (2 * PIECES)) ^ (row & 7);
+      const uint32_t g = __byte_perm(both[i], 0, 0x3232);
+      uint4* const at = reinterpret_cast<uint4*>(dst + h * Lay<D>::BLOCK + (row0 + row) * 128 + (k << 4));
+      const uint4 y = *at;
+      *at = make_uint4(mul_bf16x2(y.x, g), mul_bf16x2(y.y, g), mul_bf16x2(y.z, g), mul_bf16x2(y.w, g));
     }
   }
 }
@@ -508,7 +520,7 @@ __device__ __forceinline__ void issuer(const Cta& c) {
   auto v_desc = [&](int e) { return mv::um::smem_desc(c.base + Lay<D>::KV + (e % RING) * Lay<D>::TILE, Lay<D>::BLOCK, 1024); };
   bool ok = true;
   auto full = [&](int e) { ok = ok && c.warp_wait(sh->kv_full[e % RING], (e / RING) & 1); };
-  int tile = 0, n[2] = {0, 0};  // key tiles; those of either half
+  int tile = 0, n_second = 0;  // key tiles; those of the second half
   Reader rd;
   for (const Segment* s; (s = rd.next(c, ok)); rd.done(c)) {
     const int n_tiles = s->k1 - s->k0, halves = s->rows > a.R ? 2 : 1;
@@ -537,18 +549,17 @@ __device__ __forceinline__ void issuer(const Cta& c) {
       const bool go_on = t + 1 < n_tiles;
       full(e);
       bool next_there = go_on && __all_sync(0xffffffffu, mv::mbar_try_wait(bar(&sh->kv_full[(e + 1) % RING]), ((e + 1) / RING) & 1));  // asked while there is time
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (i == halves) break;
+#pragma unroll 1
+      for (int i = 0; i < halves; ++i) {
 #pragma unroll
         for (int part = 0; part < 2; ++part) {  // the first 64 keys while the weights of the others are being computed
-          ok = ok && c.warp_wait(sh->p_full[i][part], n[i] & 1);
+          ok = ok && c.warp_wait(sh->p_full[i][part], (i ? n_second : tile) & 1);
           if (!ok) break;
           mv::um::fence_after();
           if (lead) issue_pv<D>(tmem + 256 + 128 * i, tmem + 128 * i, v_desc(e), t > 0 || part > 0, part, min(pages, KEYS));
           __syncwarp();
         }
-        ++n[i];
+        n_second += i;
         if (!ok) break;
         if (go_on && !next_there) {
           full(e + 1);
@@ -637,11 +648,11 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
 #pragma unroll 1
     for (int t = k0; t < k1; ++t, ++tile, ++j) {
       ok = ok && c.warp_wait(sh->s_full[i], j & 1);
-      if (ok && t == k0) look(tile);
+      if (ok) look(tile);
       if (!ok) break;
       mv::um::fence_after();
-      if (t > k0 && held && own + 1 - t * BK >= BK && !far) {
-        // The way of nearly all tiles: every key is seen, no reference moves, none is far.  The scores stay in registers.
+      if (held && own + 1 - t * BK >= BK && !far) {
+        // The way of nearly all tiles: every key is seen, no reference moves but a segment's first ones, none is far.  The scores stay in registers.
         uint32_t x[4][32];
 #pragma unroll
         for (int k = 0; k < 4; ++k) mv::um::ld32(s_t + 32 * k, x[k]);
@@ -653,8 +664,10 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
           for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = mv::max3(mx[(e >> 1) & 3], __uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1]));
         // a reference moves only when a weight would otherwise pass 2^8
         const float most = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        if (__all_sync(0xffffffffu, r != -INFINITY && !((most - r) * a.scale_log2 > RESCALE_THRESHOLD))) {
-          const float n = -(r * a.scale_log2);
+        const float ref = t == k0 && r != INFINITY ? most : r, n = -(ref * a.scale_log2);
+        const bool fine = ref == INFINITY ? r == INFINITY : ref != -INFINITY && !((most - ref) * a.scale_log2 > RESCALE_THRESHOLD) && fabsf(n) <= FAR;
+        if (__all_sync(0xffffffffu, fine)) {
+          r = ref;
           const uint64_t nref = mv::pack_f32x2(n, n);
           weights(0, x[0], nref);
           weights(1, x[1], nref);
@@ -662,7 +675,6 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
           weights(2, x[2], nref);
           weights(3, x[3], nref);
           hand_over(1);
-          if (t + 1 < k1) look(tile + 1);
           continue;
         }
       }
@@ -724,7 +736,6 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
         weights(k, x, nref);
         if (k & 1) hand_over(k >> 1);
       }
-      if (t + 1 < k1) look(tile + 1);
     }
     if (!ok) break;
     // ---- the segment's result
