@@ -532,6 +532,7 @@ __device__ __forceinline__ void issuer(const Cta& c) {
     auto scores = [&](int i, int e, int left) {
       issue_qk<D>(tmem + 128 * i, q0 + uint32_t((i * Lay<D>::TILE) >> 4), k_desc(e), min(left, KEYS) * 16);
       mv::um::commit(bar(&sh->s_full[i]));
+      mv::mbar_arrive(bar(&sh->s_full[i]));  // and hands on the tile's description, which came here through the converters' barriers
     };
     auto scores_done = [&](int e, bool last) {  // of both halves
       mv::um::commit(bar(&sh->kv_empty[e % RING]));
@@ -636,22 +637,13 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
       __syncwarp();
       if (lane == 0) mv::mbar_arrive(bar(&sh->p_full[i][half]));
     };
-    // Is every key of the tile held?  Its description is waited for with the tile before still in flight; for a segment's first tile after its
-    // scores have come: a half that was left out of earlier tiles has not followed the phases of `described`, but with a tile's scores there,
-    // its description is (and the next one in its place is not).
-    bool held = false;
-    auto look = [&](int at) {
-      ok = c.warp_wait(sh->described[at % METAS], (at / METAS) & 1);
-      const uint4 valid = *reinterpret_cast<const uint4*>(sh->meta[at % METAS].valid);
-      held = (valid.x & valid.y & valid.z & valid.w) == ~0u;
-    };
 #pragma unroll 1
     for (int t = k0; t < k1; ++t, ++tile, ++j) {
-      ok = ok && c.warp_wait(sh->s_full[i], j & 1);
-      if (ok) look(tile);
+      ok = c.warp_wait(sh->s_full[i], j & 1);
       if (!ok) break;
       mv::um::fence_after();
-      if (held && own + 1 - t * BK >= BK && !far) {
+      const uint4 held = *reinterpret_cast<const uint4*>(sh->meta[tile % METAS].valid);
+      if (!far && own + 1 - t * BK >= BK && (held.x & held.y & held.z & held.w) == ~0u) {
         // The way of nearly all tiles: every key is seen, no reference moves but a segment's first ones, none is far.  The scores stay in registers.
         uint32_t x[4][32];
 #pragma unroll
@@ -829,7 +821,7 @@ __global__ void __launch_bounds__(NT, 1) chunk_attn_kernel(const __grid_constant
       mv::mbar_init(bar(&sh->kv_empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mv::mbar_init(bar(&sh->s_full[i]), 1);
+      mv::mbar_init(bar(&sh->s_full[i]), 2);  // the products, and the issuer's word
       for (int k = 0; k < 2; ++k) mv::mbar_init(bar(&sh->p_full[i][k]), SOFTMAX_WARPS);
       mv::mbar_init(bar(&sh->o_done[i]), 1);
     }
