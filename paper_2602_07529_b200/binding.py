@@ -498,11 +498,13 @@ class RopeForm:
 
 def _heads_at(t, name: str, n_tokens: int, heads: int, d: int, dtype, index: int):
     """Pointer and token stride of a tensor [tokens][heads][head_dim] whose heads are contiguous; the tokens may be further apart."""
-    if (t is None or t.dim() != 3 or t.dtype is not dtype or t.get_device() != index or t.shape[0] < n_tokens or t.shape[1] != heads or t.shape[2] != d
-            or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d)):
-        raise ValueError(f"{name}: a tensor [{n_tokens}][{heads}][{d}] of {dtype} on cuda:{index} with contiguous heads is needed, got "
-                         + ("None" if t is None else f"{tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}"))
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * d)
+    if t is not None and t.dtype is dtype and t.get_device() == index and t.dim() == 3:
+        n, h, e = t.shape
+        to_token, to_head, to_element = t.stride()
+        if n >= n_tokens and h == heads and e == d and to_element == 1 and (to_head == d or heads == 1):
+            return t.data_ptr(), to_token if n > 1 else max(to_token, heads * d)
+    raise ValueError(f"{name}: a tensor [{n_tokens}][{heads}][{d}] of {dtype} on cuda:{index} with contiguous heads is needed, got "
+                     + ("None" if t is None else f"{tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}"))
 
 
 def mv_rope_rotate(form: RopeForm, geom: _Geom, positions, q, k, q_out, k_out, backward: bool = False, stream=None):
@@ -518,19 +520,21 @@ def mv_rope_rotate(form: RopeForm, geom: _Geom, positions, q, k, q_out, k_out, b
     if isinstance(positions, Plan):
         ptr = C.c_void_p()
         _check(lib.mv_plan_positions(positions.handle, C.byref(ptr)), "mv_plan_positions")
-        if positions.stats()["n_new_tokens"] != n:
-            raise ValueError(f"the plan has {positions.stats()['n_new_tokens']} new tokens, the tensors {n}")
+        st = _Stats()
+        _check(lib.mv_plan_get_stats(positions.handle, C.byref(st)), "mv_plan_get_stats")
+        if st.n_new_tokens != n:
+            raise ValueError(f"the plan has {st.n_new_tokens} new tokens, the tensors {n}")
         pos = ptr.value
     else:
         keep = positions._keep[0] if isinstance(positions, StepTables) else positions
         pos = _arr(keep, "positions", T.int32, n, i)
     dt = T.bfloat16 if geom.dtype == MV_BF16 else T.float32
-    a = [(None, 0)] * 4
+    d, in_q, in_k, out_q, out_k = geom.head_dim, (None, 0), (None, 0), (None, 0), (None, 0)
     if q is not None:
-        a[0], a[2] = (_heads_at(t, m, n, geom.n_q_heads, geom.head_dim, dt, i) for t, m in ((q, "q"), (q_out, "q_out")))
+        in_q, out_q = _heads_at(q, "q", n, geom.n_q_heads, d, dt, i), _heads_at(q_out, "q_out", n, geom.n_q_heads, d, dt, i)
     if k is not None:
-        a[1], a[3] = (_heads_at(t, m, n, geom.n_kv_heads, geom.head_dim, dt, i) for t, m in ((k, "k"), (k_out, "k_out")))
-    _check(lib.mv_rope_rotate(form._ref, C.byref(geom), pos, n, 1 if backward else 0, *a[0], *a[1], *a[2], *a[3], s), "mv_rope_rotate")
+        in_k, out_k = _heads_at(k, "k", n, geom.n_kv_heads, d, dt, i), _heads_at(k_out, "k_out", n, geom.n_kv_heads, d, dt, i)
+    _check(lib.mv_rope_rotate(form._ref, C.byref(geom), pos, n, 1 if backward else 0, *in_q, *in_k, *out_q, *out_k, s), "mv_rope_rotate")
 
 
 def mv_rope_write_kv_form(plan: Plan, geom: _Geom, form: RopeForm, q, k, v, q_rot, k_rot, k_pages, v_pages, stream=None):

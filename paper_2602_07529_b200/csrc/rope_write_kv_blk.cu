@@ -15,7 +15,8 @@
 //
 // Bound by memory for a prompt: 17K tokens, 32 query and 8 KV heads of 128, 420 MB in 77 us (5.5 TB/s, 83 % of the measured copy
 // rate).  Measured there: 4, 8, 16 rows per CTA 82.6, 78.0, 82.7 us; with 8 rows, registers for 3, 4, 5 CTAs per SM 78.0, 76.1, 93.2;
-// two pairs of q per thread at a time instead of four 77.9.  Bound by the launch for a decode step: 9.5 us a call from a host program,
+// two pairs of q per thread at a time instead of four 77.9.  With a form (2048 new tokens of eight requests, 380 MB) 74.4 us, 78 %; there
+// two pairs at a time, since four spill registers (85.4; one 78.6).  Bound by the launch for a decode step: 9.5 us a call from a host program,
 // 4 to 5 us in a graph.
 #include <algorithm>
 #include <type_traits>
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(NT, 4) rope_write_kv_blk_kernel(const Args a, 
   }
   // q: 16-byte pieces of both halves, UNITS of them per thread at a time so that their loads are in flight together
   if (a.q) {
-    constexpr int UNITS = TPC == 1 ? 1 : 4;
+    constexpr int UNITS = TPC == 1 ? 1 : FORM ? 2 : 4;
     const int here = min(TPC, a.max_rows - t0), units = here * a.Hq * CH;
     auto q_piece = [&](int x) {
       const int c = (x % CH) * 8;

@@ -314,9 +314,11 @@ class DecodeStateFP8Blk(DecodeState):
 
 
 class PrefillState:
-    def __init__(self, wl: synth.Workload, device="cuda", with_pool: bool = True):
+    """A prompt's rotation, cache write and attention, and its backward pass.  ``form``: a rotary form in place of the geometry's own."""
+
+    def __init__(self, wl: synth.Workload, device="cuda", with_pool: bool = True, form=None):
         assert wl.kind == "prefill"
-        self.wl, self.device, self.with_pool = wl, device, with_pool
+        self.wl, self.device, self.with_pool, self.form = wl, device, with_pool, form
         g, b = wl.geom, wl.batch
         self.geom = B.geom_of(wl)
         dt = torch_dtype(g)
@@ -331,13 +333,17 @@ class PrefillState:
         self.out = torch.empty_like(self.q)
 
     def step(self, stream=None, lse=None):
-        B.mv_rope_write_kv(self.plan, self.geom, self.q, self.k, self.v, self.q_rot, self.k_rot,
-                           self.k_pages if self.with_pool else None, self.v_pages if self.with_pool else None, stream)
+        args = (self.q, self.k, self.v, self.q_rot, self.k_rot, self.k_pages if self.with_pool else None, self.v_pages if self.with_pool else None, stream)
+        if self.form is None:
+            B.mv_rope_write_kv(self.plan, self.geom, *args)
+        else:
+            B.mv_rope_write_kv_form(self.plan, self.geom, self.form, *args)
         B.mv_dag_prefill_attn(self.plan, self.geom, self.q_rot, self.k_rot, self.v, self.out, lse, stream)
         return self.out
 
-    def forward_backward(self, dout, stream=None):
-        """Forward with the rows' log-sum-exp kept, then mv_dag_prefill_attn_bwd.  Returns (out, dq_rot, dk_rot, dv)."""
+    def forward_backward(self, dout, stream=None, raw: bool = False):
+        """Forward with the rows' log-sum-exp kept, then mv_dag_prefill_attn_bwd.  Returns (out, dq_rot, dk_rot, dv), or with ``raw`` the
+        gradients of q and k themselves: those of the rotated ones turned back."""
         if not hasattr(self, "lse"):
             self.lse = _dev_bytes(self.plan.workspace_bytes(self.geom, B.OP_PREFILL_ATTN), self.device)
             self.bwd_ws = _dev_bytes(self.plan.workspace_bytes(self.geom, B.OP_PREFILL_ATTN_BWD), self.device)
@@ -345,4 +351,9 @@ class PrefillState:
         self.step(stream, self.lse)
         B.mv_dag_prefill_attn_bwd(self.plan, self.geom, self.q_rot, self.k_rot, self.v, self.out, dout, self.lse, self.dq, self.dk,
                                   self.dv, self.bwd_ws, stream)
+        if raw:
+            form = self.form
+            if form is None:
+                form = B.RopeForm(B.ROPE_HALVES, self.wl.geom.head_dim, base=self.wl.geom.rope_base)
+            B.mv_rope_rotate(form, self.geom, self.plan, self.dq, self.dk, self.dq, self.dk, backward=True, stream=stream)
         return self.out, self.dq, self.dk, self.dv
