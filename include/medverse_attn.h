@@ -466,10 +466,11 @@ mv_status mv_chunk_tables_read_status(const mv_chunk_tables* tables, void* cuda_
  *   workspace   device, 256-byte aligned, mv_chunk_attn_workspace_bytes(geom) bytes (it does not depend on the step); scratch, not to be
  *               shared by calls that may overlap on the device
  * A scale counts as the power of two that its exponent gives, at least 2^-80, and has to be at most 2^40; NaN in either scale of a block
- * gives NaN to the rows that see the block and leaves the others untouched.
+ * gives NaN to the rows that see the block and leaves the others untouched.  (The format's two NaN bytes, which the cache write never
+ * stores, count as +-480.)
  * Arithmetic: keys and values are bf16 exactly; scores, sums and softmax statistics in 32 bits; weights rounded to bf16.  The same
  * inputs give the same bits on every call.
- * dtype MV_BF16, head_dim 64 or 128, group size at most 128, sm_scale not negative; all tensors 16-byte aligned.  Errors: MV_ERR_INVALID_ARG,
+ * dtype MV_BF16, head_dim 64 or 128, group size at most 128, sm_scale not negative (and finite times log2 e); all tensors 16-byte aligned.  Errors: MV_ERR_INVALID_ARG,
  * MV_ERR_UNSUPPORTED (also a pool of 2^31 or more (page, KV head, token) rows, max_tiles * n_kv_heads past 2^31), MV_ERR_WORKSPACE, MV_ERR_CUDA.
  * In counts[4]: MV_ERR_INVALID_ARG (records, lists of more than 2^26 pages, pages outside the pool, which are skipped); a wait inside
  * the kernel that runs out (seconds) ends the call with MV_ERR_TIMEOUT there, `out` is then undefined. */

@@ -78,7 +78,8 @@ mv_status mv_sched_commit(mv_sched* sched, const uint8_t* finished);
  * filled the clone gets a page of its own, and the pair (src, dst) is listed: copy those pages (mv_pages_copy, every pool) before
  * the next step writes.  src, dst: [capacity], *n pairs (at most one per running transition).
  * Not allowed between mv_sched_step and its mv_sched_commit.
- * Errors: MV_ERR_INVALID_ARG (also a request that is done), MV_ERR_PAGE_CAPACITY, MV_ERR_WORKSPACE (capacity; *n says what is needed).
+ * Errors: MV_ERR_INVALID_ARG (also a request that is done), MV_ERR_PAGE_CAPACITY, MV_ERR_WORKSPACE (capacity; *n says what is needed.
+ * Or no host memory; *n is then as it was).
  * On an error nothing changes. */
 mv_status mv_sched_clone_request(mv_sched* sched, int32_t request_id, int32_t* new_request_id, int32_t capacity, int32_t* src, int32_t* dst,
                                  int32_t* n);
@@ -86,7 +87,8 @@ mv_status mv_sched_clone_request(mv_sched* sched, int32_t request_id, int32_t* n
 /* Moves pages in use to lower free ones, the highest first, until every page in use lies below every free one or max_moves pages
  * have moved.  The scheduler's own lists change at once; copy page src[i] to dst[i] (i < *n <= max_moves) in every pool before the
  * next step (no page is in both lists).  *top (may be null): one more than the highest page then in use, so what lies
- * from there on may be given back.  Not allowed between mv_sched_step and its mv_sched_commit.  Errors: MV_ERR_INVALID_ARG. */
+ * from there on may be given back.  Not allowed between mv_sched_step and its mv_sched_commit.  Errors: MV_ERR_INVALID_ARG,
+ * MV_ERR_WORKSPACE (no host memory). */
 mv_status mv_sched_compact(mv_sched* sched, int32_t max_moves, int32_t* src, int32_t* dst, int32_t* n, int32_t* top);
 
 /* Reference counts of the given pages (0 = free).  Errors: MV_ERR_INVALID_ARG (a page id out of range). */

@@ -16,12 +16,23 @@
 // A page whose scale is NaN: its keys become NaN, so the scores of whoever sees it; its values stay finite, so whoever does not
 // see it multiplies them by zero.
 //
-// Warps (512 threads): 0 and 2 TMA for K and V, 1 issues the products, 3 the walk over the work and TMA for q; 4-7 bytes to bf16; 8-11 and 12-15
-// softmax of the two halves, a thread per q-vector (weights written over the scores as packed bf16, O in tensor memory rescaled only when the
-// row's reference moved by more than 2^8).  A tile that is seen whole and moves nothing has a way of its own, without a branch.
+// Warps (512 threads): 0 TMA for K and V, 1 issues the products, 2 takes and frees the tensor memory, 3 the walk over the work and TMA for
+// q; 4-7 bytes to bf16; 8-11 and 12-15 softmax of the two halves, a thread per q-vector (weights written over the scores as packed bf16, O in
+// tensor memory rescaled only when the row's reference moved by more than 2^8).  A tile that is seen whole and moves nothing has a way of its
+// own, without a branch.
 // One CTA per SM walks its share of the work: (query tile, KV head) after (query tile, KV head) lie on a line of cost, a constant
 // and then one unit per key tile, which the shares cut evenly.  What a cut leaves in two or more shares is joined by a second kernel.
 // Every wait is bounded.
+//
+// Bound by the tensor cores for a long list: 2048 new tokens behind 64K, 32 query and 8 KV heads of 128, 2.2 * 10^12 operations, take
+// 1.99 to 2.37 ms from one GPU to the next, 67 to 56 % of the rate measured of a library product; a prompt with its DAG, 17 thousand
+// tokens, 64 and 8 heads, 3.27 to 3.58 ms, 58 to 53 %.  A key tile takes 3800 cycles, 2048 of them products of the two halves; the rest is the chain scores ->
+// weights -> products of a half that the other half does not cover, and shared memory (320 KB to and fro a tile, 2500 cycles at 128 bytes a
+// cycle).  A (tile, head) item costs 14500 cycles besides (first tile, epilogue 5000).  Small steps are bound by the launches: 11.6 us.
+// Built and measured slower: weights from threads in pairs, or through the 16-lane shapes of tensor memory (row maxima then cross
+// threads); a part of the exponentials by a polynomial (2 % slower: the multiply-add pipe feeds the conversion of the bytes as well); eight
+// warps for the bytes instead of four (registers); two issuing warps; halves kept in turns by a token.  What decided most is the size of the
+// code that all roles run at once: see Cta::wait.
 #include <algorithm>
 #include <cmath>
 
@@ -37,6 +48,9 @@ constexpr int BQ = 128, BK = 128;       // q-vectors of a half; keys of a tile
 constexpr int SHARES = 148;             // CTAs
 constexpr int SETUP = 2;                // cost of a (query tile, head) besides its key tiles
 constexpr int NT = 512;
+// Registers of the warpgroups: launched with 128 per thread, 56 + 72 + 2 * 192 = 4 * 128
+constexpr int REGS_TMA = 56, REGS_BYTES = 72, REGS_SOFTMAX = 192;
+static_assert(REGS_TMA + REGS_BYTES + 2 * REGS_SOFTMAX <= 4 * (65536 / NT), "registers of an SM");
 constexpr int RAW = 4;                  // pieces of bytes in flight: half a tile of K, the other half, then of V
 constexpr int RING = 4;                 // bf16 tiles (K0 V0 K1 V1 ...)
 constexpr int METAS = 4;                // descriptions of key tiles: K of tile t waits for K of t - 1 converted, so for the scores of t - 3, so for the weights of t - 4
@@ -414,7 +428,7 @@ __device__ __forceinline__ void convert_half(const unsigned char* raw, unsigned 
   uint4 in[2][PIECES];
   uint32_t both[2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {  // all loads before the first store (the compiler cannot tell the areas apart): 2760 -> 1930 cycles a tile
+  for (int i = 0; i < 2; ++i) {  // all loads before the first store (the compiler cannot tell the areas apart)
     const int row = row_of(i);
     both[i] = factor[(row0 + row) >> 4];
 #pragma unroll
@@ -840,17 +854,16 @@ __global__ void __launch_bounds__(NT, 1) chunk_attn_kernel(const __grid_constant
   mv::grid_dependency_wait();
   mv::grid_dependency_launch_dependents();
   const Cta c{&a, smem, base, sh};
-  // launched with 128 registers per thread: 56 + 72 + 2 * 192 = 4 * 128
   if (warp < 4) {
-    mv::um::reg_dec<56>();
+    mv::um::reg_dec<REGS_TMA>();
     if (warp == 0) byte_loader<D>(c, &tm_k, &tm_v);
     else if (warp == 1) issuer<D>(c);
     else if (warp == 3) q_loader<D>(c, &tm_q);
   } else if (warp < 8) {
-    mv::um::reg_dec<72>();
+    mv::um::reg_dec<REGS_BYTES>();
     converters<D>(c);
   } else {
-    mv::um::reg_inc<192>();
+    mv::um::reg_inc<REGS_SOFTMAX>();
     softmax_warp<D>(c, (warp - 8) >> 2);
   }
   mv::um::fence_before();
@@ -947,10 +960,24 @@ mv_status launch_after(K kernel, dim3 grid, int threads, int smem, cudaStream_t 
   return e == cudaSuccess ? MV_OK : MV_ERR_CUDA;
 }
 
+// The warpgroups' shares of the registers are taken from what the block is launched with: with fewer than the shares add up to, the
+// request for more would never be met.
+template <typename K>
+bool registers_suffice(K kernel) {
+  cudaFuncAttributes f{};
+  if (cudaFuncGetAttributes(&f, kernel) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return false;
+  }
+  return f.numRegs >= (REGS_TMA + REGS_BYTES + 2 * REGS_SOFTMAX) / 4;
+}
+
 template <int D>
 mv_status launch(const Args& a, const void* q, const void* k8, const void* v8, cudaStream_t st) {
   static std::atomic<uint64_t> opted{0};  // per device
   if (!mv::opt_in_smem(chunk_attn_kernel<D>, Lay<D>::SMEM, opted)) return MV_ERR_CUDA;
+  static const bool fits = registers_suffice(chunk_attn_kernel<D>);  // (a property of the build)
+  if (!fits) return MV_ERR_UNSUPPORTED;
   // a pool's row is a token of a KV head (no pages: no entry is accepted, nothing is read)
   const int64_t rows = std::max<int64_t>(1, a.num_pages * a.Hkv * PS);
   CUtensorMap tm_q, tm_k, tm_v;
@@ -990,6 +1017,9 @@ extern "C" mv_status mv_dag_chunk_attn_fp8_blk(const mv_chunk_tables* t, const m
     if ((reinterpret_cast<uintptr_t>(p) & 15) != 0) return MV_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(t->counts) & 3) return MV_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < workspace_need(g->head_dim) || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MV_ERR_WORKSPACE;
+  const uintptr_t at_q = reinterpret_cast<uintptr_t>(q_rot), at_out = reinterpret_cast<uintptr_t>(out);
+  const uintptr_t bytes = uintptr_t(t->max_rows) * uintptr_t(g->n_q_heads) * uintptr_t(g->head_dim) * sizeof(bf16);
+  if (at_q < at_out + bytes && at_out < at_q + bytes) return MV_ERR_INVALID_ARG;  // rows are read after others have been written
   Args a;
   a.tiles = reinterpret_cast<const int4*>(t->tiles);
   a.entries = reinterpret_cast<const int2*>(t->entries);
@@ -1009,6 +1039,7 @@ extern "C" mv_status mv_dag_chunk_attn_fp8_blk(const mv_chunk_tables* t, const m
   a.R = BQ / G;
   a.out_32 = (reinterpret_cast<uintptr_t>(out) & 31) == 0;
   a.scale_log2 = mv::softmax_scale(g) * 1.4426950408889634f;
+  if (!std::isfinite(a.scale_log2)) return MV_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   return g->head_dim == 128 ? launch<128>(a, q_rot, k_pages8, v_pages8, s) : launch<64>(a, q_rot, k_pages8, v_pages8, s);
 }

@@ -286,14 +286,20 @@ extern "C" mv_status mv_sched_clone_request(mv_sched* s, int32_t request_id, int
                                             int32_t* dst, int32_t* n) {
   if (!s || !new_request_id || !n || capacity < 0 || (capacity > 0 && (!src || !dst)) || s->pending) return MV_ERR_INVALID_ARG;
   if (request_id < 0 || size_t(request_id) >= s->requests.size() || s->requests[size_t(request_id)].done) return MV_ERR_INVALID_ARG;
-  Request rq = s->requests[size_t(request_id)];
+  const Request& of = s->requests[size_t(request_id)];
   int32_t need = 0;
-  for (int32_t t : rq.running) need += (rq.written[size_t(t)] % s->page_size) != 0;
+  for (int32_t t : of.running) need += (of.written[size_t(t)] % s->page_size) != 0;
   if (need > capacity) {
     *n = need;
     return MV_ERR_WORKSPACE;
   }
   if (size_t(need) > s->free_pages.size()) return MV_ERR_PAGE_CAPACITY;
+  try {  // all that needs memory, before anything changes
+    s->requests.push_back(Request(of));
+  } catch (const std::bad_alloc&) {
+    return MV_ERR_WORKSPACE;
+  }
+  Request& rq = s->requests.back();
   int32_t k = 0;
   for (int v = 0; v < rq.n; ++v) {
     std::vector<int32_t>& pages = rq.pages[size_t(v)];
@@ -310,7 +316,6 @@ extern "C" mv_status mv_sched_clone_request(mv_sched* s, int32_t request_id, int
     }
   }
   for (int32_t t : rq.running) s->hold_view(rq, t, +1);
-  s->requests.push_back(std::move(rq));
   s->stats.requests_live++;
   *new_request_id = int32_t(s->requests.size()) - 1;
   *n = k;
@@ -319,7 +324,13 @@ extern "C" mv_status mv_sched_clone_request(mv_sched* s, int32_t request_id, int
 
 extern "C" mv_status mv_sched_compact(mv_sched* s, int32_t max_moves, int32_t* src, int32_t* dst, int32_t* n, int32_t* top) {
   if (!s || max_moves < 0 || (max_moves > 0 && (!src || !dst)) || !n || s->pending) return MV_ERR_INVALID_ARG;
-  std::vector<int32_t> to(size_t(s->num_pages), -1);  // where a page goes
+  std::vector<int32_t> to, left;  // where a page goes; the free pages afterwards
+  try {
+    to.assign(size_t(s->num_pages), -1);
+    left.reserve(size_t(s->num_pages));
+  } catch (const std::bad_alloc&) {
+    return MV_ERR_WORKSPACE;
+  }
   int32_t lo = 0, hi = s->num_pages - 1, k = 0;
   for (;;) {
     while (lo < s->num_pages && s->refs[size_t(lo)] != 0) ++lo;
@@ -336,9 +347,9 @@ extern "C" mv_status mv_sched_compact(mv_sched* s, int32_t max_moves, int32_t* s
       for (auto& pages : rq.pages)
         for (int32_t& p : pages)
           if (to[size_t(p)] >= 0) p = to[size_t(p)];
-    s->free_pages = {};
     for (int32_t p = 0; p < s->num_pages; ++p)
-      if (s->refs[size_t(p)] == 0) s->free_pages.push(p);
+      if (s->refs[size_t(p)] == 0) left.push_back(p);
+    s->free_pages = decltype(s->free_pages)(std::greater<int32_t>(), std::move(left));
   }
   *n = k;
   if (top) *top = hi + 1;

@@ -33,8 +33,11 @@ def pool_tokens(pool, slot):
 def copy_pages(pools, src, dst, stream=None):
     """Copies pages in every pool, from lists on the host (what ``Scheduler.clone_request`` and ``Scheduler.compact`` return)."""
     dev = pools[0].device
-    up = lambda x: torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(dev)
-    B.mv_pages_copy(B.PagePools(pools), up(src), up(dst), stream=stream)
+    lists = [torch.from_numpy(np.asarray(x, dtype=np.int32).copy()).to(dev) for x in (src, dst)]
+    B.mv_pages_copy(B.PagePools(pools), *lists, stream=stream)
+    if stream is not None:  # the lists' memory may be handed out again only when that stream is through
+        for x in lists:
+            x.record_stream(torch.cuda.ExternalStream(stream, dev) if isinstance(stream, int) else stream)
 
 
 def _dev_bytes(n: int, device):

@@ -75,3 +75,15 @@ def test_attention_refuses():
                  B.make_geom(129, 1, 128, 100, "bf16"), B.make_geom(32, 8, 128, 1 << 24, "bf16"), B.make_geom(32, 8, 128, 100, "bf16", page_size=32)):
         assert attend(tables(rows_per_tile=1), geom) == UNSUPPORTED
     assert attend(tables(max_tiles=1 << 30), g) == UNSUPPORTED
+
+
+def test_attention_refuses_outputs_that_overlap_its_input():
+    """q_rot and out have max_rows rows of 32 heads of 128: one may end where the other begins, no closer."""
+    g, t = B.make_geom(32, 8, 128, 100, "bf16"), tables(max_rows=16)
+    size, at = 16 * 32 * 128 * 2, 1 << 30
+    for shift in (16, size - 16, -16, 16 - size):
+        assert attend(t, g, (at, P, P, P, at + shift)) == INVALID, shift
+
+
+def test_attention_refuses_a_scale_that_is_infinite_in_binary_logarithms():
+    assert attend(tables(), B.make_geom(32, 8, 128, 100, "bf16", sm_scale=3.3e38), (1 << 30, P, P, P, 1 << 40)) == INVALID

@@ -437,6 +437,18 @@ def test_captured_step_grows():
         case.check(rows=range(0, len(case.seen), 5))
 
 
+def test_tensors_aligned_to_16_bytes_only():
+    """q_rot and out at addresses that are multiples of 16 bytes and not of 32."""
+    case = Case([[([], 40, 0), ([0], 3, 90)]], (8, 2, 128), 19, max_rows=95)
+    ref = case.run().clone()
+    room = [torch.full((case.q.numel() + 8,), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    shifted = [x[8:].view(case.q.shape) for x in room]
+    assert all(x.data_ptr() % 32 == 16 for x in shifted)
+    shifted[0].copy_(case.q)
+    case.q, case.out = shifted
+    assert torch.equal(case.run(), ref) and (room[1][:8] == 7).all()
+
+
 def test_two_streams_with_workspaces_of_their_own():
     cases = [Case(random_reqs(30 + i), (32, 8, 128), 30 + i) for i in range(2)]
     refs = [c.run().clone() for c in cases]

@@ -101,6 +101,23 @@ def test_captured_and_on_another_stream():
     assert all(torch.equal(p[20], p[11]) for p in pools)
 
 
+def test_lists_from_the_host_outlive_the_call():
+    """copy_pages on a stream that is still busy: the lists' memory is not handed out again before that stream has read it."""
+    from paper_2602_07529_b200 import runtime
+    pools = pools_of(64, [4096, 64], 4)
+    want = [p.clone() for p in pools]
+    for w in want:
+        w[40:48] = w[8:16]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)      # some tens of milliseconds
+    runtime.copy_pages(pools, range(8, 16), range(40, 48), stream=side)
+    later = [torch.full((8,), 63, dtype=torch.int32, device="cuda") for _ in range(8)]
+    torch.cuda.synchronize()
+    assert len(later) == 8 and all(torch.equal(p, w) for p, w in zip(pools, want))
+
+
 def test_binding_refuses():
     from paper_2602_07529_b200 import binding as B
     pools = pools_of(8, [64, 16], 1)
