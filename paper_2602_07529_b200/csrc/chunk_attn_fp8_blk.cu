@@ -18,15 +18,15 @@
 //
 // Warps (512 threads): 0 TMA for K and V, 1 issues the products, 2 takes and frees the tensor memory, 3 the walk over the work and TMA for
 // q; 4-7 bytes to bf16; 8-11 and 12-15 softmax of the two halves, a thread per q-vector (weights written over the scores as packed bf16, O in
-// tensor memory rescaled only when the row's reference moved by more than 2^8).  A tile that is seen whole and moves nothing has a way of its
-// own, without a branch.
+// tensor memory rescaled only when the row's reference moved by more than 2^8).  A tile that moves no reference has a way of its own, with the
+// scores in registers.
 // One CTA per SM walks its share of the work: (query tile, KV head) after (query tile, KV head) lie on a line of cost, a constant
 // and then one unit per key tile, which the shares cut evenly.  What a cut leaves in two or more shares is joined by a second kernel.
 // Every wait is bounded.
 //
 // Bound by the tensor cores for a long list: 2048 new tokens behind 64K, 32 query and 8 KV heads of 128, 2.2 * 10^12 operations, take
-// 1.99 to 2.37 ms from one GPU to the next, 67 to 56 % of the rate measured of a library product; a prompt with its DAG, 17 thousand
-// tokens, 64 and 8 heads, 3.27 to 3.58 ms, 58 to 53 %.  A key tile takes 3800 cycles, 2048 of them products of the two halves; the rest is the chain scores ->
+// 1.99 to 2.36 ms from one GPU to the next, 67 to 56 % of the rate measured of a library product; a prompt with its DAG, 17 thousand
+// tokens, 64 and 8 heads, 3.09 ms, 61 %.  A key tile takes 3800 cycles, 2048 of them products of the two halves; the rest is the chain scores ->
 // weights -> products of a half that the other half does not cover, and shared memory (320 KB to and fro a tile, 2500 cycles at 128 bytes a
 // cycle).  A (tile, head) item costs 14500 cycles besides (first tile, epilogue 5000).  Small steps are bound by the launches: 11.6 us.
 // Built and measured slower: weights from threads in pairs, or through the 16-lane shapes of tensor memory (row maxima then cross
@@ -615,6 +615,7 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
   Shared* const sh = c.sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int v = (warp & 3) * 32 + lane;                       // q-vector of the half
+  const int token = v / a.G;                                  // its token, inside the half
   const uint32_t lanes = sh->tmem + (uint32_t((warp & 3) * 32) << 16);
   const uint32_t s_t = lanes + i * 128, o_t = lanes + 256 + i * 128;
   int tile = 0, j = 0, done = 0;                              // key tiles of the share, of this half; its segments
@@ -629,7 +630,7 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
     }
     const int own = s->before * PS + s->key0 + first;            // slot of the half's first token in the node's list
     // reference (a score); a row that is no token's has one that nothing passes, so that its weights are zero
-    float r = v / a.G < rows ? -INFINITY : INFINITY;
+    float r = token < rows ? -INFINITY : INFINITY;
     uint64_t l[2] = {0, 0};                                      // sums: two chains of even and odd columns
     bool far = false;                                            // some row's reference is beyond FAR
     const uint64_t scale2 = mv::pack_f32x2(a.scale_log2, a.scale_log2);
@@ -657,12 +658,24 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
       if (!ok) break;
       mv::um::fence_after();
       const uint4 held = *reinterpret_cast<const uint4*>(sh->meta[tile % METAS].valid);
-      if (!far && own + 1 - t * BK >= BK && (held.x & held.y & held.z & held.w) == ~0u) {
-        // The way of nearly all tiles: every key is seen, no reference moves but a segment's first ones, none is far.  The scores stay in registers.
+      if (!far) {
+        // The way of nearly all tiles: no reference moves but a row's first one, none is far.  The scores stay in registers.
         uint32_t x[4][32];
 #pragma unroll
         for (int k = 0; k < 4; ++k) mv::um::ld32(s_t + 32 * k, x[k]);
         mv::um::wait_ld();
+        if (own + 1 - t * BK < BK || (held.x & held.y & held.z & held.w) != ~0u) {  // some key is not seen
+          const int seen = own + 1 - t * BK + token;  // slots of the tile that the row sees
+          const uint32_t words[4] = {held.x, held.y, held.z, held.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int n = seen - 32 * k;
+            const uint32_t see = n >= 32 ? words[k] : n <= 0 ? 0u : words[k] & ((1u << n) - 1);
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (!((see >> e) & 1)) x[k][e] = __float_as_uint(-INFINITY);
+          }
+        }
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -670,8 +683,8 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
           for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = mv::max3(mx[(e >> 1) & 3], __uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1]));
         // a reference moves only when a weight would otherwise pass 2^8
         const float most = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        const float ref = t == k0 && r != INFINITY ? most : r, n = -(ref * a.scale_log2);
-        const bool fine = ref == INFINITY ? r == INFINITY : ref != -INFINITY && !((most - ref) * a.scale_log2 > RESCALE_THRESHOLD) && fabsf(n) <= FAR;
+        const float ref = r == -INFINITY ? most : r, n = ref == -INFINITY ? 0.f : -(ref * a.scale_log2);  // (-inf: nothing seen so far)
+        const bool fine = ref == INFINITY ? r == INFINITY : !((most - ref) * a.scale_log2 > RESCALE_THRESHOLD) && fabsf(n) <= FAR;
         if (__all_sync(0xffffffffu, fine)) {
           r = ref;
           const uint64_t nref = mv::pack_f32x2(n, n);
@@ -684,9 +697,9 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
           continue;
         }
       }
-      // The other tiles: masked, first ones, such that move a reference.  The scores are read again, 32 columns at a time.
+      // The other tiles: such that move a reference, and those with one that is far.  The scores are read again, 32 columns at a time.
       const uint32_t* const valid = sh->meta[tile % METAS].valid;
-      const int seen = own + 1 - t * BK + v / a.G;  // slots of the tile that the row sees
+      const int seen = own + 1 - t * BK + token;
       auto read = [&](int k, uint32_t (&x)[32]) {
         // (on a ragged tile only the leading columns were computed, the rest holds something older and is masked)
         mv::um::ld32(s_t + 32 * k, x);
@@ -753,7 +766,7 @@ __device__ __forceinline__ void softmax_warp(const Cta& c, int i) {
     mv::unpack_f32x2(mv::add_f32x2(l[0], l[1]), sum, odd);
     sum += odd;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int slot = s->slot, token = v / a.G;  // token inside the half
+    const int slot = s->slot;
     const bool live = token < rows;
     bf16* pair_dst[2];  // of this thread's row and its neighbour's, the even one first
     bool pair_live[2];
