@@ -21,14 +21,17 @@
 // tensor memory rescaled only when the row's reference moved by more than 2^8).  A tile that moves no reference has a way of its own, with the
 // scores in registers.
 // One CTA per SM walks its share of the work: (query tile, KV head) after (query tile, KV head) lie on a line of cost, a constant
-// and then one unit per key tile, which the shares cut evenly.  What a cut leaves in two or more shares is joined by a second kernel.
+// and then one unit per key tile, which the shares cut evenly (few query tiles are dealt out differently: deal).  What a cut leaves in two or
+// more shares is joined by a second kernel.
 // Every wait is bounded.
 //
 // Bound by the tensor cores for a long list: 2048 new tokens behind 64K, 32 query and 8 KV heads of 128, 2.2 * 10^12 operations, take
 // 1.99 to 2.36 ms from one GPU to the next, 67 to 56 % of the rate measured of a library product; a prompt with its DAG, 17 thousand
-// tokens, 64 and 8 heads, 3.09 ms, 61 %.  A key tile takes 3800 cycles, 2048 of them products of the two halves; the rest is the chain scores ->
+// tokens, 64 and 8 heads, 3.08 ms, 62 %.  A key tile takes 3800 cycles, 2048 of them products of the two halves; the rest is the chain scores ->
 // weights -> products of a half that the other half does not cover, and shared memory (320 KB to and fro a tile, 2500 cycles at 128 bytes a
-// cycle).  A (tile, head) item costs 14500 cycles besides (first tile, epilogue 5000).  Small steps are bound by the launches: 11.6 us.
+// cycle).  A (tile, head) item costs 14500 cycles besides (first tile, epilogue 5000).  Small steps are bound by latency:
+// 9.7 us for 40 new tokens alone, of them 2 for a joining launch where one is needed; 40 behind 1000 19.3, behind 4000 26.1 (on the line of cost
+// 11.1, 19.7 and 36.7).
 // Built and measured slower: weights from threads in pairs, or through the 16-lane shapes of tensor memory (row maxima then cross
 // threads); a part of the exponentials by a polynomial (2 % slower: the multiply-add pipe feeds the conversion of the bytes as well); eight
 // warps for the bytes instead of four (registers); two issuing warps; halves kept in turns by a token.  What decided most is the size of the
@@ -47,6 +50,9 @@ constexpr int PS = 16, KEYS = 8;        // tokens of a page; pages of a key tile
 constexpr int BQ = 128, BK = 128;       // q-vectors of a half; keys of a tile
 constexpr int SHARES = 148;             // CTAs
 constexpr int SETUP = 2;                // cost of a (query tile, head) besides its key tiles
+constexpr int FEW = 32;                 // query tiles up to which a step may be dealt out in pieces (Walk::pieces)
+constexpr int WHOLE = 4, MANY = 16;     // key tiles of a list that stays whole there; of one whose pieces have two of them at least
+constexpr int FEW_OVER = 3;             // key tiles that the pieces may have more than the line's shares
 constexpr int NT = 512;
 // Registers of the warpgroups: launched with 128 per thread, 56 + 72 + 2 * 192 = 4 * 128
 constexpr int REGS_TMA = 56, REGS_BYTES = 72, REGS_SOFTMAX = 192;
@@ -99,6 +105,36 @@ struct Segment {
   bool ends;
 };
 
+// Few query tiles: every share is one piece of one (tile, head).  Lists of more than WHOLE key tiles are cut into equal pieces of at most
+// `len`, the least with which there are shares enough.  A list that stays whole costs nothing besides; a piece has to be written and
+// joined, which takes as long as two to three key tiles, and more where the pieces are many (hence MANY).  mine: key tiles of tile `lane`; even: a share of the line of cost.
+// Gives the share's tile (-1: none; -2: the line is better, where the lists are very unlike), the pieces of its list, and which one of
+// the heads' pieces it is.  (Not inlined: it runs once, and what lies between the roles moves them against the lines of the instruction
+// cache.  Inlined, long steps took 2 % longer.)  Against the line, 40 new tokens in all, 32 and 8 heads of 128: behind 0, 130, 216, 472, 960
+// tokens 9.7, 11.8, 14.2, 18.2, 19.3 for 11.1, 16.0, 16.7, 18.8, 19.7 us; 16 times 40 behind 216, 472, 960 18.2, 23.0, 29.7 for 24.3, 31.1, 38.6;
+// 8 and 2 heads of 64 behind 472 15.2 for 13.7.
+__device__ __noinline__ int3 deal(int mine, int hkv, int c, int64_t even) {
+  const int lane = threadIdx.x & 31;
+  const int64_t all = int64_t(__reduce_add_sync(0xffffffffu, unsigned(mine))) * hkv;
+  int len = max(1, int((all + SHARES - 1) / SHARES)), n;
+  for (;; len += (len + 7) / 8) {
+    const int at_most = mine > MANY ? max(2, len) : len;
+    n = mine <= WHOLE ? int(mine > 0) : (mine + at_most - 1) / at_most;
+    if (int64_t(__reduce_add_sync(0xffffffffu, unsigned(n))) * hkv <= SHARES) break;  // (at the latest with a piece for each)
+  }
+  if (len > max(int64_t(WHOLE), even + FEW_OVER)) return make_int3(-2, 0, 0);
+  int upto = n * hkv;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += y;
+  }
+  const unsigned m = __ballot_sync(0xffffffffu, upto > c);
+  if (m == 0) return make_int3(-1, 0, 0);
+  const int from = __ffs(m) - 1;
+  return make_int3(from, __shfl_sync(0xffffffffu, n, from), c - __shfl_sync(0xffffffffu, upto - n * hkv, from));
+}
+
 // The segments of a share, in order: one warp walks and hands them to the others through shared memory (their code and registers
 // would not bear it: 660 bytes of spills a thread where every warp walked by itself).
 struct Walk {
@@ -109,8 +145,8 @@ struct Walk {
   __device__ __forceinline__ int64_t point(const Args& a, int unit0, int tile) const { return (int64_t(unit0) + int64_t(SETUP) * tile) * a.Hkv; }
   // Tile t's record.  One that is not a tile's (rows or entries outside the arrays, key tiles that do not follow) counts as
   // having no key tiles: what lies behind this check stays inside the arrays whatever the tables hold.
-  __device__ __forceinline__ void take(const Args& a) {
-    const int4 p = __ldcg(a.tiles + 2 * t), q = __ldcg(a.tiles + 2 * t + 1);
+  __device__ __forceinline__ void take(const Args& a) { take(a, __ldcg(a.tiles + 2 * t), __ldcg(a.tiles + 2 * t + 1)); }
+  __device__ __forceinline__ void take(const Args& a, const int4& p, const int4& q) {
     s.row0 = p.x;
     s.rows = p.y;
     s.ent0 = p.z;
@@ -126,10 +162,32 @@ struct Walk {
   }
   __device__ __forceinline__ void begin(const Args& a, int c) {
     const int lane = threadIdx.x & 31;
+    int units_at = 0;
+    if (lane < min(FEW, a.max_tiles)) units_at = __ldcg(reinterpret_cast<const int32_t*>(a.tiles) + 8 * lane + 6);  // asked for with the counts
     share = c;
     n_tiles = max(0, min(__ldcg(a.counts + 1), a.max_tiles));
     const int total_units = max(0, __ldcg(a.counts + 3));
     const int64_t total = n_tiles > 0 ? point(a, total_units, n_tiles) : 0;
+    if (n_tiles <= FEW && n_tiles * a.Hkv <= SHARES) {
+      int mine = lane < n_tiles ? units_at : 0;
+      if (lane < n_tiles && (mine < 1 || mine > (a.max_entries + KEYS - 1) / KEYS)) {  // no sound record
+        atomicExch(a.counts + 4, int(MV_ERR_INVALID_ARG));
+        mine = 0;
+      }
+      const int3 part = deal(mine, a.Hkv, c, total / SHARES);
+      if (part.x >= -1) {
+        t = n_tiles;
+        if (part.x < 0) return;
+        t = part.x;
+        n_tiles = t + 1;  // and no other
+        take(a);
+        head = part.z / part.y;
+        const int i = part.z - part.y * head;
+        k = int(int64_t(units) * i / part.y);
+        x_end = base + int64_t(head) * (SETUP + units) + SETUP + int64_t(units) * (i + 1) / part.y;
+        return;
+      }
+    }
     const int64_t each = total / SHARES, more = total % SHARES;
     const int64_t x = each * c + min(int64_t(c), more);
     x_end = x + each + (c < more ? 1 : 0);
@@ -884,30 +942,47 @@ __global__ void __launch_bounds__(NT, 1) chunk_attn_kernel(const __grid_constant
   if (warp == 2) mv::um::tmem_dealloc(sh->tmem, 512);
 }
 
-// Joins the cut items: out = sum_i w_i O_i / sum_i w_i l_i, w_i = 2^(c (r_i - max r)) over the item's parts i.  CTA (c, y): the item that starts in
-// share c and ends in a later one, a slice of its q-vectors; a warp per q-vector, four parts in flight.
-constexpr int MERGE_WARPS = 8, SLICES = 8;
+// Joins the cut items: out = sum_i w_i O_i / sum_i w_i l_i, w_i = 2^(c (r_i - max r)) over the item's parts i.  The items that start in a
+// share and end in a later one are listed; their q-vectors are dealt to the warps of all CTAs, FLY parts of each in flight.
+constexpr int MERGE_WARPS = 16, MERGE_CTAS = 4 * SHARES;
 template <int D>
-__global__ void __launch_bounds__(MERGE_WARPS * 32) chunk_merge_kernel(const Args a) {
-  constexpr int VEC = D / 32, FLY = 4;
+__global__ void __launch_bounds__(MERGE_WARPS * 32, 3) chunk_merge_kernel(const Args a) {
+  constexpr int VEC = D / 32, FLY = 8 / VEC;
+  __shared__ int s_own[SHARES], s_more[SHARES + 1], s_row0[SHARES], s_rows[SHARES], s_list[SHARES], s_n[MERGE_WARPS];
+  // item that goes on behind a share; begun before it; the former's rows; shares that have one
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   mv::grid_dependency_wait();
-  const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int4* const cuts = reinterpret_cast<const int4*>(a.cuts);
-  const int4 own = __ldcg(cuts + 2 * c + 1);
-  if (own.x < 0) return;
-  // the parts: slot 2 c + 1, then slots 2 i of the shares behind, without gaps
-  int parts = 1;
-  for (int i0 = c + 1; i0 < SHARES; i0 += 32) {
-    const bool here = i0 + lane < SHARES && __ldcg(reinterpret_cast<const int*>(cuts + 2 * (i0 + lane))) == own.x;
-    const unsigned m = __ballot_sync(0xffffffffu, here);
-    const int run = m == ~0u ? 32 : __ffs(~m) - 1;
-    parts += run;
-    if (run < 32) break;
+  static_assert(SHARES <= MERGE_WARPS * 32, "a thread per share");
+  if (threadIdx.x < SHARES) {
+    const int4 own = __ldcg(cuts + 2 * threadIdx.x + 1);
+    s_own[threadIdx.x] = own.x;
+    s_row0[threadIdx.x] = own.y;
+    s_rows[threadIdx.x] = own.z;
+    s_more[threadIdx.x] = __ldcg(reinterpret_cast<const int*>(cuts + 2 * threadIdx.x));
   }
-  const int head = own.x % a.Hkv;
-  for (int q = blockIdx.y * MERGE_WARPS + warp; q < MAXQV; q += SLICES * MERGE_WARPS) {
+  if (threadIdx.x == 0) s_more[SHARES] = -1;
+  const bool here = threadIdx.x < SHARES && s_own[threadIdx.x] >= 0;  // (its own word)
+  const unsigned m = __ballot_sync(0xffffffffu, here);
+  if (lane == 0) s_n[warp] = __popc(m);
+  __syncthreads();
+  int n_items = 0, at = __popc(m & ((1u << lane) - 1));
+#pragma unroll
+  for (int w = 0; w < MERGE_WARPS; ++w) {
+    if (w < warp) at += s_n[w];
+    n_items += s_n[w];
+  }
+  if (n_items == 0) return;  // (all of the CTA)
+  if (here) s_list[at] = threadIdx.x;
+  __syncthreads();
+  for (int x = blockIdx.x * MERGE_WARPS + warp; x < n_items * MAXQV; x += MERGE_CTAS * MERGE_WARPS) {
+    const int c = s_list[x / MAXQV], q = x % MAXQV, item = s_own[c], head = item % a.Hkv;
+    const int2 rows = make_int2(s_row0[c], s_rows[c]);
     const int half = q / BQ, v = q % BQ, token = v / a.G;
-    if (token >= min(a.R, own.z - half * a.R)) continue;
+    if (token >= min(a.R, rows.y - half * a.R)) continue;
+    // the parts: slot 2 c + 1, then slots 2 i of the shares behind, without gaps
+    int parts = 1;
+    while (s_more[c + parts] == item) ++parts;
     float top = -INFINITY, sum = 0.f, acc[VEC] = {};
     for (int p0 = 0; p0 < parts; p0 += FLY) {
       float2 ml[FLY];
@@ -948,7 +1023,7 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) chunk_merge_kernel(const Arg
       top = now;
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int64_t row = int64_t(own.y) + half * a.R + token;
+    const int64_t row = int64_t(rows.x) + half * a.R + token;
     uint32_t* const out = reinterpret_cast<uint32_t*>(a.out + (row * a.Hq + head * a.G + (v - token * a.G)) * D + lane * VEC);
     if (VEC == 4) *reinterpret_cast<uint2*>(out) = make_uint2(mv::pack_bf16(acc[0] * inv, acc[1] * inv), mv::pack_bf16(acc[VEC - 2] * inv, acc[VEC - 1] * inv));
     else *out = mv::pack_bf16(acc[0] * inv, acc[1] * inv);
@@ -999,7 +1074,9 @@ mv_status launch(const Args& a, const void* q, const void* k8, const void* v8, c
     return MV_ERR_CUDA;
   const mv_status e = launch_after(chunk_attn_kernel<D>, dim3(SHARES), NT, Lay<D>::SMEM, st, a, tm_q, tm_k, tm_v);
   if (e != MV_OK) return e;
-  return launch_after(chunk_merge_kernel<D>, dim3(SHARES, SLICES), MERGE_WARPS * 32, 0, st, a);
+  // where no list can be long enough to be cut there is nothing to join
+  if (a.max_tiles <= FEW && a.max_tiles * a.Hkv <= SHARES && a.max_entries <= WHOLE * KEYS) return MV_OK;
+  return launch_after(chunk_merge_kernel<D>, dim3(MERGE_CTAS), MERGE_WARPS * 32, 0, st, a);
 }
 
 }  // namespace

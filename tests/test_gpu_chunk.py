@@ -520,3 +520,12 @@ def test_runtime_state_against_the_definition():
         case.b, case.seen, case.hq, case.hkv, case.d = wl.batch, seen, g.n_q_heads, g.n_kv_heads, g.head_dim
         case.geom, case.q, case.k8, case.v8, case.scale, case.out = st.geom, st.q_rot, st.k_pages, st.v_pages, st.kv_scale, out
         case.check(rows=range(0, len(seen), 11))
+
+
+@pytest.mark.parametrize("heads", [(32, 8, 128), (8, 2, 64), (5, 5, 128), (148, 148, 64)])
+@pytest.mark.parametrize("held", [(0,), (400, 3), (600, 20, 1), (9000,), (20, 5000, 700, 130, 1, 1)])
+def test_few_tiles_of_unlike_lengths(heads, held):
+    """Steps of few query tiles, whose lists stay whole, are cut into equal pieces, or lie on the line where they are too unlike."""
+    case = Case([[([], n, 0 if n else 3), ([0], 0, 1 + i)] for i, n in enumerate(held)], heads, 41, max_rows=40)
+    case.run()
+    case.check(rows=range(0, len(case.seen), 3))
