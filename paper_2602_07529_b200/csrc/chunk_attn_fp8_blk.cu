@@ -107,7 +107,8 @@ struct Segment {
 
 // Few query tiles: every share is one piece of one (tile, head).  Lists of more than WHOLE key tiles are cut into equal pieces of at most
 // `len`, the least with which there are shares enough.  A list that stays whole costs nothing besides; a piece has to be written and
-// joined, which takes as long as two to three key tiles, and more where the pieces are many (hence MANY).  mine: key tiles of tile `lane`; even: a share of the line of cost.
+// joined, which takes as long as two to three key tiles, and more where the pieces are many (hence MANY).
+// mine: key tiles of tile `lane`; even: a share of the line of cost.
 // Gives the share's tile (-1: none; -2: the line is better, where the lists are very unlike), the pieces of its list, and which one of
 // the heads' pieces it is.  (Not inlined: it runs once, and what lies between the roles moves them against the lines of the instruction
 // cache.  Inlined, long steps took 2 % longer.)  Against the line, 40 new tokens in all, 32 and 8 heads of 128: behind 0, 130, 216, 472, 960
@@ -170,7 +171,7 @@ struct Walk {
     const int64_t total = n_tiles > 0 ? point(a, total_units, n_tiles) : 0;
     if (n_tiles <= FEW && n_tiles * a.Hkv <= SHARES) {
       int mine = lane < n_tiles ? units_at : 0;
-      if (lane < n_tiles && (mine < 1 || mine > (a.max_entries + KEYS - 1) / KEYS)) {  // no sound record
+      if (lane < n_tiles && (mine < 1 || mine > min((a.max_entries - 1) / KEYS + 1, kMaxList / KEYS))) {  // no sound record
         atomicExch(a.counts + 4, int(MV_ERR_INVALID_ARG));
         mine = 0;
       }
