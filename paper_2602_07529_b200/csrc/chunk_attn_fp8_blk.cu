@@ -1052,21 +1052,25 @@ mv_status launch_after(K kernel, dim3 grid, int threads, int smem, cudaStream_t 
 // The warpgroups' shares of the registers are taken from what the block is launched with: with fewer than the shares add up to, the
 // request for more would never be met.
 template <typename K>
-bool registers_suffice(K kernel) {
-  cudaFuncAttributes f{};
-  if (cudaFuncGetAttributes(&f, kernel) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return false;
+mv_status registers_suffice(K kernel, std::atomic<int>& regs) {
+  if (regs == 0) {  // (a property of the build, asked for once)
+    cudaFuncAttributes f{};
+    if (cudaFuncGetAttributes(&f, kernel) != cudaSuccess) {
+      (void)cudaGetLastError();
+      return MV_ERR_CUDA;
+    }
+    regs = f.numRegs;
   }
-  return f.numRegs >= (REGS_TMA + REGS_BYTES + 2 * REGS_SOFTMAX) / 4;
+  return regs >= (REGS_TMA + REGS_BYTES + 2 * REGS_SOFTMAX) / 4 ? MV_OK : MV_ERR_UNSUPPORTED;
 }
 
 template <int D>
 mv_status launch(const Args& a, const void* q, const void* k8, const void* v8, cudaStream_t st) {
   static std::atomic<uint64_t> opted{0};  // per device
   if (!mv::opt_in_smem(chunk_attn_kernel<D>, Lay<D>::SMEM, opted)) return MV_ERR_CUDA;
-  static const bool fits = registers_suffice(chunk_attn_kernel<D>);  // (a property of the build)
-  if (!fits) return MV_ERR_UNSUPPORTED;
+  static std::atomic<int> regs{0};
+  const mv_status fits = registers_suffice(chunk_attn_kernel<D>, regs);
+  if (fits != MV_OK) return fits;
   // a pool's row is a token of a KV head (no pages: no entry is accepted, nothing is read)
   const int64_t rows = std::max<int64_t>(1, a.num_pages * a.Hkv * PS);
   CUtensorMap tm_q, tm_k, tm_v;

@@ -113,6 +113,7 @@ def test_lists_from_the_host_outlive_the_call():
     with torch.cuda.stream(side):
         torch.cuda._sleep(50_000_000)      # some tens of milliseconds
     runtime.copy_pages(pools, range(8, 16), range(40, 48), stream=side)
+    runtime.copy_pages(pools, [], [], stream=side)
     later = [torch.full((8,), 63, dtype=torch.int32, device="cuda") for _ in range(8)]
     torch.cuda.synchronize()
     assert len(later) == 8 and all(torch.equal(p, w) for p, w in zip(pools, want))
