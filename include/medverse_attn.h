@@ -243,8 +243,11 @@ typedef enum {
 } mv_rope_scaling;
 
 /* Fills a form (host only).  factor is read unless the scaling is MV_ROPE_PLAIN; length, slow and fast with MV_ROPE_RAMP only.
+ * The angles before any stretching are computed as the calls without a form compute theirs: whole heads in halves with amplitude 1 and
+ * rope_base for base give the bits of mv_rope_write_kv.  mv_rope_write_kv_fp8_blk fuses other products of k, so there k_rot, or a byte of K,
+ * may come out one rounding apart.
  * The struct may as well be filled, or changed, by the caller's own code.
- * Errors: MV_ERR_INVALID_ARG (enums, base < 1, factor < 1, length <= 0, slow < 0, fast <= slow, amplitude),
+ * Errors: MV_ERR_INVALID_ARG (enums, base < 1 or, stretched, beyond a double, factor < 1, length <= 0, slow < 0, fast <= slow, amplitude),
  * MV_ERR_UNSUPPORTED (first or rotary_dim not a multiple of 16, rotary_dim outside 16 .. 128, first < 0 or > 112). */
 mv_status mv_rope_form_init(mv_rope_form* form, int32_t layout, int32_t first, int32_t rotary_dim, double base, int32_t scaling,
                             double factor, double length, double slow, double fast, float amplitude);

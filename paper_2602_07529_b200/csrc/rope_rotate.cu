@@ -195,15 +195,19 @@ extern "C" mv_status mv_rope_form_init(mv_rope_form* form, int32_t layout, int32
   if (scaling != MV_ROPE_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor))) return MV_ERR_INVALID_ARG;
   if (scaling == MV_ROPE_RAMP && (!(length > 0.0) || !std::isfinite(length) || !(slow >= 0.0) || !(fast > slow) || !std::isfinite(fast))) return MV_ERR_INVALID_ARG;
   if (first < 0 || first > 112 || (first & 15) || rotary_dim < 16 || rotary_dim > 128 || (rotary_dim & 15)) return MV_ERR_UNSUPPORTED;
+  if (scaling == MV_ROPE_BASE) {
+    const double r = double(rotary_dim);
+    base *= std::pow(factor, r / (r - 2.0));
+    if (!std::isfinite(base)) return MV_ERR_INVALID_ARG;
+  }
   *form = mv_rope_form{};
   form->layout = layout;
   form->first = first;
   form->rotary_dim = rotary_dim;
   form->amplitude = amplitude;
-  const double r = double(rotary_dim);
-  if (scaling == MV_ROPE_BASE) base *= std::pow(factor, r / (r - 2.0));
+  const mv::ThetaTable plain = mv::theta_table(base, rotary_dim);  // the very angles of the calls without a form
   for (int i = 0; i < rotary_dim / 2; ++i) {
-    double t = std::pow(base, -2.0 * double(i) / r);
+    double t = plain.theta[i];
     if (scaling == MV_ROPE_LINEAR) t /= factor;
     if (scaling == MV_ROPE_RAMP) {
       const double turns = length * t / 6.283185307179586476925;

@@ -346,7 +346,10 @@ class PrefillState:
 
     def forward_backward(self, dout, stream=None, raw: bool = False):
         """Forward with the rows' log-sum-exp kept, then mv_dag_prefill_attn_bwd.  Returns (out, dq_rot, dk_rot, dv), or with ``raw`` the
-        gradients of q and k themselves: those of the rotated ones turned back."""
+        gradients of q and k themselves: those of the rotated ones turned back (a geometry's own rotation needs a rope_base of at least 1
+        for that)."""
+        if raw:  # a form of the geometry's own rotation has the forward call's angles; refused before anything is launched
+            turn = self.form if self.form is not None else B.RopeForm(B.ROPE_HALVES, self.wl.geom.head_dim, base=self.wl.geom.rope_base)
         if not hasattr(self, "lse"):
             self.lse = _dev_bytes(self.plan.workspace_bytes(self.geom, B.OP_PREFILL_ATTN), self.device)
             self.bwd_ws = _dev_bytes(self.plan.workspace_bytes(self.geom, B.OP_PREFILL_ATTN_BWD), self.device)
@@ -355,8 +358,5 @@ class PrefillState:
         B.mv_dag_prefill_attn_bwd(self.plan, self.geom, self.q_rot, self.k_rot, self.v, self.out, dout, self.lse, self.dq, self.dk,
                                   self.dv, self.bwd_ws, stream)
         if raw:
-            form = self.form
-            if form is None:
-                form = B.RopeForm(B.ROPE_HALVES, self.wl.geom.head_dim, base=self.wl.geom.rope_base)
-            B.mv_rope_rotate(form, self.geom, self.plan, self.dq, self.dk, self.dq, self.dk, backward=True, stream=stream)
+            B.mv_rope_rotate(turn, self.geom, self.plan, self.dq, self.dk, self.dq, self.dk, backward=True, stream=stream)
         return self.out, self.dq, self.dk, self.dv
