@@ -502,21 +502,24 @@ def _heads_at(t, name: str, n_tokens: int, heads: int, d: int, dtype, index: int
         n, h, e = t.shape
         to_token, to_head, to_element = t.stride()
         if n >= n_tokens and h == heads and e == d and to_element == 1 and (to_head == d or heads == 1):
-            return t.data_ptr(), to_token if n > 1 else max(to_token, heads * d)
+            return t.data_ptr(), to_token if n_tokens > 1 else heads * d  # (a single token has no next one)
     raise ValueError(f"{name}: a tensor [{n_tokens}][{heads}][{d}] of {dtype} on cuda:{index} with contiguous heads is needed, got "
                      + ("None" if t is None else f"{tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}"))
 
 
 def mv_rope_rotate(form: RopeForm, geom: _Geom, positions, q, k, q_out, k_out, backward: bool = False, stream=None):
     """Rotates q and k (either may be None) by ``positions``: an int32 CUDA tensor, StepTables, or an uploaded Plan whose tokens they are.
+    q and k have the same number of tokens, the outputs and the positions at least as many (what lies behind those is left alone).
     ``backward``: the transposed map, from the gradients of the rotated tensors to those of the raw ones."""
     T = _torch()
     some = q if q is not None else k
     if some is None:
         raise ValueError("q and k are both None")
+    n, keep = some.shape[0], None
+    if k is not None and k.shape[0] != n:
+        raise ValueError(f"q has {n} tokens, k {k.shape[0]}")
     i = some.get_device()
     s = _launch_stream(i, stream)
-    n, keep = some.shape[0], None
     if isinstance(positions, Plan):
         ptr = C.c_void_p()
         _check(lib.mv_plan_positions(positions.handle, C.byref(ptr)), "mv_plan_positions")
