@@ -258,7 +258,8 @@ mv_status mv_rope_form_init(mv_rope_form* form, int32_t layout, int32_t first, i
  *   pos_id   device int32 [n_tokens], positions -2^30 .. 2^30: mv_step_tables.pos_id, mv_plan_positions, or the caller's own
  *   q, k     device, token t's heads at q + t * q_stride elements ([n_q_heads][head_dim], contiguous), k likewise: q and k may lie side by side
  *            in the rows of one projection.  Either may be NULL with its output
- *   q_out, k_out  device, with strides of their own; may be q and k with the same strides.  Otherwise no output may overlap an input
+ *   q_out, k_out  device, with strides of their own; may be q and k with the same strides.  Otherwise no row of an output may overlap a row of
+ *            an input or of the other output (refused)
  * geom: n_q_heads, n_kv_heads, head_dim and dtype are read.  Strides are multiples of 16 bytes and at least a token's heads;
  * all tensors are 16-byte aligned.
  * Errors: MV_ERR_INVALID_ARG, MV_ERR_UNSUPPORTED, MV_ERR_CUDA. */

@@ -10,6 +10,7 @@
 // Measured: 17K tokens, 32 query and 8 KV heads of 128, 349 MB, 61.5 us (5.67 TB/s, 87 % of the measured copy rate); 4, 8, 16 tokens per CTA
 // 65.0, 61.0, 66.6 us, four pieces in flight instead of two 62.5, vectors that do not pass L2 by 63.5.  64 tokens: 3.1 us in a graph, the rest
 // of a call is the host's.
+#include <algorithm>
 #include <cmath>
 #include <limits>
 
@@ -185,6 +186,33 @@ bool sound(const void* in, int64_t in_stride, const void* out, int64_t out_strid
   return in_stride <= most && out_stride <= most && (in != out || in_stride == out_stride);
 }
 
+// n rows of `length` bytes, `stride` apart (a sound tensor's: n * stride fits an int64_t, length is at most stride)
+struct Rows {
+  const void* base;
+  int64_t stride, length;
+};
+// floor(a / b), b > 0
+int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0 ? 1 : 0); }
+// Do some row of a and some row of b share a byte?  Rows of one stride (tensors side by side in the rows of one projection) by arithmetic;
+// others, where the areas meet at all, row after row.
+bool overlap(const Rows& a, const Rows& b, int64_t n) {
+  if (!a.base || !b.base) return false;
+  const int64_t d = int64_t(reinterpret_cast<uintptr_t>(b.base) - reinterpret_cast<uintptr_t>(a.base));
+  const int64_t end_a = (n - 1) * a.stride + a.length, end_b = (n - 1) * b.stride + b.length;
+  if (d >= end_a || -d >= end_b) return false;
+  // rows i of a and j of b meet where -b.length < d + j * b.stride - i * a.stride < a.length
+  if (a.stride == b.stride) {  // so where j - i is in lo .. hi
+    const int64_t lo = floor_div(-b.length - d, a.stride) + 1, hi = -floor_div(d - a.length, a.stride) - 1;
+    return std::max(lo, 1 - n) <= std::min(hi, n - 1);
+  }
+  for (int64_t i = 0; i < n; ++i) {
+    const int64_t at = i * a.stride - d;  // row i, as b counts
+    const int64_t lo = floor_div(at - b.length, b.stride) + 1, hi = -floor_div(-at - a.length, b.stride) - 1;
+    if (std::max<int64_t>(lo, 0) <= std::min(hi, n - 1)) return true;
+  }
+  return false;
+}
+
 }  // namespace
 
 extern "C" mv_status mv_rope_form_init(mv_rope_form* form, int32_t layout, int32_t first, int32_t rotary_dim, double base, int32_t scaling,
@@ -232,7 +260,14 @@ extern "C" mv_status mv_rope_rotate(const mv_rope_form* form, const mv_attn_geom
   if (k && !sound(k, k_stride, k_out, k_out_stride, int64_t(g->n_kv_heads) * g->head_dim, size, n_tokens)) return MV_ERR_INVALID_ARG;
   if (n_tokens == 0 || (!q && !k)) return MV_OK;
   if (!pos_id || (reinterpret_cast<uintptr_t>(pos_id) & 3)) return MV_ERR_INVALID_ARG;
-  if (n_tokens > int64_t(INT32_MAX) || g->n_q_heads > 4096) return MV_ERR_UNSUPPORTED;
+  if (n_tokens > int64_t(INT32_MAX)) return MV_ERR_UNSUPPORTED;
+  const int64_t token_q = int64_t(g->n_q_heads) * g->head_dim * size, token_k = int64_t(g->n_kv_heads) * g->head_dim * size;
+  const Rows in_q{q, q_stride * size, token_q}, in_k{k, k_stride * size, token_k}, in_pos{pos_id, 4, 4};
+  const Rows to_q{q_out, q_out_stride * size, token_q}, to_k{k_out, k_out_stride * size, token_k};
+  if ((q != q_out && overlap(to_q, in_q, n_tokens)) || (k != k_out && overlap(to_k, in_k, n_tokens)) || overlap(to_q, in_k, n_tokens) ||
+      overlap(to_k, in_q, n_tokens) || overlap(to_q, to_k, n_tokens) || overlap(to_q, in_pos, n_tokens) || overlap(to_k, in_pos, n_tokens))
+    return MV_ERR_INVALID_ARG;
+  if (g->n_q_heads > 4096) return MV_ERR_UNSUPPORTED;
   Args a;
   a.q = q;
   a.k = k;
