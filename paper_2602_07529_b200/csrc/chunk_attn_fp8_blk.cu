@@ -30,8 +30,7 @@
 // tokens, 64 and 8 heads, 3.08 ms, 62 %.  A key tile takes 3800 cycles, 2048 of them products of the two halves; the rest is the chain scores ->
 // weights -> products of a half that the other half does not cover, and shared memory (320 KB to and fro a tile, 2500 cycles at 128 bytes a
 // cycle).  A (tile, head) item costs 14500 cycles besides (first tile, epilogue 5000).  Small steps are bound by latency:
-// 9.7 us for 40 new tokens alone, of them 2 for a joining launch where one is needed; 40 behind 1000 19.3, behind 4000 26.1 (on the line of cost
-// 11.1, 19.7 and 36.7).
+// 9.8 us for 40 new tokens alone (12 with a joining launch, where the tables have room for longer lists); 40 behind 960 18.4, behind 4000 25.8 (see deal).
 // Built and measured slower: weights from threads in pairs, or through the 16-lane shapes of tensor memory (row maxima then cross
 // threads); a part of the exponentials by a polynomial (2 % slower: the multiply-add pipe feeds the conversion of the bytes as well); eight
 // warps for the bytes instead of four (registers); two issuing warps; halves kept in turns by a token.  What decided most is the size of the
@@ -51,8 +50,8 @@ constexpr int BQ = 128, BK = 128;       // q-vectors of a half; keys of a tile
 constexpr int SHARES = 148;             // CTAs
 constexpr int SETUP = 2;                // cost of a (query tile, head) besides its key tiles
 constexpr int FEW = 32;                 // query tiles up to which a step may be dealt out in pieces (Walk::pieces)
-constexpr int WHOLE = 4, MANY = 16;     // key tiles of a list that stays whole there; of one whose pieces have two of them at least
-constexpr int FEW_OVER = 3;             // key tiles that the pieces may have more than the line's shares
+constexpr int WHOLE = 4, MANY = 16;     // key tiles of a list that stays whole where nothing is joined; of one whose pieces have two of them at least
+constexpr int FEW_OVER = 3, CUT_OVER = 1, CUT_SHORT = 6;  // key tiles: see deal
 constexpr int NT = 512;
 // Registers of the warpgroups: launched with 128 per thread, 56 + 72 + 2 * 192 = 4 * 128
 constexpr int REGS_TMA = 56, REGS_BYTES = 72, REGS_SOFTMAX = 192;
@@ -87,6 +86,7 @@ struct Args {
   int64_t num_pages;
   int max_rows, max_tiles, max_entries;
   int Hq, Hkv, G, R;
+  int join;             // a joining launch follows
   int out_32;           // out is aligned to 32 bytes
   float scale_log2;
 };
@@ -105,25 +105,33 @@ struct Segment {
   bool ends;
 };
 
-// Few query tiles: every share is one piece of one (tile, head).  Lists of more than WHOLE key tiles are cut into equal pieces of at most
-// `len`, the least with which there are shares enough.  A list that stays whole costs nothing besides; a piece has to be written and
-// joined, which takes as long as two to three key tiles, and more where the pieces are many (hence MANY).
-// mine: key tiles of tile `lane`; even: a share of the line of cost.
-// Gives the share's tile (-1: none; -2: the line is better, where the lists are very unlike), the pieces of its list, and which one of
-// the heads' pieces it is.  (Not inlined: it runs once, and what lies between the roles moves them against the lines of the instruction
-// cache.  Inlined, long steps took 2 % longer.)  Against the line, 40 new tokens in all, 32 and 8 heads of 128: behind 0, 130, 216, 472, 960
-// tokens 9.7, 11.8, 14.2, 18.2, 19.3 for 11.1, 16.0, 16.7, 18.8, 19.7 us; 16 times 40 behind 216, 472, 960 18.2, 23.0, 29.7 for 24.3, 31.1, 38.6;
-// 8 and 2 heads of 64 behind 472 15.2 for 13.7.
-__device__ __noinline__ int3 deal(int mine, int hkv, int c, int64_t even) {
+// Few query tiles: every share is one piece of one (tile, head).  Lists are cut into equal pieces of at most `len` key tiles, the least with
+// which there are shares enough.  A list that stays whole costs nothing besides; a piece has to be written and joined, which takes as long as
+// two to three key tiles, and more where the pieces are many (hence MANY).  So a list stays whole
+//   where no joining launch follows (the tables have no room for longer ones): always, it has at most WHOLE key tiles;
+//   else: of two key tiles, or where a cut would shorten it by no more than one.
+// Left to the line of cost: lists so unlike that the longest one left whole has more than FEW_OVER key tiles above an even share, and, since
+// equal pieces have no other advantage, cuts whose pieces have more than CUT_OVER above it (unless they are short: CUT_SHORT).
+// mine: key tiles of tile `lane`; even: a share of the line of cost; whole: key tiles of a list that is not cut.
+// Gives the share's tile (-1: none; -2: the line is better), the pieces of its list, and which one of the heads' pieces it is.  (Not inlined: it
+// runs once, and what lies between the roles moves them against the lines of the instruction cache.  Inlined, long steps took 2 % longer.)
+// Measured against the line (second figures), us in a graph, behind 0, 130, 300, 472, 960, 4000 tokens:
+//   40 new tokens, 32 and 8 heads of 128: 9.8 11.8 14.1 17.2 18.4 25.8 / 12.1 15.0 16.4 16.5 17.8 30.6; 8 and 2 heads of 64: 8.7 10.6 12.4 15.0 15.2 19.7 /
+//   11.1 13.2 13.5 14.4 14.7 22.0; 16 requests, 32 and 8 heads of 128: 13.9 15.8 18.1 22.7 29.1 82.5 / 13.9 17.6 22.5 30.9 37.7 87.5; 500 new tokens, 8 and 2
+//   heads of 64: 16.0 17.1 17.2 17.4 19.1 24.2 / 15.2 16.8 16.6 16.8 19.7 23.9.  Of 260 steps (1 to 16 requests, 40 or 500 new tokens, seven kinds of
+// heads of 64 and 128, behind 0 to 16000) the line takes more than 3 % longer at 131, up to 36 %, and less at 31, up to 6 % (lists of 4 to 8 key tiles cut
+// into single ones).
+__device__ __noinline__ int3 deal(int mine, int hkv, int c, int64_t even, int whole) {
   const int lane = threadIdx.x & 31;
   const int64_t all = int64_t(__reduce_add_sync(0xffffffffu, unsigned(mine))) * hkv;
   int len = max(1, int((all + SHARES - 1) / SHARES)), n;
   for (;; len += (len + 7) / 8) {
     const int at_most = mine > MANY ? max(2, len) : len;
-    n = mine <= WHOLE ? int(mine > 0) : (mine + at_most - 1) / at_most;
+    n = mine <= max(whole, len + 1) ? int(mine > 0) : (mine + at_most - 1) / at_most;
     if (int64_t(__reduce_add_sync(0xffffffffu, unsigned(n))) * hkv <= SHARES) break;  // (at the latest with a piece for each)
   }
-  if (len > max(int64_t(WHOLE), even + FEW_OVER)) return make_int3(-2, 0, 0);
+  const bool cut = __any_sync(0xffffffffu, n > 1);
+  if (len > (cut ? max(int64_t(CUT_SHORT), even + CUT_OVER) : max(int64_t(WHOLE), even + FEW_OVER))) return make_int3(-2, 0, 0);
   int upto = n * hkv;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -175,7 +183,7 @@ struct Walk {
         atomicExch(a.counts + 4, int(MV_ERR_INVALID_ARG));
         mine = 0;
       }
-      const int3 part = deal(mine, a.Hkv, c, total / SHARES);
+      const int3 part = deal(mine, a.Hkv, c, total / SHARES, a.join ? 2 : WHOLE);
       if (part.x >= -1) {
         t = n_tiles;
         if (part.x < 0) return;
@@ -1079,8 +1087,7 @@ mv_status launch(const Args& a, const void* q, const void* k8, const void* v8, c
     return MV_ERR_CUDA;
   const mv_status e = launch_after(chunk_attn_kernel<D>, dim3(SHARES), NT, Lay<D>::SMEM, st, a, tm_q, tm_k, tm_v);
   if (e != MV_OK) return e;
-  // where no list can be long enough to be cut there is nothing to join
-  if (a.max_tiles <= FEW && a.max_tiles * a.Hkv <= SHARES && a.max_entries <= WHOLE * KEYS) return MV_OK;
+  if (!a.join) return MV_OK;
   return launch_after(chunk_merge_kernel<D>, dim3(MERGE_CTAS), MERGE_WARPS * 32, 0, st, a);
 }
 
@@ -1132,6 +1139,9 @@ extern "C" mv_status mv_dag_chunk_attn_fp8_blk(const mv_chunk_tables* t, const m
   a.Hkv = g->n_kv_heads;
   a.G = G;
   a.R = BQ / G;
+  // where no list can be long enough to be cut there is nothing to join.  (The host knows the tables' capacities, not the step: tables made for
+  // steps that grow have the second launch, 2 us, in the short ones too.)
+  a.join = !(t->max_tiles <= FEW && t->max_tiles * g->n_kv_heads <= SHARES && t->max_entries <= WHOLE * KEYS);
   a.out_32 = (reinterpret_cast<uintptr_t>(out) & 31) == 0;
   a.scale_log2 = mv::softmax_scale(g) * 1.4426950408889634f;
   if (!std::isfinite(a.scale_log2)) return MV_ERR_INVALID_ARG;
