@@ -70,8 +70,8 @@ constexpr float FAR = 4096.f;
 constexpr int kMaxList = 1 << 26;       // pages of a list: its slots are counted in 32 bits
 constexpr int V_MIN = -80;              // a scale of zero (a block nobody has quantised) counts as 2^-80
 
-struct Cut {  // a cut (tile, head) at one end of a share
-  int item, row0, rows, ends;  // item: tile * Hkv + head, -1: none; ends: its last key tile is here
+struct alignas(16) Cut {  // the cut (tile, head)s at the ends of a share
+  int begun, item, row0, rows;  // item (tile * Hkv + head, -1: none) begun in an earlier share; one that goes on in a later share, its rows
 };
 
 struct Args {
@@ -82,7 +82,7 @@ struct Args {
   bf16* out;
   float* part_o;        // [2 SHARES][MAXQV][D]
   float2* part_ml;      // [2 SHARES][MAXQV]: reference (a score), sum
-  Cut* cuts;            // [2 SHARES]: item begun earlier, item that goes on in a later share
+  Cut* cuts;            // [SHARES]
   int64_t num_pages;
   int max_rows, max_tiles, max_entries;
   int Hq, Hkv, G, R;
@@ -93,7 +93,7 @@ struct Args {
 
 constexpr size_t part_o_bytes(int d) { return size_t(2) * SHARES * MAXQV * d * sizeof(float); }
 constexpr size_t part_ml_bytes() { return size_t(2) * SHARES * MAXQV * sizeof(float2); }
-constexpr size_t workspace_need(int d) { return part_o_bytes(d) + part_ml_bytes() + ((2 * SHARES * sizeof(Cut) + 255) & ~size_t(255)); }
+constexpr size_t workspace_need(int d) { return part_o_bytes(d) + part_ml_bytes() + ((SHARES * sizeof(Cut) + 255) & ~size_t(255)); }
 
 // A run of key tiles of one (query tile, KV head) inside a share.
 struct Segment {
@@ -102,7 +102,6 @@ struct Segment {
   int head, item;
   int k0, k1;              // key tiles
   int slot;                // partial result, or -1: all key tiles are here
-  bool ends;
 };
 
 // Few query tiles: every share is one piece of one (tile, head).  Lists are cut into equal pieces of at most `len` key tiles, the least with
@@ -240,8 +239,7 @@ struct Walk {
       s.item = t * a.Hkv + head;
       s.k0 = k;
       s.k1 = end;
-      s.ends = end == units;
-      s.slot = k == 0 && s.ends ? -1 : 2 * share + (k > 0 ? 0 : 1);
+      s.slot = k == 0 && end == units ? -1 : 2 * share + (k > 0 ? 0 : 1);
       k = end;
       return true;
     }
@@ -427,7 +425,7 @@ __device__ __forceinline__ void q_loader(const Cta& c, const CUtensorMap* map) {
   const bool lead = mv::um::elect_one();
   Walk w;
   w.begin(a, blockIdx.x);
-  Cut first{-1, 0, 0, 0}, last{-1, 0, 0, 0};
+  Cut cut{-1, -1, 0, 0};
   int n = 0, loads = 0;
   bool ok = true;
   for (bool more = true; ok && more; ++n) {
@@ -442,7 +440,10 @@ __device__ __forceinline__ void q_loader(const Cta& c, const CUtensorMap* map) {
     }
     __syncwarp();
     if (!more) break;
-    if (s.slot >= 0) (s.k0 > 0 ? first : last) = Cut{s.item, s.row0, s.rows, s.ends ? 1 : 0};
+    if (s.slot >= 0) {
+      if (s.k0 > 0) cut.begun = s.item;
+      else cut = Cut{cut.begun, s.item, s.row0, s.rows};
+    }
     ok = c.warp_wait(sh->q_empty, (n & 1) ^ 1);
     if (!ok) break;
     const int halves = s.rows > a.R ? 2 : 1;
@@ -455,11 +456,7 @@ __device__ __forceinline__ void q_loader(const Cta& c, const CUtensorMap* map) {
     ++loads;
     __syncwarp();
   }
-  if (lead) {  // the share's cut items, for the merge
-    int4* const cuts = reinterpret_cast<int4*>(a.cuts) + 2 * blockIdx.x;
-    cuts[0] = make_int4(first.item, first.row0, first.rows, first.ends);
-    cuts[1] = make_int4(last.item, last.row0, last.rows, last.ends);
-  }
+  if (lead) a.cuts[blockIdx.x] = cut;  // for the merge
   if (!ok && loads > 0 && lead) (void)mv::mbar_wait_bounded(bar(&sh->q_full), (loads - 1) & 1, 20000000ull);  // in flight
   __syncwarp();
 }
@@ -894,7 +891,7 @@ __global__ void __launch_bounds__(NT, 1) chunk_attn_kernel(const __grid_constant
   if ((base & 1023u) != 0) {  // the swizzle pattern is anchored at 1024-byte boundaries
     mv::grid_dependency_wait();
     if (tid == 0) atomicExch(a.counts + 4, int(MV_ERR_UNSUPPORTED));
-    if (tid < 2) reinterpret_cast<int4*>(a.cuts)[2 * blockIdx.x + tid] = make_int4(-1, 0, 0, 0);
+    if (tid == 0) a.cuts[blockIdx.x] = Cut{-1, -1, 0, 0};
     return;
   }
   if (tid == 0) {
@@ -961,14 +958,13 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32, 3) chunk_merge_kernel(const 
   // item that goes on behind a share; begun before it; the former's rows; shares that have one
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   mv::grid_dependency_wait();
-  const int4* const cuts = reinterpret_cast<const int4*>(a.cuts);
   static_assert(SHARES <= MERGE_WARPS * 32, "a thread per share");
   if (threadIdx.x < SHARES) {
-    const int4 own = __ldcg(cuts + 2 * threadIdx.x + 1);
-    s_own[threadIdx.x] = own.x;
-    s_row0[threadIdx.x] = own.y;
-    s_rows[threadIdx.x] = own.z;
-    s_more[threadIdx.x] = __ldcg(reinterpret_cast<const int*>(cuts + 2 * threadIdx.x));
+    const int4 cut = __ldcg(reinterpret_cast<const int4*>(a.cuts) + threadIdx.x);
+    s_more[threadIdx.x] = cut.x;
+    s_own[threadIdx.x] = cut.y;
+    s_row0[threadIdx.x] = cut.z;
+    s_rows[threadIdx.x] = cut.w;
   }
   if (threadIdx.x == 0) s_more[SHARES] = -1;
   const bool here = threadIdx.x < SHARES && s_own[threadIdx.x] >= 0;  // (its own word)
