@@ -96,13 +96,32 @@ def _stack_values(wl: synth.Workload, which: str, device, heads=None):
     return q, cat(ks, hkv), cat(vs, hkv)
 
 
+def _write_kv(plan, geom, form, q, k, v, q_rot, k_rot, k_pages, v_pages, stream=None):
+    """The plan's rotation and cache write, by a rotary form where there is one."""
+    args = (q, k, v, q_rot, k_rot, k_pages, v_pages, stream)
+    if form is None:
+        B.mv_rope_write_kv(plan, geom, *args)
+    else:
+        B.mv_rope_write_kv_form(plan, geom, form, *args)
+
+
+def _write_kv_fp8_blk(tables, geom, form, q, k, v, q_rot, k_pages, v_pages, kv_scale, stream=None):
+    """The same into the block-scaled 8-bit cache, from a step's tables."""
+    args = (q, k, v, q_rot, None, k_pages, v_pages, kv_scale, stream)
+    if form is None:
+        B.mv_rope_write_kv_fp8_blk(tables, geom, *args)
+    else:
+        B.mv_rope_write_kv_fp8_blk_form(tables, geom, form, *args)
+
+
 class DecodeState:
-    """Pools holding the history of a decode workload, plus this step's inputs, plan and workspace."""
+    """Pools holding the history of a decode workload, plus this step's inputs, plan and workspace.  ``form``: a rotary form in place of the
+    geometry's own, in history and step."""
 
     def __init__(self, wl: synth.Workload, device="cuda", chunk_tokens: int = 0, canary: bool = False,
-                 n_pool_copies: int = 1, heads=None):
+                 n_pool_copies: int = 1, heads=None, form=None):
         assert wl.kind == "decode"
-        self.wl, self.device = wl, device
+        self.wl, self.device, self.form = wl, device, form
         g, b = wl.geom, wl.batch
         if heads is not None:   # this process owns a slice of the KV heads, their query heads and their pools
             g = dataclasses.replace(g, n_q_heads=heads[1], n_kv_heads=heads[3])
@@ -119,7 +138,7 @@ class DecodeState:
         _, kh, vh = _stack_values(wl, "history", device, heads)
         hp = PlanOnDevice(hist, device, geom=g)
         for kp, vp in self.pools:
-            B.mv_rope_write_kv(hp.plan, self.geom, None, kh, vh, None, None, kp, vp)
+            _write_kv(hp.plan, self.geom, form, None, kh, vh, None, None, kp, vp)
         torch.cuda.synchronize()
         del kh, vh, hp
         self.q, self.k, self.v = _stack_values(wl, "new", device, heads)
@@ -131,13 +150,14 @@ class DecodeState:
 
     def step(self, pool: int = 0, stream=None):
         kp, vp = self.pools[pool]
-        B.mv_rope_write_kv(self.plan, self.geom, self.q, self.k, self.v, self.q_rot, None, kp, vp, stream)
+        _write_kv(self.plan, self.geom, self.form, self.q, self.k, self.v, self.q_rot, None, kp, vp, stream)
         B.mv_dag_decode_attn(self.plan, self.geom, self.q_rot, kp, vp, self.out, self.workspace, stream)
         return self.out
 
 
 class DecodeStateFP8(DecodeState):
-    """The same decode workload with the KV history in FP8 pools (8-bit floats, one scale per KV head)."""
+    """The same decode workload with the KV history in FP8 pools (8-bit floats, one scale per KV head).  No rotary forms: the write into these
+    pools knows the geometry's own rotation only."""
 
     def __init__(self, wl: synth.Workload, device="cuda", n_pool_copies: int = 1):
         assert wl.kind == "decode" and wl.geom.dtype == "bf16" and wl.geom.head_dim == 128
@@ -259,7 +279,7 @@ class ChunkStateFP8Blk:
                                   b.page_off, b.page_idx, b.page_size, b.num_pages, b.vis_mode, b.pos_mode)
             _, kh, vh = _stack_values(wl, "history", device)
             hs = StepOnDevice(hist, g.group, device, blocks=False)
-            self._write(hs.build(), None, kh, vh, None, None)
+            _write_kv_fp8_blk(hs.build(), self.geom, form, None, kh, vh, None, self.k_pages, self.v_pages, self.kv_scale)
             torch.cuda.synchronize()
             assert hs.read_status() == 0
             del kh, vh, hs
@@ -269,26 +289,20 @@ class ChunkStateFP8Blk:
         self.out = torch.empty_like(self.q)
         self.workspace = _dev_bytes(B.mv_chunk_attn_workspace_bytes(self.geom), device)
 
-    def _write(self, tables, q, k, v, q_rot, stream):
-        args = (q, k, v, q_rot, None, self.k_pages, self.v_pages, self.kv_scale, stream)
-        if self.form is None:
-            B.mv_rope_write_kv_fp8_blk(tables, self.geom, *args)
-        else:
-            B.mv_rope_write_kv_fp8_blk_form(tables, self.geom, self.form, *args)
-
     def step(self, stream=None):
         t = self.chunk.build(stream)
-        self._write(self.chunk.steps.tables, self.q, self.k, self.v, self.q_rot, stream)
+        _write_kv_fp8_blk(self.chunk.steps.tables, self.geom, self.form, self.q, self.k, self.v, self.q_rot, self.k_pages, self.v_pages, self.kv_scale, stream)
         B.mv_dag_chunk_attn_fp8_blk(t, self.geom, self.q_rot, self.k_pages, self.v_pages, self.kv_scale, self.out, self.workspace, stream)
         return self.out
 
 
 class DecodeStateFP8Blk(DecodeState):
-    """The same decode workload planned on the device, with the KV history in FP8 pools that carry a scale per (page, KV head)."""
+    """The same decode workload planned on the device, with the KV history in FP8 pools that carry a scale per (page, KV head).  ``form``: a
+    rotary form in place of the geometry's own."""
 
-    def __init__(self, wl: synth.Workload, device="cuda"):
+    def __init__(self, wl: synth.Workload, device="cuda", form=None):
         assert wl.kind == "decode" and wl.geom.dtype == "bf16"
-        self.wl, self.device = wl, device
+        self.wl, self.device, self.form = wl, device, form
         g, b = wl.geom, wl.batch
         self.local_geom = g
         self.geom = B.make_geom(g.n_q_heads, g.n_kv_heads, g.head_dim, b.num_pages, g.dtype, g.page_size, 0.0, g.rope_base)
@@ -299,7 +313,7 @@ class DecodeStateFP8Blk(DecodeState):
                               b.page_off, b.page_idx, b.page_size, b.num_pages, b.vis_mode, b.pos_mode)
         _, kh, vh = _stack_values(wl, "history", device)
         hs = StepOnDevice(hist, g.group, device, blocks=False)
-        B.mv_rope_write_kv_fp8_blk(hs.build(), self.geom, None, kh, vh, None, None, self.k_pages, self.v_pages, self.kv_scale)
+        _write_kv_fp8_blk(hs.build(), self.geom, form, None, kh, vh, None, self.k_pages, self.v_pages, self.kv_scale)
         torch.cuda.synchronize()
         assert hs.read_status() == 0
         del kh, vh, hs
@@ -311,7 +325,7 @@ class DecodeStateFP8Blk(DecodeState):
 
     def step(self, stream=None):
         t = self.steps.build(stream)
-        B.mv_rope_write_kv_fp8_blk(t, self.geom, self.q, self.k, self.v, self.q_rot, None, self.k_pages, self.v_pages, self.kv_scale, stream)
+        _write_kv_fp8_blk(t, self.geom, self.form, self.q, self.k, self.v, self.q_rot, self.k_pages, self.v_pages, self.kv_scale, stream)
         B.mv_dag_decode_attn_fp8_blk(t, self.geom, self.q_rot, self.k_pages, self.v_pages, self.kv_scale, self.out, self.workspace, stream)
         return self.out
 
@@ -336,11 +350,8 @@ class PrefillState:
         self.out = torch.empty_like(self.q)
 
     def step(self, stream=None, lse=None):
-        args = (self.q, self.k, self.v, self.q_rot, self.k_rot, self.k_pages if self.with_pool else None, self.v_pages if self.with_pool else None, stream)
-        if self.form is None:
-            B.mv_rope_write_kv(self.plan, self.geom, *args)
-        else:
-            B.mv_rope_write_kv_form(self.plan, self.geom, self.form, *args)
+        pools = (self.k_pages, self.v_pages) if self.with_pool else (None, None)
+        _write_kv(self.plan, self.geom, self.form, self.q, self.k, self.v, self.q_rot, self.k_rot, *pools, stream)
         B.mv_dag_prefill_attn(self.plan, self.geom, self.q_rot, self.k_rot, self.v, self.out, lse, stream)
         return self.out
 
