@@ -239,7 +239,8 @@ typedef enum {
   MV_ROPE_LINEAR = 1,  /* theta_i / factor                                                                    */
   MV_ROPE_BASE = 2,    /* with base * factor^(R / (R - 2)) for base: the slowest pair is stretched by factor, the fastest not */
   MV_ROPE_RAMP = 3     /* by the turns n = length * theta_i / (2 pi) a pair makes over the length it was trained on: with
-                          w = (n - slow) / (fast - slow), held in [0, 1], w theta_i + (1 - w) theta_i / factor            */
+                          w = (n - slow) / (fast - slow), held in [0, 1], w theta_i + (1 - w) theta_i / factor.  (Where a checkpoint's
+                          ramp runs over the pair's index i between two rounded bounds instead, write its angles into theta.)  */
 } mv_rope_scaling;
 
 /* Fills a form (host only).  factor is read unless the scaling is MV_ROPE_PLAIN; length, slow and fast with MV_ROPE_RAMP only.
@@ -310,6 +311,7 @@ mv_status mv_dag_decode_attn(const mv_plan* plan, const mv_attn_geom* geom, cons
  * to the format's rounding.  Inside the kernel the queries and the softmax weights are 8-bit floats as well (one scale
  * per q-vector; each as a rounded value plus a rounded remainder, about seven bits of mantissa), so that both products
  * run on the tensor cores' 8-bit path straight on the pool bytes.
+ * The write rotates as geom says; it has no counterpart that takes a rotary form.
  * MV_BF16 queries and outputs, head_dim 128, single-token steps only (max one new token per node); anything else is
  * MV_ERR_UNSUPPORTED.  Other errors as for mv_rope_write_kv and mv_dag_decode_attn. */
 mv_status mv_rope_write_kv_fp8(const mv_plan* plan, const mv_attn_geom* geom, const void* q, const void* k, const void* v,
@@ -464,8 +466,10 @@ mv_status mv_chunk_tables_read_status(const mv_chunk_tables* tables, void* cuda_
 /* Attention of every row of the tables over what it sees: for row r and query head h
  *   out[r][h] = sum_j softmax_j(sm_scale * <q_rot[r][h], K_j>) V_j.
  * The step's new tokens must be in the cache first.  Rows that no tile names are left as they were.  Single tokens are served as well
- * (mv_dag_decode_attn_fp8_blk is the faster call where no node receives more than a few, since there the rows of different nodes share
- * what they read).
+ * (mv_dag_decode_attn_fp8_blk is the faster call where no node receives more than about ten, since there the rows of different nodes share what they
+ * read, and the more accurate one: its weights keep more bits.  32 and 8 heads of 128, us, that call / this one, for 1, 4, 8, 16, 32 new tokens on each node:
+ * 16 requests with four branches each behind 2304 tokens 36, 66, 92, 149, 266 / 151, 152, 153, 155, 158; 64 requests behind 1088 60, 61, 76, 109, 183 / 86, 88, 88, 89, 92;
+ * one request with four branches 18, 26, 29, 31, 43 / 23, 23, 23, 24, 26).
  *   q_rot, out  device [max_rows][n_q_heads][head_dim] bf16, not overlapping;  pools, kv_scale as above
  *   workspace   device, 256-byte aligned, mv_chunk_attn_workspace_bytes(geom) bytes (it does not depend on the step); scratch, not to be
  *               shared by calls that may overlap on the device

@@ -11,7 +11,7 @@
 // exactly (three mantissa bits of seven, exponents within range), so a warpgroup turns the bytes of a tile into bf16 operands between
 // TMA and the products, and everything behind it is plain bf16 arithmetic with 32-bit accumulators: the byte's exponent
 // and mantissa are moved to the low end of a bf16 pattern, which is the value times 2^-120 (the format's subnormals are bf16 subnormals
-// there), and one multiplication by 2^(120 + e) brings the page's scale in.  Softmax weights are rounded to bf16 (2^-9 of each, as
+// there), and one multiplication by 2^(120 + e) brings the page's scale in.  Softmax weights are rounded to bf16 (off by at most 2^-8 of each, as
 // in the other prefill kernels); their sum is of the unrounded ones, in 32 bits.
 // A page whose scale is NaN: its keys become NaN, so the scores of whoever sees it; its values stay finite, so whoever does not
 // see it multiplies them by zero.
@@ -26,8 +26,9 @@
 // Every wait is bounded.
 //
 // Bound by the tensor cores for a long list: 2048 new tokens behind 64K, 32 query and 8 KV heads of 128, 2.2 * 10^12 operations, take
-// 1.99 to 2.36 ms from one GPU to the next, 67 to 56 % of the rate measured of a library product; a prompt with its DAG, 17 thousand
-// tokens, 64 and 8 heads, 3.08 ms, 62 %.  A key tile takes 3800 cycles, 2048 of them products of the two halves; the rest is the chain scores ->
+// 1.99 ms at 1965 MHz, 67 % of the rate measured of a library product in a burst; in a loop of seconds the power limit takes the clock to 1670 MHz:
+// 2.31 ms, 68 % of the rate of such products under that limit (2.25 to 2.37 from one GPU to the next).  A prompt with its DAG, 17 thousand tokens,
+// 64 and 8 heads: 3.04 to 3.1 ms, 62 %, and 3.4 (3.33 to 3.45), 67 %, at 1785 MHz.  A key tile takes 3800 cycles, 2048 of them products of the two halves; the rest is the chain scores ->
 // weights -> products of a half that the other half does not cover, and shared memory (320 KB to and fro a tile, 2500 cycles at 128 bytes a
 // cycle).  A (tile, head) item costs 14500 cycles besides (first tile, epilogue 5000).  Small steps are bound by latency:
 // 9.8 us for 40 new tokens alone (12 with a joining launch, where the tables have room for longer lists); 40 behind 960 18.4, behind 4000 25.8 (see deal).
@@ -48,7 +49,10 @@ using bf16 = __nv_bfloat16;
 constexpr int PS = 16, KEYS = 8;        // tokens of a page; pages of a key tile
 constexpr int BQ = 128, BK = 128;       // q-vectors of a half; keys of a tile
 constexpr int SHARES = 148;             // CTAs
-constexpr int SETUP = 2;                // cost of a (query tile, head) besides its key tiles
+// cost of a (query tile, head) besides its key tiles.  The cycles above would make it 3.8, but part of them passes beside the neighbours' key tiles:
+// 1, 2, 3, 4 give 39.5, 38.5, 40.7, 43.0 us for chunks on branches (heads of 64), 89.8, 92.4, 93.9, 93.3 for 16 prompts of 500 tokens, 61.5, 58.4, 53.9, 55.5 for
+// 64 times 40 tokens behind 300 (32 and 8 heads of 128); over 31 steps of both head sizes 1.006, 1, 1.002, 1.004 times as long.
+constexpr int SETUP = 2;
 constexpr int FEW = 32;                 // query tiles up to which a step may be dealt out in pieces (Walk::pieces)
 constexpr int WHOLE = 4, MANY = 16;     // key tiles of a list that stays whole where nothing is joined; of one whose pieces have two of them at least
 constexpr int FEW_OVER = 3, CUT_OVER = 1, CUT_SHORT = 6;  // key tiles: see deal
