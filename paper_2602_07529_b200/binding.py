@@ -233,6 +233,7 @@ class Plan:
     def __init__(self, batch=None, chunk_tokens: int = 0, n_kv_heads: int = 0, group_size: int = 0, sched_ctas: int = 0, geom=None):
         self._h = C.c_void_p(None)
         self._keep = None
+        self.index = None      # the GPU it was uploaded to
         if batch is not None:
             self.replan(batch, chunk_tokens, n_kv_heads, group_size, sched_ctas, geom)
 
@@ -289,6 +290,7 @@ class Plan:
     def upload(self, device_buf, stream=None):
         _check(lib.mv_plan_upload(self._h, _ptr(device_buf), device_buf.numel() * device_buf.element_size(),
                                   _stream_ptr(stream)), "mv_plan_upload")
+        self.index = device_buf.get_device()
 
     def read_status(self, stream=None) -> int:
         """Device status word of the last kernels run with this plan (0 = fine); synchronises the stream."""
@@ -519,6 +521,8 @@ def mv_rope_rotate(form: RopeForm, geom: _Geom, positions, q, k, q_out, k_out, b
     if k is not None and k.shape[0] != n:
         raise ValueError(f"q has {n} tokens, k {k.shape[0]}")
     i = some.get_device()
+    if isinstance(positions, Plan) and positions.index not in (None, i):
+        raise ValueError(f"the plan is on cuda:{positions.index}, the tensors on cuda:{i}")
     s = _launch_stream(i, stream)
     if isinstance(positions, Plan):
         ptr = C.c_void_p()

@@ -26,3 +26,39 @@ def test_a_single_token_has_no_stride():
     assert B._heads_at(one, "q", 1, 4, 64, torch.bfloat16, -1) == (room.data_ptr(), 256)
     assert B._heads_at(two, "q", 1, 4, 64, torch.bfloat16, -1) == (room.data_ptr(), 256)
     assert B._heads_at(two, "q", 2, 4, 64, torch.bfloat16, -1) == (room.data_ptr(), 1001)
+
+
+def test_a_plan_on_another_gpu_is_refused():
+    """The plan's positions are memory of the GPU it was uploaded to: a launch on another one must not read them."""
+    from paper_2602_07529_b200 import synth
+    wl = synth.config1()
+    plan = B.Plan(wl.batch)
+    assert plan.index is None       # not uploaded
+    plan.index = 3                  # as if on a GPU that the tensors are not on
+    form, geom = B.RopeForm(B.ROPE_HALVES, 64), B.make_geom(4, 2, 64, 0, "bf16")
+    q = heads(4, 4)
+    with pytest.raises(ValueError, match="plan is on cuda:3"):
+        B.mv_rope_rotate(form, geom, plan, q, None, q, None)
+
+
+class Uploads:
+    """A device buffer as far as Plan.upload looks at one."""
+
+    def __init__(self, index):
+        self.index = index
+
+    numel = element_size = data_ptr = lambda self: 0
+
+    def get_device(self):
+        return self.index
+
+
+def test_an_upload_says_where_the_plan_is(monkeypatch):
+    from paper_2602_07529_b200 import synth
+    plan = B.Plan(synth.config1().batch)
+    with pytest.raises(B.MvError):
+        plan.upload(Uploads(2), stream=0)      # too small: nothing is uploaded
+    assert plan.index is None
+    monkeypatch.setattr(B.lib, "mv_plan_upload", lambda *a: 0, raising=False)
+    plan.upload(Uploads(2), stream=0)
+    assert plan.index == 2
