@@ -28,7 +28,8 @@
 // Bound by the tensor cores for a long list: 2048 new tokens behind 64K, 32 query and 8 KV heads of 128, 2.2 * 10^12 operations, take
 // 1.99 ms at 1965 MHz, 67 % of the rate measured of a library product in a burst; in a loop of seconds the power limit takes the clock to 1670 MHz:
 // 2.31 ms, 68 % of the rate of such products under that limit (2.25 to 2.37 from one GPU to the next).  A prompt with its DAG, 17 thousand tokens,
-// 64 and 8 heads: 3.04 to 3.1 ms, 62 %, and 3.4 (3.33 to 3.45), 67 %, at 1785 MHz.  A key tile takes 3800 cycles, 2048 of them products of the two halves; the rest is the chain scores ->
+// 64 and 8 heads: 3.04 to 3.1 ms, 62 %, and 3.4 (3.33 to 3.45), 67 %, at 1785 MHz.
+// A key tile takes 3800 cycles, 2048 of them products of the two halves; the rest is the chain scores ->
 // weights -> products of a half that the other half does not cover, and shared memory (320 KB to and fro a tile, 2500 cycles at 128 bytes a
 // cycle).  A (tile, head) item costs 14500 cycles besides (first tile, epilogue 5000).  Small steps are bound by latency:
 // 9.8 us for 40 new tokens alone (12 with a joining launch, where the tables have room for longer lists); 40 behind 960 18.4, behind 4000 25.8 (see deal).
@@ -122,7 +123,7 @@ struct Segment {
 //   40 new tokens, 32 and 8 heads of 128: 9.8 11.8 14.1 17.2 18.4 25.8 / 12.1 15.0 16.4 16.5 17.8 30.6; 8 and 2 heads of 64: 8.7 10.6 12.4 15.0 15.2 19.7 /
 //   11.1 13.2 13.5 14.4 14.7 22.0; 16 requests, 32 and 8 heads of 128: 13.9 15.8 18.1 22.7 29.1 82.5 / 13.9 17.6 22.5 30.9 37.7 87.5; 500 new tokens, 8 and 2
 //   heads of 64: 16.0 17.1 17.2 17.4 19.1 24.2 / 15.2 16.8 16.6 16.8 19.7 23.9.  Of 260 steps (1 to 16 requests, 40 or 500 new tokens, seven kinds of
-// heads of 64 and 128, behind 0 to 16000) the line takes more than 3 % longer at 131, up to 36 %, and less at 31, up to 6 % (lists of 4 to 8 key tiles cut
+// heads of 64 and 128, behind 0 to 16000) the line takes more than 3 % longer at 131, up to 36 %, and less at 31, up to 6 % (mostly lists of 4 to 8 key tiles cut
 // into single ones).
 __device__ __noinline__ int3 deal(int mine, int hkv, int c, int64_t even, int whole) {
   const int lane = threadIdx.x & 31;

@@ -7,7 +7,8 @@
 // Bound by memory: every element is read and written once.  A CTA takes TPC tokens: their cosines and sines once into shared
 // memory (double-precision angles, rope.cuh), then all heads of q and k in 16-byte vectors, UNITS pieces in flight per thread.  As halves
 // a piece is two vectors, half the rotated part apart; as pairs it is one vector, which holds whole pairs, so neighbouring threads read neighbouring bytes.
-// Measured: 17K tokens, 32 query and 8 KV heads of 128, 349 MB, 60.5 to 64 us from one GPU to the next (83 to 88 % of the measured copy rate); on one GPU 4, 8, 16 tokens per CTA
+// Measured: 17K tokens, 32 query and 8 KV heads of 128, 349 MB, 60.5 to 64 us from one GPU to the next (83 to 88 % of the measured
+// copy rate); on one GPU 4, 8, 16 tokens per CTA
 // 65.0, 61.0, 66.6 us, four pieces in flight instead of two 62.5, vectors that do not pass L2 by 63.5.  64 tokens: 3.1 us in a graph, the rest
 // of a call is the host's.
 #include <algorithm>
